@@ -1,7 +1,8 @@
-"""Fused Sampling-VT (FlashBEV) and FlashSCA for AMD MI355X.
+"""Fused Sampling-VT (FlashBEV), FlashSCA and the operators around it in an
+encoder block for AMD MI355X.
 
-A thin Python binding over the C ABI of ``include/flashbev.h`` and
-``include/flashsca.h`` (``libflashbev.so``).  It only marshals arguments: every step of the
+A thin Python binding over the C ABI of ``include/flashbev.h``,
+``include/flashsca.h`` and ``include/flashblock.h`` (``libflashbev.so``).  It only marshals arguments: every step of the
 operator runs in the library's HIP kernel.  PyTorch supplies device memory
 and the current stream.  If the built library is missing the calls raise;
 there is no fallback implementation.
@@ -22,6 +23,7 @@ __all__ = [
     "launch_info", "backward_launch_info", "status_string", "abi_version", "library_path",
     "FlashBevError", "DTYPE_CODES", "REDUCE_CODES", "STATUS",
     "sample_vt_autograd", "sca_autograd",
+    "linear_forward", "linear_backward", "linear_autograd",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -1163,3 +1165,9 @@ def sca_autograd(value, lidar2img, anchors, grid: BevGrid, img_hw: Tuple[int, in
     camera matrices and anchors get none."""
     return _autograd_functions()["sca"].apply(value, lidar2img, offsets, logits, anchors, grid,
                                               img_hw, levels, heads, reduce)
+
+
+# ---------------------------------------------------------------------------
+# the operators around FlashSCA in an encoder block (include/flashblock.h)
+# ---------------------------------------------------------------------------
+from .block import linear_autograd, linear_backward, linear_forward  # noqa: E402

@@ -3,19 +3,22 @@
     python -m paper_2607_10071_amd.build
 
 Produces ``paper_2607_10071_amd/libflashbev.so`` (the fused Sampling-VT
-forward and backward behind the C ABI of ``include/flashbev.h``, and FlashSCA
-behind ``include/flashsca.h``) and
+forward and backward behind the C ABI of ``include/flashbev.h``, FlashSCA
+behind ``include/flashsca.h`` and the encoder block's product behind
+``include/flashblock.h``) and
 ``libflashbev_membench.so`` (the memory-ceiling micro-benchmarks of
 ``include/flashbev_membench.h`` that bench.py uses) and
 ``libflashbev_phases.so`` (the same operator library with the forward's
 phase clock compiled in, ``include/flashbev_phases.h``, for
-``python -m paper_2607_10071_amd.phases``).  The three compile in parallel.
+``python -m paper_2607_10071_amd.phases``, without the encoder block's
+operators).  The sources compile in parallel.
 """
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -23,6 +26,8 @@ ROOT = os.path.dirname(HERE)
 INCLUDE = os.path.join(ROOT, "include")
 SRC = os.path.join(HERE, "csrc", "flashbev.hip")
 SCA_SRC = os.path.join(HERE, "csrc", "flashsca.hip")
+# the operators around FlashSCA in an encoder block
+BLOCK_SRCS = [os.path.join(HERE, "csrc", f) for f in ("flashlinear.hip",)]
 LIB = os.path.join(HERE, "libflashbev.so")
 # memory-ceiling micro-benchmarks used by bench.py (not part of the operator)
 MEMBENCH_SRC = os.path.join(HERE, "csrc", "membench.hip")
@@ -52,8 +57,10 @@ def hipcc() -> str:
 
 
 def _compile(srcs, lib: str, verbose: bool, extra=()) -> str:
+    """One hipcc call: sources (or, with -c among ``extra``, one source) to ``lib``."""
     tmp = lib + ".tmp"
-    cmd = [hipcc(), *HIPCC_FLAGS, *extra, f"-I{INCLUDE}", *srcs, "-o", tmp]
+    flags = [f for f in HIPCC_FLAGS if f != "-shared" or "-c" not in extra]
+    cmd = [hipcc(), *flags, *extra, f"-I{INCLUDE}", *srcs, "-o", tmp]
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -87,13 +94,15 @@ def _build_c_abi_program(verbose: bool) -> str:
 def build(verbose: bool = False) -> str:
     """Compile the operator library, the micro-benchmark library and the
     C-ABI test program."""
-    with ThreadPoolExecutor(max_workers=3) as ex:
-        jobs = [ex.submit(_compile, [MEMBENCH_SRC], MEMBENCH_LIB, verbose),
-                ex.submit(_compile, [SRC, SCA_SRC], LIB, verbose),
-                ex.submit(_compile, [SRC, SCA_SRC], PHASES_LIB, verbose,
-                          ("-DFLASHBEV_PHASE_CLOCK",))]
-        lib = jobs[1].result()
-        for j in jobs:
+    srcs = [SRC, SCA_SRC, *BLOCK_SRCS]
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(max_workers=6) as ex:
+        jobs = [ex.submit(_compile, [s], os.path.join(tmp, os.path.basename(s) + ".o"), verbose,
+                          ("-c",)) for s in srcs]
+        others = [ex.submit(_compile, [MEMBENCH_SRC], MEMBENCH_LIB, verbose),
+                  ex.submit(_compile, [SRC, SCA_SRC], PHASES_LIB, verbose,
+                            ("-DFLASHBEV_PHASE_CLOCK",))]
+        lib = _compile([j.result() for j in jobs], LIB, verbose)
+        for j in others:
             j.result()
     _build_c_abi_program(verbose)
     return lib

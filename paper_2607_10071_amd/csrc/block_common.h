@@ -1,0 +1,146 @@
+// Helpers of the encoder block's operators: 16-byte vectors at any element
+// alignment, conversion of stored elements to float32 and back, and on the host
+// the byte ranges of strided tensors.
+#pragma once
+
+#include "flashblock.h"
+#include "hip_common.h"
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));   // 16 bytes at any 16-bit alignment
+
+// Rows of odd widths start at any element; gfx950 loads and stores 16 bytes at
+// any 2-byte address in one instruction.
+__device__ __forceinline__ u32x4 load16(const void *p)
+{
+    return *reinterpret_cast<const u32x4_any *>(p);
+}
+
+__device__ __forceinline__ void store16(void *p, u32x4 v)
+{
+    *reinterpret_cast<u32x4_any *>(p) = v;
+}
+
+constexpr int elem_size(int dt) { return dt == FLASHBEV_F32 ? 4 : 2; }
+
+// One stored element as float32 (exact) and a float32 rounded to it.
+template <int DT>
+__device__ __forceinline__ float load_elem(const void *p, int64_t i)
+{
+    if constexpr (DT == FLASHBEV_F32) {
+        return static_cast<const float *>(p)[i];
+    } else if constexpr (DT == FLASHBEV_F16) {
+        return (float)static_cast<const _Float16 *>(p)[i];
+    } else {
+        return (float)static_cast<const __bf16 *>(p)[i];
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ void store_elem(void *p, int64_t i, float v)
+{
+    if constexpr (DT == FLASHBEV_F32) {
+        static_cast<float *>(p)[i] = v;
+    } else if constexpr (DT == FLASHBEV_F16) {
+        static_cast<_Float16 *>(p)[i] = (_Float16)v;
+    } else {
+        static_cast<__bf16 *>(p)[i] = (__bf16)v;
+    }
+}
+
+// V consecutive elements (V times the element size is a multiple of 16 bytes)
+// as float32, in 16-byte vectors.
+template <int DT, int V>
+__device__ __forceinline__ void load_elems(const void *p, float (&v)[V])
+{
+    constexpr int E = 16 / elem_size(DT);
+    static_assert(V % E == 0, "whole vectors");
+#pragma unroll
+    for (int q = 0; q < V / E; ++q) {
+        const u32x4 r = load16(static_cast<const char *>(p) + 16 * q);
+        if constexpr (DT == FLASHBEV_F32) {
+            const f32x4 f = __builtin_bit_cast(f32x4, r);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * q + e] = f[e];
+        } else if constexpr (DT == FLASHBEV_BF16) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[8 * q + 2 * e] = __builtin_bit_cast(float, r[e] << 16);
+                v[8 * q + 2 * e + 1] = __builtin_bit_cast(float, r[e] & 0xffff0000u);
+            }
+        } else {
+            typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t w = r[e];
+                const h2 h = __builtin_bit_cast(h2, w);
+                v[8 * q + 2 * e] = (float)h[0];
+                v[8 * q + 2 * e + 1] = (float)h[1];
+            }
+        }
+    }
+}
+
+template <int DT, int V>
+__device__ __forceinline__ void store_elems(void *p, const float (&v)[V])
+{
+    constexpr int E = 16 / elem_size(DT);
+    static_assert(V % E == 0, "whole vectors");
+#pragma unroll
+    for (int q = 0; q < V / E; ++q) {
+        u32x4 r;
+        if constexpr (DT == FLASHBEV_F32) {
+            r = __builtin_bit_cast(u32x4, f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]});
+        } else if constexpr (DT == FLASHBEV_BF16) {
+            typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                r[e] = __builtin_bit_cast(uint32_t, b2{(__bf16)v[8 * q + 2 * e],
+                                                       (__bf16)v[8 * q + 2 * e + 1]});
+        } else {
+            typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                r[e] = __builtin_bit_cast(uint32_t, h2{(_Float16)v[8 * q + 2 * e],
+                                                       (_Float16)v[8 * q + 2 * e + 1]});
+        }
+        store16(static_cast<char *>(p) + 16 * q, r);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+inline bool ranges_overlap(const void *a, uint64_t na, const void *b, uint64_t nb)
+{
+    if (!na || !nb || !a || !b) return false;
+    const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+    return a0 < b0 + nb && b0 < a0 + na;
+}
+
+// bytes from the first to the last element of `rows` rows at a stride
+inline uint64_t span_bytes(int64_t rows, int64_t ld, int64_t width, int es)
+{
+    return rows <= 0 || width <= 0 ? 0 : ((uint64_t)(rows - 1) * ld + width) * es;
+}
+
+inline bool finite_value(float v) { return v == v && v - v == 0.0f; }
+
+inline bool known_dtype(int dt) { return dt >= FLASHBEV_F32 && dt <= FLASHBEV_BF16; }
+
+inline bool misaligned(const void *p, int a) { return ((uintptr_t)p & (uintptr_t)(a - 1)) != 0; }
+
+template <class P>
+int launch_kernel(const void *fn, uint64_t blocks, int threads, P &p, size_t lds, hipStream_t st)
+{
+    if (blocks == 0) return FLASHBEV_OK;
+    if (blocks > 0x7fffffffull) return FLASHBEV_ERR_UNSUPPORTED;
+    void *args[] = {&p};
+    return hipLaunchKernel(fn, dim3((unsigned)blocks), dim3(threads), args, lds, st) == hipSuccess
+               ? FLASHBEV_OK : FLASHBEV_ERR_HIP;
+}
+
+}  // namespace

@@ -1,0 +1,275 @@
+"""The linear operator on the GPU against float64, over odd sizes, types, strides and
+activations; its gradients against the formulas' and against differences."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+import torch  # noqa: E402
+
+import block_ref as ref  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def fb():
+    import paper_2607_10071_amd as m
+    return m
+
+
+def rand(gen, *shape, dtype=torch.float32, std=1.0):
+    return (torch.randn(shape, generator=gen) * std).to(dtype)
+
+
+def make(seed, M, K, N, dtype, out_dtype, bias=True, residual=True):
+    gen = torch.Generator().manual_seed(seed)
+    x = rand(gen, M, K, dtype=dtype)
+    w = rand(gen, N, K, dtype=dtype, std=max(K, 1) ** -0.5)
+    b = rand(gen, N, dtype=dtype) if bias else None
+    r = rand(gen, M, N, dtype=out_dtype) if residual else None
+    return x, w, b, r
+
+
+def dev(*ts):
+    return [None if t is None else t.to("cuda") for t in ts]
+
+
+# one row to a few tiles; widths below, at and past a granule, a step and a tile
+SIZES = [(1, 1, 1), (1, 64, 64), (1, 4096, 257), (2, 7, 5), (5, 8192, 40), (16, 129, 33), (17, 32, 32),
+         (31, 515, 777), (33, 136, 1000), (64, 72, 8), (65, 65, 65), (127, 256, 129), (128, 128, 128),
+         (129, 31, 127), (300, 200, 130), (529, 32, 32), (1000, 1000, 72), (257, 8, 520), (4099, 64, 136)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,K,N", SIZES)
+def test_forward_sizes(fb, device, M, K, N, dtype):
+    dt = ref.DTYPES[dtype]
+    x, w, b, r = make(M * 7 + K, M, K, N, dt, dt)
+    want, pre, e, e_pre = ref.linear(x, w, b, "none", r, 0.5)
+    xd, wd, bd, rd = dev(x, w, b, r)
+    got_pre = torch.empty(M, N, dtype=dt, device=device)
+    got = fb.linear_forward(xd, wd, bd, residual=rd, scale=0.5, pre=got_pre)
+    assert got.dtype == dt and got.shape == (M, N)
+    ref.close(got, want, e)
+    ref.close(got_pre, pre, e_pre)
+    again = fb.linear_forward(xd, wd, bd, residual=rd, scale=0.5)
+    assert torch.equal(got, again)
+
+
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("f16", "f32"),
+                                       ("bf16", "f32")])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("M,K,N", [(3, 96, 70), (150, 65, 131), (7, 4096, 48)])
+def test_forward_epilogues(fb, device, M, K, N, act, dtype, out):
+    dt, odt = ref.DTYPES[dtype], ref.DTYPES[out]
+    for bias, residual, scale in ((True, True, -1.5), (False, False, 1.0)):
+        x, w, b, r = make(11 * M, M, K, N, dt, odt, bias, residual)
+        w = w * 3   # activations away from zero too
+        want, _, e, _ = ref.linear(x, w, b, act, r, scale)
+        xd, wd, bd, rd = dev(x, w, b, r)
+        got = fb.linear_forward(xd, wd, bd, act, rd, scale, out_dtype=odt)
+        assert got.dtype == odt
+        ref.close(got, want, e)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(1, 32, 32), (9, 33, 17), (140, 257, 150), (40, 2056, 24)])
+def test_forward_strides(fb, device, M, K, N, dtype):
+    """Rows inside wider tensors, at odd element offsets, with what lies around the
+    output left as it was; the residual in place."""
+    dt = ref.DTYPES[dtype]
+    x, w, b, r = make(5, M, K, N, dt, dt)
+    want, pre, e, e_pre = ref.linear(x, w, b, "silu", r, 1.0)
+
+    def inside(t, before, after):
+        big = torch.full((t.shape[0] + 2, before + t.shape[1] + after), float("nan"), dtype=dt,
+                         device=device)
+        view = big[1:-1, before:before + t.shape[1]]
+        view.copy_(t)
+        return big, view
+
+    _, xv = inside(x, 3, 5)
+    _, wv = inside(w, 1, 0)
+    big, rv = inside(r, 7, 2)
+    pbig, pv = inside(torch.zeros_like(r), 1, 1)
+    bb = torch.full((N + 2,), float("nan"), dtype=dt, device=device)
+    bb[1:-1] = b.to(device)
+    got = fb.linear_forward(xv, wv, bb[1:-1], "silu", rv, out=rv, pre=pv)
+    assert got is rv
+    ref.close(rv, want, e)
+    ref.close(pv, pre, e_pre)
+    for t, lo in ((big, 7), (pbig, 1)):
+        keep = torch.ones_like(t, dtype=torch.bool)
+        keep[1:-1, lo:lo + N] = False
+        assert t[keep].isnan().all()
+
+
+def test_forward_leading_dimensions(fb, device):
+    x = torch.randn(2, 3, 5, 16, device=device)
+    w = torch.randn(24, 16, device=device)
+    out = fb.linear_forward(x, w)
+    assert out.shape == (2, 3, 5, 24)
+    assert torch.equal(out.reshape(-1, 24), fb.linear_forward(x.reshape(-1, 16), w))
+    assert torch.equal(out[0, 0, 0], fb.linear_forward(x[0, 0, 0], w))
+    half = x[..., :8]   # rows at a stride of 16 over all leading dimensions
+    assert torch.equal(fb.linear_forward(half, w[:, :8]), fb.linear_forward(half.contiguous(),
+                                                                           w[:, :8].contiguous()))
+
+
+def test_nan_and_infinity_stay_in_their_rows(fb, device):
+    """A row of NaN or infinities reaches its own row of the output alone, and a
+    channel of the weight its own channel, whatever shares their tiles."""
+    for dt in ref.DTYPES.values():
+        for M, K, N in ((70, 37, 45), (6, 1029, 45), (200, 128, 130)):
+            x, w, b, _ = make(3, M, K, N, dt, dt)
+            xd, wd, bd = dev(x, w, b)
+            clean = fb.linear_forward(xd, wd, bd, "relu")
+            xd[2] = float("nan")
+            xd[4, K - 1] = float("inf")
+            wd2 = wd.clone()
+            wd2[N - 1] = float("nan")
+            got = fb.linear_forward(xd, wd2, bd, "relu")
+            keep = torch.ones(M, N, dtype=torch.bool, device=device)
+            keep[2] = keep[4] = False
+            keep[:, N - 1] = False
+            assert torch.equal(got[keep], clean[keep])
+            assert got[2].isnan().all() and got[:, N - 1].isnan().all()
+
+
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("M,K,N", [(1, 8, 8), (1, 70, 3), (13, 33, 65), (130, 256, 129), (515, 40, 777),
+                                   (3000, 72, 48)])
+def test_backward(fb, device, M, K, N, act, dtype, out):
+    dt, odt = ref.DTYPES[dtype], ref.DTYPES[out]
+    x, w, _, g = make(M + K, M, K, N, dt, odt)
+    pre = rand(torch.Generator().manual_seed(9), M, N, dtype=dt, std=1.5)
+    for scale in (1.0, 0.5):
+        formed = act != "none" or dt != odt
+        want = ref.linear_grads(g, x, w, pre, act, scale, dt, formed)
+        xd, wd, gd, pd = dev(x, w, g, pre)
+        got = fb.linear_backward(gd, xd, wd, pd, act, scale)
+        for k in ("x", "weight", "bias"):
+            assert got[k].dtype == dt
+            ref.close(got[k], *want[k])
+        again = fb.linear_backward(gd, xd, wd, pd, act, scale)
+        assert all(torch.equal(got[k], again[k]) for k in got)
+
+
+def test_backward_wanted_gradients_and_strides(fb, device):
+    x, w, _, g = make(2, 77, 50, 90, torch.bfloat16, torch.bfloat16)
+    xd, wd, gd = dev(x, w, g)
+    full = fb.linear_backward(gd, xd, wd)
+    for k in full:
+        one = fb.linear_backward(gd, xd, wd, want=(k,))
+        assert torch.equal(one[k], full[k]) and all(v is None for n, v in one.items() if n != k)
+    # rows inside wider tensors, what lies around them left as it was
+    gx = torch.full((77, 61), 7.0, dtype=torch.bfloat16, device=device)
+    gw = torch.full((90, 53), 7.0, dtype=torch.bfloat16, device=device)
+    gb = torch.full((95,), 7.0, dtype=torch.bfloat16, device=device)
+    r = fb.linear_backward(gd, xd, wd, grad_x=gx[:, 3:53], grad_weight=gw[:, 1:51], grad_bias=gb[2:92])
+    assert torch.equal(gx[:, 3:53], full["x"]) and torch.equal(gw[:, 1:51], full["weight"])
+    assert torch.equal(gb[2:92], full["bias"]) and r["x"].data_ptr() == gx[:, 3:53].data_ptr()
+    assert (gx[:, :3] == 7).all() and (gx[:, 53:] == 7).all() and (gw[:, 0] == 7).all()
+    assert (gw[:, 51:] == 7).all() and (gb[:2] == 7).all() and (gb[92:] == 7).all()
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+def test_backward_against_differences(fb, device, act):
+    """<grad, v> against (L(+h v) - L(-h v)) / 2h in float32, L = <out, g>.  With h =
+    2^-5 and unit inputs: the third derivative of L along v is at most about 4 of
+    the activations' (2 at most) times |v x|^3, and each of the two L is off by
+    (K + 4) 2^-24 of its terms' magnitude, the quotient 1 / h of that."""
+    M, K, N, h = 37, 24, 29, 2.0 ** -5
+    x, w, b, g = make(4, M, K, N, torch.float32, torch.float32)
+    xd, wd, bd, gd = dev(x, w, b, g)
+    pre = torch.empty(M, N, device=device)
+    fb.linear_forward(xd, wd, bd, act, pre=pre)
+    if act == "relu":   # no sum within a step of the kink
+        keep = (pre.abs() > 1.0).float()
+        gd = gd * keep
+    grads = fb.linear_backward(gd, xd, wd, pre, act)
+    gen = torch.Generator().manual_seed(8)
+    for k, t in (("x", xd), ("weight", wd), ("bias", bd)):
+        v = rand(gen, *t.shape).to(device)
+        v = v / (v.norm() / t.shape[0] ** 0.5)   # a step of about h in each sum
+
+        def loss(s):
+            ins = {"x": xd, "weight": wd, "bias": bd}
+            ins[k] = t + s * v
+            o = fb.linear_forward(ins["x"], ins["weight"], ins["bias"], act)
+            return (o.double() * gd.double()).sum()
+
+        num = float((loss(h) - loss(-h)) / (2 * h))
+        ana = float((grads[k].double() * v.double()).sum())
+        step = {"x": lambda: v @ wd.t(), "weight": lambda: xd @ v.t(),
+                "bias": lambda: v.expand(M, N)}[k]().double()
+        trunc = h * h / 6 * 2.0 * float((gd.double().abs() * step.abs() ** 3).sum())
+        mag = float((gd.double().abs() * (xd.double().abs() @ wd.double().abs().t()
+                                          + bd.double().abs() + 1)).sum())
+        rounding = (K + 24) * ref.F32 * mag / h
+        if act == "relu":
+            assert float((step.abs() * (gd != 0)).max()) * h < 1.0
+        assert abs(num - ana) <= trunc + rounding, (k, num, ana, trunc, rounding)
+
+
+@pytest.mark.parametrize("act", ["none", "gelu", "relu"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_autograd_is_the_explicit_calls(fb, device, act, dtype):
+    dt = ref.DTYPES[dtype]
+    x, w, b, r = make(6, 90, 48, 72, dt, dt)
+    leaves = [t.requires_grad_() for t in dev(x, w, b, r)]
+    out = fb.linear_autograd(*leaves[:3], act, leaves[3], 0.5)
+    g = torch.randn_like(out)
+    got = torch.autograd.grad(out, leaves, g)
+    xd, wd, bd, rd = dev(x, w, b, r)
+    pre = torch.empty_like(rd)
+    assert torch.equal(out.detach(), fb.linear_forward(xd, wd, bd, act, rd, 0.5, pre=pre))
+    want = fb.linear_backward(g, xd, wd, pre, act, 0.5)
+    assert torch.equal(got[0], want["x"]) and torch.equal(got[1], want["weight"])
+    assert torch.equal(got[2], want["bias"]) and torch.equal(got[3], g)
+    # a gradient that is one number at a stride of zero
+    leaves = [t.detach().requires_grad_() for t in dev(x, w, b)]
+    one = torch.autograd.grad(fb.linear_autograd(*leaves, act).sum(), leaves)
+    pre = torch.empty_like(rd)
+    fb.linear_forward(xd, wd, bd, act, pre=pre)
+    want = fb.linear_backward(torch.ones_like(rd), xd, wd, pre, act)
+    assert all(torch.equal(a, want[k]) for a, k in zip(one, ("x", "weight", "bias")))
+    # only what needs a gradient
+    w2 = wd.clone().requires_grad_()
+    fb.linear_autograd(xd, w2, bd, act).sum().backward()
+    assert torch.equal(w2.grad, one[1])
+
+
+def test_autograd_second_derivative_is_refused(fb, device):
+    x = torch.randn(4, 8, device=device, requires_grad=True)
+    w = torch.randn(8, 8, device=device)
+    (g,) = torch.autograd.grad(fb.linear_autograd(x, w, None, "gelu").sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
+def test_empty(fb, device):
+    for dt in ref.DTYPES.values():
+        for M, K, N in ((0, 8, 8), (8, 8, 0), (3, 0, 5), (0, 0, 0)):
+            x, w, b = (torch.ones(s, dtype=dt, device=device) for s in ((M, K), (N, K), (N,)))
+            out = fb.linear_forward(x, w, b, "relu")
+            assert out.shape == (M, N) and (out == 1).all()
+            r = fb.linear_backward(torch.ones(M, N, dtype=dt, device=device), x, w)
+            assert r["x"].shape == (M, K) and r["weight"].shape == (N, K)
+            assert (r["x"] == N).all() and (r["weight"] == M).all() and (r["bias"] == M).all()
+
+
+def test_long_rows_past_32_bits(fb, device):
+    """x and out past 2^32 bytes: the last rows are their own products."""
+    M, K, N = (1 << 23) + 5, 320, 8
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device=device)
+    x[-5:] = torch.randn(5, K, device=device).to(torch.bfloat16)
+    w = torch.randn(N, K, device=device).to(torch.bfloat16)
+    out = fb.linear_forward(x, w)
+    assert torch.equal(out[-5:], fb.linear_forward(x[-5:], w)) or torch.allclose(
+        out[-5:].float(), fb.linear_forward(x[-5:], w).float(), rtol=2.0 ** -7, atol=2.0 ** -7)
+    assert (out[:-5] == 0).all()
+    g = torch.ones(M, N, dtype=torch.bfloat16, device=device)
+    r = fb.linear_backward(g, x, w)
+    want = x[-5:].double().sum(0)
+    assert ((r["weight"].double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-5).all()
+    assert (r["bias"].float() == float(torch.tensor(float(M)).to(torch.bfloat16))).all()
