@@ -37,7 +37,7 @@
 
 #include <stdint.h>
 
-#include "flashbev.h"
+#include "../flashbev.h"
 
 #ifdef __cplusplus
 extern "C" {

@@ -2,7 +2,7 @@
 encoder block for AMD MI355X.
 
 A thin Python binding over the C ABI of ``include/flashbev.h``,
-``include/flashsca.h`` and ``include/flashblock.h`` (``libflashbev.so``).  It only marshals arguments: every step of the
+``include/flashsca.h`` and ``include/block/flashblock.h`` (``libflashbev.so``).  It only marshals arguments: every step of the
 operator runs in the library's HIP kernel.  PyTorch supplies device memory
 and the current stream.  If the built library is missing the calls raise;
 there is no fallback implementation.
@@ -1168,6 +1168,6 @@ def sca_autograd(value, lidar2img, anchors, grid: BevGrid, img_hw: Tuple[int, in
 
 
 # ---------------------------------------------------------------------------
-# the operators around FlashSCA in an encoder block (include/flashblock.h)
+# the operators around FlashSCA in an encoder block (include/block/flashblock.h)
 # ---------------------------------------------------------------------------
 from .block import linear_autograd, linear_backward, linear_forward  # noqa: E402

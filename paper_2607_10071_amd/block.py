@@ -1,4 +1,4 @@
-"""The operators around FlashSCA in an encoder block (``include/flashblock.h``):
+"""The operators around FlashSCA in an encoder block (``include/block/flashblock.h``):
 the matrix product with bias, activation and residual in its epilogue.
 
 As in the package's other calls, this only marshals arguments: every product and

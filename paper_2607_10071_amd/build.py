@@ -5,7 +5,7 @@
 Produces ``paper_2607_10071_amd/libflashbev.so`` (the fused Sampling-VT
 forward and backward behind the C ABI of ``include/flashbev.h``, FlashSCA
 behind ``include/flashsca.h`` and the encoder block's product behind
-``include/flashblock.h``) and
+``include/block/flashblock.h``) and
 ``libflashbev_membench.so`` (the memory-ceiling micro-benchmarks of
 ``include/flashbev_membench.h`` that bench.py uses) and
 ``libflashbev_phases.so`` (the same operator library with the forward's

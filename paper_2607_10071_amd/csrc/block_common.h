@@ -3,7 +3,7 @@
 // the byte ranges of strided tensors.
 #pragma once
 
-#include "flashblock.h"
+#include "block/flashblock.h"
 #include "hip_common.h"
 
 namespace {

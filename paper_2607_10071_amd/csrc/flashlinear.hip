@@ -1,5 +1,5 @@
 // The matrix product with bias, activation and residual in its epilogue, and
-// its gradients, for AMD MI355X (gfx950).  C ABI: include/flashblock.h.
+// its gradients, for AMD MI355X (gfx950).  C ABI: include/block/flashblock.h.
 //
 // Three products, one kernel.  With an operand's rows over the reduction axis
 // ("along") or its columns ("across"),

@@ -1,6 +1,10 @@
 """The linear operator's argument checks (CPU only): every refusal comes before any
 HIP call, so device addresses here are numbers that nothing reads."""
 import ctypes
+import os
+import re
+import shutil
+import subprocess
 
 import pytest
 import torch
@@ -8,6 +12,8 @@ import torch
 import paper_2607_10071_amd as fb
 from paper_2607_10071_amd import block
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "block", "flashblock.h")
 S = fb.STATUS
 BASE = 0x7F0000000000
 MB = 1 << 20
@@ -27,6 +33,31 @@ def backward(args, g=BASE, x=BASE + MB, w=BASE + 2 * MB, pre=0, gx=BASE + 3 * MB
              gw=BASE + 4 * MB, ldgw=32, gb=BASE + 5 * MB, ws=BASE + 6 * MB, wsb=1 << 30):
     return fb._packed_call("flashblock_linear_backward", "PPPPPPQPQPPQP")(
         args, g, x, w, pre, gx, ldgx, gw, ldgw, gb, ws, wsb, 0)
+
+
+def test_the_library_exports_what_the_header_declares():
+    src = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"\b(flashblock_\w+)\s*\(", src))
+    out = subprocess.run(["nm", "-D", "--defined-only", fb.library_path()], capture_output=True,
+                         text=True, check=True).stdout
+    assert names and set(re.findall(r" T (flashblock_\w+)", out)) == names
+
+
+def test_header_is_plain_c(tmp_path):
+    if not shutil.which("gcc"):
+        pytest.skip("gcc not found")
+    c = tmp_path / "t.c"
+    c.write_text('#include "block/flashblock.h"\nint main(void) { return sizeof(flashblock_linear) != 72; }\n')
+    exe = str(tmp_path / "t")
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Wextra", "-Werror", "-pedantic",
+                    "-I" + os.path.join(ROOT, "include"), str(c), "-o", exe], check=True)
+    subprocess.run([exe], check=True)
+
+
+def test_header_constants():
+    src = open(HEADER).read()
+    for k, v in block.ACTIVATIONS.items():
+        assert re.search(rf"FLASHBLOCK_ACT_{k.upper()} = {v}\b", src), k
 
 
 def test_packed_structure_is_the_c_one():
