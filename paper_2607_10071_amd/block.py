@@ -1,8 +1,9 @@
 """The operators around FlashSCA in an encoder block (``include/block/flashblock.h``):
-the matrix product with bias, activation and residual in its epilogue.
+the matrix product with bias, activation and residual in its epilogue, and the
+norms before and after a block with its gate and residual scale.
 
-As in the package's other calls, this only marshals arguments: every product and
-gradient runs in the library's HIP kernels.
+As in the package's other calls, this only marshals arguments: every product, norm
+and gradient runs in the library's HIP kernels.
 """
 from __future__ import annotations
 
@@ -13,9 +14,12 @@ from . import (FlashBevError, _dtype_code, _on_device, _one_device,
                _packed_call, _stream_handle, _workspace)
 
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+NORMS = {"none": 0, "layer": 1, "rms": 2}
 
 # The C structures as packed bytes (see the package's other calls).
 _PACK_LINEAR = struct.Struct("@6q5if")
+_PACK_NORM = struct.Struct("@6q6i2f")
+_PACK_VECTORS = struct.Struct("@5P")
 
 
 class Linear(ctypes.Structure):
@@ -25,7 +29,15 @@ class Linear(ctypes.Structure):
                 ("out_dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
-assert _PACK_LINEAR.size == ctypes.sizeof(Linear)
+class Norm(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("ldx", ctypes.c_int64), ("ldr", ctypes.c_int64),
+                ("lds", ctypes.c_int64), ("ldy", ctypes.c_int64), ("groups", ctypes.c_int64),
+                ("C", ctypes.c_int32), ("dtype", ctypes.c_int32), ("stream_dtype", ctypes.c_int32),
+                ("param_dtype", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("post_norm", ctypes.c_int32), ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+assert _PACK_LINEAR.size == ctypes.sizeof(Linear) and _PACK_NORM.size == ctypes.sizeof(Norm)
 
 
 def _rows(t, name: str):
@@ -240,6 +252,183 @@ def linear_backward(grad_out, x, weight, pre=None, activation="none", scale: flo
     return outs
 
 
+_VECTORS = ("gate", "weight", "bias", "post_weight", "post_bias")
+
+
+def _norm_code(kind, name: str) -> int:
+    try:
+        return NORMS[kind or "none"]
+    except KeyError:
+        raise ValueError(f"{name} must be one of {tuple(NORMS)}") from None
+
+
+def _norm_vectors(x, gate, weight, bias, post_weight, post_bias):
+    """(samples, dtype code, packed addresses) of a norm call's vectors."""
+    import torch
+
+    C = x.shape[-1]
+    groups, dtype = 1, None
+    for t in (gate, weight, bias, post_weight, post_bias):
+        if t is None:
+            continue
+        if dtype is None:
+            dtype = t.dtype
+            if dtype != x.dtype and dtype != torch.float32:
+                raise ValueError(f"gate, weights and biases must be {x.dtype} or torch.float32")
+        elif t.dtype != dtype:
+            raise ValueError("gate, weights and biases must have one dtype")
+    if gate is not None and gate.dim() == 2:
+        if x.dim() < 2 or tuple(gate.shape) != (x.shape[0], C):
+            raise ValueError(f"gate must be [{C}] or, one row for each of x's first dimension, "
+                             f"[{x.shape[0]}, {C}]")
+        if not gate.is_cuda or not gate.is_contiguous():
+            raise ValueError("gate must be a contiguous device tensor")
+        groups = gate.shape[0]
+        g = gate.data_ptr()
+    else:
+        g = _vector(gate, "gate", dtype, C)
+    ptrs = (g, _vector(weight, "weight", dtype, C), _vector(bias, "bias", dtype, C),
+            _vector(post_weight, "post_weight", dtype, C), _vector(post_bias, "post_bias", dtype, C))
+    return groups or 1, dtype, _PACK_VECTORS.pack(*ptrs)
+
+
+def _adds_nothing(x, residual, gate, scale, post_norm, out_s) -> bool:
+    """Whether s is x itself."""
+    return residual is None and gate is None and scale == 1.0 and not _norm_code(
+        post_norm, "post_norm") and (out_s is None)
+
+
+def norm_forward(x, weight=None, bias=None, residual=None, gate=None, scale: float = 1.0,
+                 norm="layer", post_norm=None, post_weight=None, post_bias=None, eps: float = 1e-5,
+                 out=None, out_s=None, stream=None):
+    """The norms around a block, on the GPU:
+
+        u = N_post(x) post_weight + post_bias        (x without ``post_norm``)
+        s = residual + (scale * gate) * u
+        y = N(s) weight + bias                       (None without ``norm``)
+
+    x            CUDA tensor [..., C] (float32, float16 or bfloat16): a block's
+                 output, rows at any one row stride.
+    weight, bias, post_weight, post_bias
+                 optional [C], in x's dtype or float32 (one for all vectors).
+    residual     optional [..., C] in x's dtype or float32: the stream that the
+                 block is added to.  s has its dtype (x's without it).
+    gate         optional [C], or [G, C] with x [G, ..., C]: a row for each
+                 sample.
+    scale        residual scale.
+    norm, post_norm
+                 "layer", "rms" or None; one of them at least.
+    eps          of both norms.
+    out, out_s   optional tensors to write y and s into; ``out_s`` may be
+                 ``residual``.
+    stream       as in the package's other calls.
+
+    N(s) reads s as it is stored.  Returns (y, s); s is x itself where nothing
+    changes it.  Asynchronous.
+    """
+    import torch
+
+    M, ldx = _rows(x, "x")
+    code = _dtype_code(x)
+    kind, post = _norm_code(norm, "norm"), _norm_code(post_norm, "post_norm")
+    C = x.shape[-1]
+    groups, pdt, vectors = _norm_vectors(x, gate, weight, bias, post_weight, post_bias)
+    sdt = residual.dtype if residual is not None else x.dtype
+    if sdt != x.dtype and sdt != torch.float32:
+        raise ValueError(f"residual must be {x.dtype} or torch.float32")
+    ldr = lds = ldy = C
+    if residual is not None:
+        _same(residual, "residual", sdt, x.shape)
+        ldr = _rows(residual, "residual")[1]
+    same = kind and _adds_nothing(x, residual, gate, scale, post_norm, out_s)
+    if out_s is not None:
+        _same(out_s, "out_s", sdt, x.shape)
+        lds = _rows(out_s, "out_s")[1]
+    elif not same:
+        out_s = torch.empty(x.shape, dtype=sdt, device=x.device)
+    if not kind:
+        if out is not None:
+            raise ValueError("out needs a norm")
+    elif out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _same(out, "out", x.dtype, x.shape)
+        ldy = _rows(out, "out")[1]
+    args = _PACK_NORM.pack(M, ldx, ldr, lds, ldy, groups, C, code, code if sdt == x.dtype else 0,
+                           code if pdt is None or pdt == x.dtype else 0, kind, post, eps, scale)
+    dev = _one_device(x, weight, bias, residual, gate, post_weight, post_bias, out, out_s)
+    s = _stream_handle(stream, dev)
+    call = _packed_call("flashblock_norm_forward", "PPPPPPP")
+    with _on_device(dev):
+        rc = call(args, vectors, x.data_ptr(), _addr(residual), _addr(out_s), _addr(out), s)
+    if rc != 0:
+        raise FlashBevError(rc, "flashblock_norm_forward")
+    return out, x if same else out_s
+
+
+def norm_backward(grad_y, grad_s, x, s, weight=None, gate=None, scale: float = 1.0, norm="layer",
+                  post_norm=None, post_weight=None, post_bias=None, eps: float = 1e-5, want=("x",),
+                  stream=None):
+    """The gradients of ``norm_forward`` for ``grad_y`` (in x's dtype) and
+    ``grad_s`` (in the stream's), either of which may be None.
+
+    x, s     the forward's input and its second result.
+    want     which of "x", "residual", "gate", "weight", "bias", "post_weight" and
+             "post_bias"; the vectors' gradients come in the vectors' dtype
+             (x's, where no vector is given).
+
+    Returns a dict of those gradients.  Asynchronous.
+    """
+    import torch
+
+    M, ldx = _rows(x, "x")
+    code = _dtype_code(x)
+    kind, post = _norm_code(norm, "norm"), _norm_code(post_norm, "post_norm")
+    C = x.shape[-1]
+    groups, pdt, vectors = _norm_vectors(x, gate, weight, None, post_weight, post_bias)
+    pdt = pdt or x.dtype
+    sdt = s.dtype
+    if sdt != x.dtype and sdt != torch.float32:
+        raise ValueError(f"s must be {x.dtype} or torch.float32")
+    _same(s, "s", sdt, x.shape)
+    lds = _rows(s, "s")[1]
+    ldgy = ldgs = C
+    if grad_y is not None:
+        _same(grad_y, "grad_y", x.dtype, x.shape)
+        ldgy = _rows(grad_y, "grad_y")[1]
+    if grad_s is not None:
+        _same(grad_s, "grad_s", sdt, x.shape)
+        ldgs = _rows(grad_s, "grad_s")[1]
+    outs = {}
+    for k in want:
+        if k == "x":
+            outs[k] = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        elif k == "residual":
+            outs[k] = torch.empty(x.shape, dtype=sdt, device=x.device)
+        elif k not in _VECTORS:
+            raise ValueError(f"want takes 'x', 'residual' and {_VECTORS}")
+        elif k == "gate":
+            outs[k] = torch.empty((C,) if gate is None else gate.shape, dtype=pdt, device=x.device)
+        else:
+            outs[k] = torch.empty(C, dtype=pdt, device=x.device)
+    if not outs:
+        return outs
+    args = _PACK_NORM.pack(M, ldx, ldgs, lds, ldgy, groups, C, code, code if sdt == x.dtype else 0,
+                           code if pdt == x.dtype else 0, kind, post, eps, scale)
+    grads = _PACK_VECTORS.pack(*(_addr(outs.get(k)) for k in _VECTORS))
+    dev = _one_device(grad_y, grad_s, x, s, weight, gate, post_weight, post_bias)
+    st = _stream_handle(stream, dev)
+    need = _size("flashblock_norm_backward_workspace_size", "PPP", args, grads)
+    ws = _workspace(need, dev, st) if need else None
+    call = _packed_call("flashblock_norm_backward", "PPPPPPPQPQPPQP")
+    with _on_device(dev):
+        rc = call(args, vectors, _addr(grad_y), _addr(grad_s), x.data_ptr(), s.data_ptr(),
+                  _addr(outs.get("x")), C, _addr(outs.get("residual")), C, grads, _addr(ws), need, st)
+    if rc != 0:
+        raise FlashBevError(rc, "flashblock_norm_backward")
+    return outs
+
+
 # ---------------------------------------------------------------------------
 # autograd
 # ---------------------------------------------------------------------------
@@ -286,7 +475,34 @@ def _autograd_functions():
                 r = linear_backward(_as_rows(grad_out), x, weight, pre, activation, scale, want)
             return (r["x"], r["weight"], r["bias"], grad_out if needs[3] else None, None, None, None)
 
+    class _Norm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, residual, gate, weight, bias, post_weight, post_bias, scale, norm,
+                    post_norm, eps):
+            ctx.set_materialize_grads(False)
+            y, s = norm_forward(x, weight, bias, residual, gate, scale, norm, post_norm, post_weight,
+                                post_bias, eps)
+            same = s is x
+            ctx.save_for_backward(x, None if same else s, weight, gate, post_weight, post_bias)
+            ctx.meta = (scale, norm, post_norm, eps)
+            return y, None if same else s
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, grad_y, grad_s):
+            x, s, weight, gate, post_weight, post_bias = ctx.saved_tensors
+            scale, norm, post_norm, eps = ctx.meta
+            names = ("x", "residual", "gate", "weight", "bias", "post_weight", "post_bias")
+            r = dict.fromkeys(names)
+            if grad_y is not None or grad_s is not None:
+                want = tuple(k for k, n in zip(names, ctx.needs_input_grad) if n)
+                grads = (None if g is None else _as_rows(g) for g in (grad_y, grad_s))
+                r.update(norm_backward(*grads, x, x if s is None else s, weight, gate, scale, norm,
+                                       post_norm, post_weight, post_bias, eps, want))
+            return (*(r[k] for k in names), None, None, None, None)
+
     _AUTOGRAD["linear"] = _Linear
+    _AUTOGRAD["norm"] = _Norm
     return _AUTOGRAD
 
 
@@ -297,3 +513,13 @@ def linear_autograd(x, weight, bias=None, activation="none", residual=None, scal
     that need them."""
     return _autograd_functions()["linear"].apply(x, weight, bias, residual, activation, scale,
                                                  out_dtype)
+
+
+def norm_autograd(x, weight=None, bias=None, residual=None, gate=None, scale: float = 1.0,
+                  norm="layer", post_norm=None, post_weight=None, post_bias=None, eps: float = 1e-5):
+    """``norm_forward`` as a differentiable function of x, residual, gate, weights
+    and biases; the gradients are ``norm_backward``'s, computed only for the inputs
+    that need them."""
+    y, s = _autograd_functions()["norm"].apply(x, residual, gate, weight, bias, post_weight, post_bias,
+                                               scale, norm, post_norm, eps)
+    return y, x if s is None else s

@@ -94,3 +94,115 @@ def linear_grads(g, x, w, pre, name, scale, dtype, formed):
            "weight": (d.t() @ x, ed.t() @ x.abs() + (M + 4) * F32 * (dm.t() @ x.abs())),
            "bias": (d.sum(0), (e32 + (M + 4) * F32 * dm).sum(0))}
     return out
+
+
+# ---- norms -----------------------------------------------------------------------------------
+
+# A row's sums: 16 terms in a lane, then at most six lane exchanges and 16
+# wavefronts, plus the roundings of the terms themselves.
+DEPTH = 48
+
+
+def stats(v, kind, eps):
+    """(vhat, r, bound of vhat's float32 value, relative bound of r's)."""
+    v = v.double()
+    mean = v.mean(-1, keepdim=True) if kind == "layer" else torch.zeros_like(v[..., :1])
+    em = DEPTH * F32 * v.abs().mean(-1, keepdim=True) if kind == "layer" else torch.zeros_like(mean)
+    d = v - mean
+    var = (d * d).mean(-1, keepdim=True) + eps
+    r = 1 / torch.sqrt(var)
+    # the mean's error is second order in the variance: sum d is 0
+    dr = (DEPTH / 2 + 4) * F32 + (em * em + 2 * em * DEPTH * F32 * d.abs().mean(-1, keepdim=True)) / var
+    return d * r, r, r * (em + F32 * d.abs()) + (d * r).abs() * (dr + 2 * F32), dr
+
+
+def normed(v, kind, eps, weight, bias):
+    """(N(v) weight + bias, bound)."""
+    h, _, e, _ = stats(v, kind, eps)
+    if weight is not None:
+        h, e = h * weight.double(), e * weight.double().abs()
+    e = e + 3 * F32 * h.abs()
+    if bias is not None:
+        h = h + bias.double()
+        e = e + F32 * (bias.double().abs() + h.abs())
+    return h, e
+
+
+def stream(x, residual, gate, scale, kind, pw, pb, eps):
+    """(s before its rounding, bound, u, bound of u)."""
+    u, eu = (normed(x, kind, eps, pw, pb) if kind else (x.double(), torch.zeros_like(x.double())))
+    f = factor(gate, scale, x)
+    s = f * u
+    e = f.abs() * eu + 3 * F32 * s.abs()
+    if residual is not None:
+        s = s + residual.double()
+        e = e + 2 * F32 * s.abs()
+    return s, e, u, eu
+
+
+def factor(gate, scale, x):
+    """scale * gate over x's rows [M, C]."""
+    if gate is None:
+        return torch.full_like(x.double(), scale)
+    g = gate.double()
+    if g.dim() == 2:
+        g = g.repeat_interleave(x.shape[0] // g.shape[0], 0)
+    return scale * g.expand(x.shape)
+
+
+def norm_grad(h, eh, v, kind, eps):
+    """r (h - mean(h) - vhat mean(h vhat)) and its bound, `eh` that of h."""
+    vh, r, ev, dr = stats(v, kind, eps)
+    m1 = h.mean(-1, keepdim=True) if kind == "layer" else torch.zeros_like(r)
+    m2 = (h * vh).mean(-1, keepdim=True)
+    out = r * (h - m1 - vh * m2)
+    a = h.abs().mean(-1, keepdim=True) if kind == "layer" else torch.zeros_like(r)
+    b = (h * vh).abs().mean(-1, keepdim=True)
+    am = eh.mean(-1, keepdim=True) if kind == "layer" else torch.zeros_like(r)
+    e = r * (eh + am + vh.abs() * (eh * vh.abs()).mean(-1, keepdim=True)
+             + ev * b + vh.abs() * (h.abs() * ev).mean(-1, keepdim=True)
+             + DEPTH * F32 * (h.abs() + a + vh.abs() * b))
+    return out, e + out.abs() * dr + 4 * F32 * r * (h.abs() + a + vh.abs() * b)
+
+
+def norm_grads(gy, gs, x, s, gate, scale, norm, weight, post, pw, pb, eps):
+    """{name: (gradient, bound)} of rows [M, C]."""
+    M = x.shape[0]
+    zero = torch.zeros_like(x.double())
+    ds, eds = (gs.double() if gs is not None else zero), zero
+    out = {}
+    if norm and gy is not None:
+        g = gy.double()
+        h = g * (weight.double() if weight is not None else 1.0)
+        t, e = norm_grad(h, F32 * h.abs(), s, norm, eps)
+        sh, _, es, _ = stats(s, norm, eps)
+        out["weight"] = total(g * sh, g.abs() * es, M)
+        out["bias"] = total(g, zero, M)
+        ds = ds + t
+        eds = e + 2 * F32 * (ds.abs() + t.abs())
+    out["residual"] = (ds, eds)
+    f = factor(gate, scale, x)
+    du = f * ds
+    edu = f.abs() * eds + 3 * F32 * du.abs()
+    u, eu = normed(x, post, eps, pw, pb) if post else (x.double(), zero)
+    dg, edg = scale * ds * u, abs(scale) * (eds * u.abs() + ds.abs() * eu + eds * eu)
+    G = gate.shape[0] if gate is not None and gate.dim() == 2 else 0
+    if G:
+        parts = [total(a, b, M // G) for a, b in zip(dg.chunk(G), edg.chunk(G))]
+        out["gate"] = tuple(torch.stack(p) for p in zip(*parts))
+    else:
+        out["gate"] = total(dg, edg, M)
+    if post:
+        xh, _, ex, _ = stats(x, post, eps)
+        out["post_weight"] = total(du * xh, edu * xh.abs() + du.abs() * ex, M)
+        out["post_bias"] = total(du, edu, M)
+        h = pw.double() if pw is not None else 1.0
+        out["x"] = norm_grad(du * h, edu * abs(h) + F32 * (du * h).abs(), x, post, eps)
+    else:
+        out["x"] = (du, edu)
+    return out
+
+
+def total(v, e, n):
+    """A sum over rows in float32 and its bound."""
+    return v.sum(0), e.sum(0) + (n + 24) * F32 * (v.abs() + e).sum(0)
