@@ -53,14 +53,13 @@ __device__ __forceinline__ void store_elem(void *p, int64_t i, float v)
 
 // V consecutive elements (V times the element size is a multiple of 16 bytes)
 // as float32, in 16-byte vectors.
-template <int DT, int V>
-__device__ __forceinline__ void load_elems(const void *p, float (&v)[V])
+template <int DT, int W, int V>
+__device__ __forceinline__ void elems_of(const u32x4 (&raw)[W], float (&v)[V])
 {
-    constexpr int E = 16 / elem_size(DT);
-    static_assert(V % E == 0, "whole vectors");
+    static_assert(V * elem_size(DT) == W * 16, "whole vectors");
 #pragma unroll
-    for (int q = 0; q < V / E; ++q) {
-        const u32x4 r = load16(static_cast<const char *>(p) + 16 * q);
+    for (int q = 0; q < W; ++q) {
+        const u32x4 r = raw[q];
         if constexpr (DT == FLASHBEV_F32) {
             const f32x4 f = __builtin_bit_cast(f32x4, r);
 #pragma unroll
@@ -82,6 +81,16 @@ __device__ __forceinline__ void load_elems(const void *p, float (&v)[V])
             }
         }
     }
+}
+
+template <int DT, int V>
+__device__ __forceinline__ void load_elems(const void *p, float (&v)[V])
+{
+    constexpr int W = V * elem_size(DT) / 16;
+    u32x4 raw[W];
+#pragma unroll
+    for (int q = 0; q < W; ++q) raw[q] = load16(static_cast<const char *>(p) + 16 * q);
+    elems_of<DT>(raw, v);
 }
 
 template <int DT, int V>

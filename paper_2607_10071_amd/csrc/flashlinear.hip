@@ -25,18 +25,57 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // ---------------------------------------------------------------------------
 // activations
 // ---------------------------------------------------------------------------
-constexpr float kSqrtHalf = 0.70710678118654752f;
+// On the hardware's exp2 and reciprocal (one unit in the last place each): an
+// output of 40000 x 1024 gelus is 41 M of them, and the library's erff, expf and
+// IEEE division took longer than the product before them (119 us of the whole
+// call, and 80 with these).
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSqrt2OverPi = 0.79788456080286536f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
+
+__device__ __forceinline__ float sigmoid(float v)
+{
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * v));
+}
+
+// v, or the nearest of -m and m: factors of terms that are 0 there, so that an
+// infinite v does not make them NaN
+__device__ __forceinline__ float within(float v, float m)
+{
+    return __builtin_fminf(__builtin_fmaxf(v, -m), m);
+}
+
+// erfc(|v| / sqrt 2) = t P(t) exp(-v^2 / 2) with t = 1 / (1 + 0.43 |v| / sqrt 2): P is
+// the polynomial of degree 7 with the least relative error over |v| <= 17
+// (1.8e-7), found by weighted least squares in float64.  `e` gets the exponential.
+// From erfc of |v| neither tail of gelu cancels.
+__device__ __forceinline__ float erfc_half(float v, float &e)
+{
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(v), 0.30405591591021541f, 1.0f));
+    e = __builtin_amdgcn_exp2f(v * v * (-0.5f * kLog2e));
+    float q = 0.070911642f;
+    q = __builtin_fmaf(q, t, -0.299038637f);
+    q = __builtin_fmaf(q, t, 0.364747453f);
+    q = __builtin_fmaf(q, t, -0.068830498f);
+    q = __builtin_fmaf(q, t, 0.238214638f);
+    q = __builtin_fmaf(q, t, 0.207467761f);
+    q = __builtin_fmaf(q, t, 0.243988763f);
+    q = __builtin_fmaf(q, t, 0.242538700f);
+    return q * t * e;
+}
 
 __device__ __forceinline__ float act_value(int act, float v)
 {
     switch (act) {
     case FLASHBLOCK_ACT_RELU: return v > 0.0f ? v : (v == v ? 0.0f : v);
-    case FLASHBLOCK_ACT_GELU: return 0.5f * v * (1.0f + erff(v * kSqrtHalf));
-    case FLASHBLOCK_ACT_GELU_TANH:
-        return 0.5f * v * (1.0f + tanhf(kSqrt2OverPi * (v + 0.044715f * v * v * v)));
-    case FLASHBLOCK_ACT_SILU: return v / (1.0f + expf(-v));
+    case FLASHBLOCK_ACT_GELU: {
+        float e;
+        const float h = 0.5f * __builtin_fminf(__builtin_fabsf(v), 20.0f) * erfc_half(v, e);
+        return v > 0.0f ? v - h : -h;   // (erfc is 0 at 20 already)
+    }
+    case FLASHBLOCK_ACT_GELU_TANH:   // (1 + tanh z) / 2 = 1 / (1 + exp(-2 z))
+        return v * sigmoid(2.0f * kSqrt2OverPi * v * __builtin_fmaf(0.044715f, v * v, 1.0f));
+    case FLASHBLOCK_ACT_SILU: return v * sigmoid(v);
     default: return v;
     }
 }
@@ -45,16 +84,20 @@ __device__ __forceinline__ float act_slope(int act, float v)
 {
     switch (act) {
     case FLASHBLOCK_ACT_RELU: return v > 0.0f ? 1.0f : 0.0f;
-    case FLASHBLOCK_ACT_GELU:
-        return 0.5f * (1.0f + erff(v * kSqrtHalf)) + v * kInvSqrt2Pi * expf(-0.5f * v * v);
+    case FLASHBLOCK_ACT_GELU: {
+        float e;
+        const float h = 0.5f * erfc_half(v, e);
+        return __builtin_fmaf(within(v, 20.0f) * kInvSqrt2Pi, e, v > 0.0f ? 1.0f - h : h);
+    }
     case FLASHBLOCK_ACT_GELU_TANH: {
-        const float t = tanhf(kSqrt2OverPi * (v + 0.044715f * v * v * v));
-        return 0.5f * (1.0f + t) +
-               0.5f * v * (1.0f - t * t) * kSqrt2OverPi * (1.0f + 0.134145f * v * v);
+        const float p = sigmoid(2.0f * kSqrt2OverPi * v * __builtin_fmaf(0.044715f, v * v, 1.0f));
+        const float w = within(v, 20.0f);
+        return __builtin_fmaf(w * p * (1.0f - p), 2.0f * kSqrt2OverPi * __builtin_fmaf(0.134145f, w * w, 1.0f),
+                              p);
     }
     case FLASHBLOCK_ACT_SILU: {
-        const float p = 1.0f / (1.0f + expf(-v));
-        return p * (1.0f + v * (1.0f - p));
+        const float p = sigmoid(v);
+        return p * __builtin_fmaf(within(v, 100.0f), 1.0f - p, 1.0f);
     }
     default: return 1.0f;
     }
@@ -170,9 +213,9 @@ __device__ __forceinline__ void epilogue(const Epilogue &e, int64_t m, int n, in
 // lane's share of four 32x32x2 MFMAs (MFMA q takes element q of both operands'
 // granules, so the reduction index runs in the same order on both sides).
 //
-// LDS layout.  Along: row i holds its 8 granules, granule g at place g ^ (i & 7),
-// so that 8 lanes reading the same granule of 8 rows hit 8 different 16-byte
-// places.  Across: row r of the reduction axis holds the tile's columns.  16-bit
+// LDS layout.  Along: row i holds its 8 granules, granule g at place g ^ (i / 2 & 7),
+// so that 16 lanes reading the same granule of 16 rows use all 64 banks (rows are
+// 32 banks long).  Across: row r of the reduction axis holds the tile's columns.  16-bit
 // columns are read transposed (ds_read_b64_tr_b16: 16 lanes take a 4 x 16 block
 // and each ends with one column's 4 rows); the 32-byte column blocks of row r
 // stand at places XORed with (r & 3) + 4 (r >> 3 & 1), so that the 8 rows that one
@@ -208,14 +251,26 @@ __device__ __forceinline__ void mma(f32x16 &c, const u32x4 &a, const u32x4 &b)
     }
 }
 
-// 16 bytes at element `i` of a row that ends at element `end`; zeros past it
+// 16 bytes at element `i` of a row that ends at element `end`, zeros past it: the
+// row's last 16 bytes where they begin before `i`, shifted down.
 template <int DT>
 __device__ __forceinline__ u32x4 load_granule_edge(const char *row, int i, int end)
 {
-    constexpr int E = 16 / elem_size(DT);
+    constexpr int ES = elem_size(DT), E = 16 / ES;
     u32x4 v = {0, 0, 0, 0};
-    if (i + E <= end) {
-        v = load16(row + (int64_t)i * elem_size(DT));
+    if (end >= E) {
+        const int at = min(i, end - E);
+        v = load16(row + (int64_t)at * ES);
+        const int shift = (i - at) * ES * 8;   // bits
+        uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+        if (shift >= 64) {
+            lo = shift < 128 ? hi >> (shift - 64) : 0;
+            hi = 0;
+        } else if (shift > 0) {
+            lo = lo >> shift | hi << (64 - shift);
+            hi >>= shift;
+        }
+        v = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
     } else {
 #pragma unroll
         for (int q = 0; q < E; ++q) {
@@ -223,13 +278,15 @@ __device__ __forceinline__ u32x4 load_granule_edge(const char *row, int i, int e
             if constexpr (DT == FLASHBEV_F32) {
                 v[q] = reinterpret_cast<const uint32_t *>(row)[i + q];
             } else {
-                v[q >> 1] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[i + q]
-                             << (16 * (q & 1));
+                v[q >> 1] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[i + q] << (16 * (q & 1));
             }
         }
     }
     return v;
 }
+
+// the place of an "along" row's granules (see above)
+__device__ __forceinline__ int along_swizzle(int row) { return row >> 1 & 7; }
 
 // One operand's tile of R rows (or columns) of C on its way from memory to LDS.
 template <int DT, bool ACROSS, int R, int NT>
@@ -286,7 +343,7 @@ struct Tile {
             const int q = tid + i * NT;
             const int row = q / GPR, g = q % GPR;
             int place = g;
-            if constexpr (!ACROSS) place = g ^ (row & 7);
+            if constexpr (!ACROSS) place = g ^ along_swizzle(row);
             else if constexpr (ES == 2) place = g ^ (swizzle(row) << 1);
             *reinterpret_cast<u32x4 *>(lds + (row * GPR + place) * 16) = v[i];
         }
@@ -298,7 +355,7 @@ struct Tile {
         const int h = lane >> 5;
         if constexpr (!ACROSS) {
             const int row = c0 + (lane & 31), g = 2 * kk + h;
-            return *reinterpret_cast<const u32x4 *>(lds + (row * 8 + (g ^ (row & 7))) * 16);
+            return *reinterpret_cast<const u32x4 *>(lds + (row * 8 + (g ^ along_swizzle(row))) * 16);
         } else if constexpr (ES == 2) {
             const int j = lane & 15;
             const int pair = (c0 >> 4) + (lane >> 4 & 1);
@@ -423,6 +480,423 @@ __global__ void __launch_bounds__(WM *WN * 64) linear_tiles(Gemm p)
                 epilogue<DT>(p.e, m, n, p.cols, v);
         }
         wave_lds_sync();
+    }
+}
+
+// ---------------------------------------------------------------------------
+// the streamed product: rows at 16-byte places, widths of whole granules
+// ---------------------------------------------------------------------------
+// As linear_tiles, with three differences.  Granules go from memory to LDS
+// without passing registers (global_load_lds), into a ring of S stages, S - 1 of
+// them in flight.  A workgroup takes tile after tile, and the ring runs on over
+// the border: the next tile's first steps load while this one's results are
+// written.  And the MFMA's operands are swapped, so that a lane ends with one row's
+// columns: two half-wavefront swaps of neighbouring groups of four give it 8
+// consecutive ones, which need no pass through LDS.
+//
+// Granules past the reduction axis's end come from 16 bytes of zeros.
+__device__ const uint32_t kZeros[4] = {0, 0, 0, 0};
+
+// 16 bytes of each lane to LDS at `lds` + 16 lane.  Written in assembly, without
+// registers to be written: the compiler would wait for every load in flight before
+// the next LDS read, whichever stage it reads.
+__device__ __forceinline__ void to_lds(const void *base, uint32_t off, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :: "s"(lds), "v"(off), "s"(base) : "memory");
+}
+
+__device__ __forceinline__ void to_lds(const void *p, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :: "s"(lds), "v"(p) : "memory");
+}
+
+// Until at most N vector memory operations are in flight: s_waitcnt with vmcnt N
+// (bits 3..0 and 15..14) and no other limit.  Not in assembly: the compiler has to
+// know that its own loads are back, or it waits for them inside the loop.
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    static_assert(N < 64, "vmcnt");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70);
+    asm volatile("" ::: "memory");
+}
+
+// One operand's granules of a tile: where they are read from and what of a step is there.
+template <int DT, bool ACROSS, int R, int NT>
+struct Stream {
+    using T = Tile<DT, ACROSS, R, NT>;
+    static constexpr int G = T::G;
+    static constexpr int ES = T::ES, E = T::E, KT = T::KT;
+    static constexpr int STEP = NT / T::GPR;     // LDS rows between a lane's granules
+    static_assert(STEP % (!ACROSS ? 16 : ES == 2 ? 16 : 1) == 0, "a lane's granules share one swizzle");
+
+    // a lane's byte offsets from its tile's first row (along) or column (across)
+    static __device__ __forceinline__ void offsets(uint32_t (&off)[G], int64_t ld, int c0, int cend,
+                                                   int tid)
+    {
+        const int row = tid / T::GPR, place = tid % T::GPR;
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const int r = row + i * STEP;
+            if constexpr (!ACROSS) {
+                const int g = place ^ along_swizzle(row);
+                off[i] = (uint32_t)(min(c0 + r, cend - 1) - c0) * (uint32_t)ld + g * 16;
+            } else {
+                const int g = ES == 2 ? place ^ (T::swizzle(row) << 1) : place;
+                off[i] = (uint32_t)r * (uint32_t)ld + (uint32_t)(min(c0 + g * E, cend - E) - c0) * ES;
+            }
+        }
+    }
+
+    static __device__ __forceinline__ const char *at(const char *p, int64_t ld, int c0, int r0)
+    {
+        return ACROSS ? p + (int64_t)r0 * ld + (int64_t)c0 * ES : p + (int64_t)c0 * ld + (int64_t)r0 * ES;
+    }
+
+    static __device__ __forceinline__ void load(const char *base, const uint32_t (&off)[G], uint32_t lds)
+    {
+#pragma unroll
+        for (int i = 0; i < G; ++i) to_lds(base, off[i], lds + i * NT * 16);
+    }
+
+    // a step that holds `left` < KT elements of the reduction axis
+    static __device__ __forceinline__ void load_last(const char *base, const uint32_t (&off)[G],
+                                                     uint32_t lds, int left, int tid)
+    {
+        const int row = tid / T::GPR, place = tid % T::GPR;
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const bool there = ACROSS ? row + i * STEP < left : (place ^ along_swizzle(row)) * E < left;
+            to_lds(there ? base + off[i] : reinterpret_cast<const char *>(kZeros), lds + i * NT * 16);
+        }
+    }
+};
+
+// The MFMA leaves a lane with four groups of four columns of a row in each block
+// (group k: columns 8 k + 4 (lane / 32) ..); swapping halves of the wavefront
+// between groups 2 q and 2 q + 1 makes them columns 16 q + 8 (lane / 32) .. + 7.
+__device__ __forceinline__ void columns_of(const f32x16 &acc, int q, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float x = acc[8 * q + i], y = acc[8 * q + 4 + i];
+        const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x),
+                                                        __builtin_bit_cast(unsigned, y), false, false);
+        const unsigned a = r[0], b = r[1];
+        v[i] = __builtin_bit_cast(float, a);
+        v[4 + i] = __builtin_bit_cast(float, b);
+    }
+}
+
+// A wavefront's epilogue, its blocks' first row and column at (m, n).  Loads and
+// stores come back in one order, so a load behind a store waits for it (with each
+// vector's bias read before its store, these waits were two thirds of a 256-long
+// product's time): the bias and the residual of the first row blocks are read first
+// (of all, where there are two), each further one before its predecessor's stores.
+// The scheduling barriers keep the compiler from working on all vectors at once, which
+// spilled.
+template <int DT, int ODT, int ACT, bool FULL, int FM, int FN>
+__device__ __forceinline__ void write_tile(const Gemm &p, int m, int n, int lane,
+                                           const f32x16 (&acc)[FM][FN])
+{
+    constexpr int ES = elem_size(DT), OS = elem_size(ODT);
+    constexpr int BW = ES / 2, OW = OS / 2;     // 16-byte words of 8 elements
+    constexpr int AHEAD = FM <= 2 ? FM : 1;     // row blocks of residual in registers
+    const Epilogue &e = p.e;
+    const int m0 = m + (lane & 31), n0 = n + 8 * (lane >> 5);
+    u32x4 res[AHEAD][FN][2][OW], bias[FN][2][BW];
+    auto fetch = [&](int f) {
+        const char *r = static_cast<const char *>(e.residual) + ((int64_t)(m0 + f * 32) * e.ldr + n0) * OS;
+        if (m0 + f * 32 < p.rows) {
+#pragma unroll
+            for (int g = 0; g < FN; ++g)
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    if (n0 + g * 32 + q * 16 < p.cols) {
+#pragma unroll
+                        for (int w = 0; w < OW; ++w)
+                            res[f % AHEAD][g][q][w] = load16(r + (g * 32 + q * 16) * OS + w * 16);
+                    }
+        }
+    };
+    if (FULL && e.residual) {
+#pragma unroll
+        for (int f = 0; f < AHEAD; ++f) fetch(f);
+    }
+    if (FULL && e.bias) {
+        const char *b = static_cast<const char *>(e.bias) + (int64_t)n0 * ES;
+#pragma unroll
+        for (int g = 0; g < FN; ++g)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                if (n0 + g * 32 + q * 16 < p.cols) {
+#pragma unroll
+                    for (int w = 0; w < BW; ++w)
+                        bias[g][q][w] = load16(b + (g * 32 + q * 16) * ES + w * 16);
+                }
+    }
+#pragma unroll
+    for (int f = 0; f < FM; ++f) {
+        const int64_t row = m0 + f * 32;
+        float v[FN][2][8];
+#pragma unroll
+        for (int g = 0; g < FN; ++g)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                float b[8];
+                columns_of(acc[f][g], q, v[g][q]);
+                if (FULL && e.bias) {
+                    elems_of<DT>(bias[g][q], b);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[g][q][i] += b[i];
+                }
+                if (FULL && e.pre && row < p.rows && n0 + g * 32 + q * 16 < p.cols)
+                    store_elems<DT>(static_cast<char *>(e.pre) +
+                                        (row * e.ldp + n0 + g * 32 + q * 16) * ES, v[g][q]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[g][q][i] = act_value(ACT, v[g][q][i]) * e.scale;
+                if (FULL && e.residual) {
+                    elems_of<ODT>(res[f % AHEAD][g][q], b);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[g][q][i] += b[i];
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        if (FULL && f == FM - 1) {
+            // For the compiler, which sees a path on which these loads are not waited
+            // for and would wait for everything at the loop over the steps.
+#pragma unroll
+            for (int g = 0; g < FN; ++g)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+#pragma unroll
+                    for (int w = 0; w < BW; ++w) asm volatile("" ::"v"(bias[g][q][w]));
+#pragma unroll
+                    for (int a = 0; a < AHEAD; ++a)
+#pragma unroll
+                        for (int w = 0; w < OW; ++w) asm volatile("" ::"v"(res[a][g][q][w]));
+                }
+        }
+        if (FULL && e.residual && f + AHEAD < FM) fetch(f + AHEAD);
+        char *o = static_cast<char *>(e.out) + (row * e.ldo + n0) * OS;
+#pragma unroll
+        for (int g = 0; g < FN; ++g)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                if (row < p.rows && n0 + g * 32 + q * 16 < p.cols)
+                    store_elems<ODT>(o + (g * 32 + q * 16) * OS, v[g][q]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// The float32 sums of a part of the reduction axis.
+template <int FM, int FN>
+__device__ __forceinline__ void write_part(const Gemm &p, int part, int m, int n, int lane,
+                                           const f32x16 (&acc)[FM][FN])
+{
+    const int m0 = m + (lane & 31), n0 = n + 8 * (lane >> 5);
+    float *o = p.partial + ((int64_t)part * p.rows + m0) * p.pld + n0;
+#pragma unroll
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+        for (int g = 0; g < FN; ++g)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                float v[8];
+                columns_of(acc[f][g], q, v);
+                if (m0 + f * 32 < p.rows && n0 + g * 32 + q * 16 < p.cols)
+                    store_elems<FLASHBEV_F32>(o + f * 32 * p.pld + g * 32 + q * 16, v);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+}
+
+// FULL: the forward, with every activation and type of output; else a gradient
+// in the inputs' type.
+template <int DT, bool FULL, int FM, int FN>
+__device__ __forceinline__ void write_any(const Gemm &p, int part, int m, int n, int lane,
+                                          const f32x16 (&acc)[FM][FN])
+{
+    // nothing of the epilogue is to be computed ahead of the loop over the steps,
+    // whose registers are short
+    asm volatile("" : "+v"(lane));
+    if (p.split > 1) return write_part(p, part, m, n, lane, acc);
+    constexpr int F32 = FLASHBEV_F32;
+    if constexpr (!FULL) {
+        write_tile<DT, DT, FLASHBLOCK_ACT_NONE, FULL>(p, m, n, lane, acc);
+    } else if (DT == F32 || !p.e.out_f32) {
+        switch (p.e.act) {
+        case FLASHBLOCK_ACT_RELU: return write_tile<DT, DT, FLASHBLOCK_ACT_RELU, FULL>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_GELU: return write_tile<DT, DT, FLASHBLOCK_ACT_GELU, FULL>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_GELU_TANH:
+            return write_tile<DT, DT, FLASHBLOCK_ACT_GELU_TANH, FULL>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_SILU: return write_tile<DT, DT, FLASHBLOCK_ACT_SILU, FULL>(p, m, n, lane, acc);
+        default: return write_tile<DT, DT, FLASHBLOCK_ACT_NONE, FULL>(p, m, n, lane, acc);
+        }
+    } else {
+        switch (p.e.act) {
+        case FLASHBLOCK_ACT_RELU: return write_tile<DT, F32, FLASHBLOCK_ACT_RELU, FULL>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_GELU: return write_tile<DT, F32, FLASHBLOCK_ACT_GELU, FULL>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_GELU_TANH:
+            return write_tile<DT, F32, FLASHBLOCK_ACT_GELU_TANH, FULL>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_SILU: return write_tile<DT, F32, FLASHBLOCK_ACT_SILU, FULL>(p, m, n, lane, acc);
+        default: return write_tile<DT, F32, FLASHBLOCK_ACT_NONE, FULL>(p, m, n, lane, acc);
+        }
+    }
+}
+
+template <int DT, bool AX, bool BX, int BM, int BN, int WM, int WN, int S>
+__global__ void __launch_bounds__(WM *WN * 64, 2) linear_stream(Gemm p)
+{
+    constexpr int NT = WM * WN * 64;
+    constexpr int TM = BM / WM, TN = BN / WN;
+    constexpr int FM = TM / 32, FN = TN / 32;
+    using SA = Stream<DT, AX, BM, NT>;
+    using SB = Stream<DT, BX, BN, NT>;
+    using TA = typename SA::T;
+    using TB = typename SB::T;
+    constexpr int KT = TA::KT;
+    constexpr int STAGE = TA::BYTES + TB::BYTES;
+    constexpr int LOADS = SA::G + SB::G;
+    extern __shared__ __attribute__((aligned(16))) char ring[];   // S stages
+
+    int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const uint32_t lds0 =
+        __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)ring +
+                                       wave * 1024);
+    const int total = (p.red + KT - 1) / KT;
+    const int items = p.tiles_m * p.tiles_n * p.split;
+    // An XCD's workgroups (one in eight of the grid) take a contiguous share of the
+    // items, which runs over blocks of eight tile rows: what is read together
+    // meets in one L2.
+    const int per = (items + 7) / 8, first = blockIdx.x % 8 * per;
+    const int mine = min(per, items - first), stride = gridDim.x / 8;
+
+    struct Item {
+        int m0, n0, part, s0, s1;
+    };
+    auto item_at = [&](int i) {
+        Item it;
+        const int id = first + i;
+        const int tile = id / p.split;
+        it.part = id - tile * p.split;
+        const int group = tile / (8 * p.tiles_n), rest = tile - group * 8 * p.tiles_n;
+        const int rows = min(8, p.tiles_m - 8 * group);
+        it.n0 = rest / rows * BN;
+        it.m0 = (group * 8 + rest % rows) * BM;
+        it.s0 = it.part * p.steps;
+        it.s1 = min(total, it.s0 + p.steps);
+        return it;
+    };
+
+    f32x16 acc[FM][FN];
+    auto clear = [&] {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    };
+
+    // the loading end of the ring
+    int li = blockIdx.x / 8, ls = 0, slot = 0;
+    Item load{};
+    uint32_t oa[SA::G], ob[SB::G];
+    const char *pa = nullptr, *pb = nullptr;
+    bool loading = li < mine;
+    auto offsets = [&] {
+        SA::offsets(oa, p.lda, load.m0, p.rows, tid);
+        SB::offsets(ob, p.ldb, load.n0, p.cols, tid);
+    };
+    auto open = [&] {
+        load = item_at(li);
+        offsets();
+        ls = load.s0;
+        pa = SA::at(p.a, p.lda, load.m0, ls * KT);
+        pb = SB::at(p.b, p.ldb, load.n0, ls * KT);
+    };
+    auto fetch = [&] {
+        const uint32_t la = lds0 + slot * STAGE, lb = la + TA::BYTES;
+        const int left = p.red - ls * KT;
+        if (left >= KT) {
+            SA::load(pa, oa, la);
+            SB::load(pb, ob, lb);
+        } else {
+            SA::load_last(pa, oa, la, left, tid);
+            SB::load_last(pb, ob, lb, left, tid);
+        }
+        slot = slot + 1 == S ? 0 : slot + 1;
+        pa += AX ? (int64_t)KT * p.lda : (int64_t)128;
+        pb += BX ? (int64_t)KT * p.ldb : (int64_t)128;
+        if (++ls == load.s1) {
+            li += stride;
+            loading = li < mine;
+            if (loading) open();
+        }
+    };
+    if (loading) open();
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i)
+        if (loading) fetch();
+
+    // Fragments of a quarter step are read while the quarter before it is multiplied
+    // (left alone, the compiler reads each one just before its use); the barrier
+    // between steps stands before the last quarter's products, whose operands are in
+    // registers, so that the matrix cores work on through it.
+    u32x4 fa[2][FM], fb[2][FN];
+    int read = 0;
+    auto quarter = [&](int kk) {
+        const char *la = ring + read * STAGE, *lb = la + TA::BYTES;
+#pragma unroll
+        for (int g = 0; g < FN; ++g) fb[kk & 1][g] = TB::fragment(lb, wn * TN + g * 32, kk, lane);
+#pragma unroll
+        for (int f = 0; f < FM; ++f) fa[kk & 1][f] = TA::fragment(la, wm * TM + f * 32, kk, lane);
+    };
+    // to the ring's next stage: it is the oldest in flight, of S - 1 (fewer near the
+    // end, where all are waited for); past the barrier every wavefront has read the
+    // stage before it, whose place is filled again
+    auto advance = [&] {
+        if (loading) wait_loads<(S - 2) * LOADS>();
+        else wait_loads<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (loading) fetch();
+        quarter(0);
+    };
+    for (int i = blockIdx.x / 8; i < mine; i += stride) {
+        const Item it = item_at(i);
+        clear();
+        if (it.s0 < it.s1) advance();
+        for (int s = it.s0; s < it.s1; ++s) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+                if (kk < 3) {
+                    quarter(kk + 1);
+                } else {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    read = read + 1 == S ? 0 : read + 1;
+                    if (s + 1 < it.s1) advance();
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int f = 0; f < FM; ++f)
+#pragma unroll
+                    for (int g = 0; g < FN; ++g) mma<DT>(acc[f][g], fb[kk & 1][g], fa[kk & 1][f]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        write_any<DT, !BX>(p, it.part, it.m0 + wm * TM, it.n0 + wn * TN, lane, acc);
+        // what the lanes' addresses are made of is computed again rather than kept
+        // in registers through the epilogue (where it spilled, the ring's loads
+        // waited for its way back)
+        tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        lane = tid & 63;
+        if (loading) offsets();
     }
 }
 
@@ -570,52 +1044,134 @@ constexpr int kCus = 256;
 
 uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 
+// Tile, and parts of the reduction axis, with the least estimated time.  A tile's
+// time is its steps' and a fixed part (filling the ring, writing the results);
+// `resident` workgroups run at once.  The constants (us) are fitted to measured
+// products: in 256, 128 and 64 tiles, bfloat16, 8192 x 8192 over 4096 takes 461, 536 and
+// 937; 184950 x 256 over 256 51, 57 and 86; 40000 x 512 over 256 with a float32 output
+// 41, 27 and 38; 1024 x 256 over 40000 (in parts) 57, 57 and 74; float32
+// 40000 x 256 over 256 75, 60 and 55.
 struct TilePlan {
-    int bm, bn, split, steps;
+    int tile, split, steps;
     uint64_t workspace;    // bytes of partial sums
 };
 
-TilePlan plan_tiles(int64_t rows, int64_t cols, int64_t red, int dt)
+struct TileCost {
+    int tile, resident;
+    float step, fixed;
+};
+constexpr TileCost kStream16[] = {{256, kCus, 1.72f, 7.5f}, {128, 2 * kCus, 1.02f, 4.0f},
+                                  {64, 2 * kCus, 0.5f, 3.0f}};
+constexpr TileCost kStream32[] = {{256, kCus, 7.4f, 7.5f}, {128, 2 * kCus, 3.8f, 4.0f},
+                                  {64, 2 * kCus, 1.0f, 3.0f}};
+// linear_tiles, which widths of other than whole granules take
+constexpr TileCost kChecked[] = {{128, 2 * kCus, 3.0f, 4.0f}, {64, 4 * kCus, 1.5f, 3.0f}};
+
+TilePlan plan_tiles(int64_t rows, int64_t cols, int64_t red, int dt, bool checked)
 {
-    TilePlan t;
-    const int kt = 128 / elem_size(dt);
-    const int64_t total = (red + kt - 1) / kt;
-    t.bm = t.bn = 128;
-    int64_t tiles = ((rows + 127) / 128) * ((cols + 127) / 128);
-    if (tiles < kCus) {
-        t.bm = t.bn = 64;
-        tiles = ((rows + 63) / 64) * ((cols + 63) / 64);
+    const int64_t total = (red + 128 / elem_size(dt) - 1) / (128 / elem_size(dt));
+    TilePlan best{64, 1, (int)(total > 0 ? total : 1), 0};
+    const TileCost *costs = checked ? kChecked : dt == FLASHBEV_F32 ? kStream32 : kStream16;
+    float least = 0.0f;
+    for (int k = 0; k < (checked ? 2 : 3); ++k) {
+        const TileCost &c = costs[k];
+        const int64_t tiles = ((rows + c.tile - 1) / c.tile) * ((cols + c.tile - 1) / c.tile);
+        for (int64_t split = 1; split == 1 || (split <= total / 2 && split * tiles <= 2 * c.resident);
+             split *= 2) {
+            const int64_t steps = total > 0 ? (total + split - 1) / split : 1;
+            const int64_t parts = total > 0 ? (total + steps - 1) / steps : 1;
+            const int64_t rounds = (tiles * parts + c.resident - 1) / c.resident;
+            float us = (float)rounds * (c.fixed + c.step * (float)steps);
+            if (parts > 1)   // the sums' way to memory and back, another launch
+                us += 3.0f + (float)parts * (float)rows * (float)cols * 2e-6f;
+            if (least == 0.0f || us < least) {
+                least = us;
+                best = {c.tile, (int)parts, (int)steps, 0};
+            }
+        }
     }
-    // split the reduction axis until the chip has two workgroups per CU, in
-    // parts of four steps or more
-    int64_t split = tiles > 0 ? 2 * kCus / tiles : 1;
-    if (split > total / 4) split = total / 4;
-    if (split < 1) split = 1;
-    t.steps = (int)((total + split - 1) / split);
-    if (t.steps < 1) t.steps = 1;
-    split = (total + t.steps - 1) / t.steps;
-    t.split = (int)(split < 1 ? 1 : split);
-    t.workspace = t.split > 1 ? round_up((uint64_t)t.split * rows * round_up(cols, 8) * 4, 256) : 0;
-    return t;
+    if (best.split > 1)
+        best.workspace = round_up((uint64_t)best.split * rows * round_up(cols, 8) * 4, 256);
+    return best;
+}
+
+// What the sizes alone say about linear_stream's layout (linear_stream also needs
+// its strides and addresses): widths of whole granules, the reduction axis of an
+// operand along it or the columns of one across it, and outputs of whole vectors.
+bool whole_granules(int64_t rows, int64_t cols, int64_t red, int dt, bool ax, bool bx)
+{
+    const int e = 16 / elem_size(dt);
+    return (ax ? rows : red) % e == 0 && (bx ? cols : red) % e == 0 && cols % 8 == 0;
+}
+
+TilePlan plan_forward(const flashblock_linear *p)
+{
+    return plan_tiles(p->M, p->N, p->K, p->dtype,
+                      !whole_granules(p->M, p->N, p->K, p->dtype, false, false));
+}
+
+TilePlan plan_grad_x(const flashblock_linear *p)
+{
+    return plan_tiles(p->M, p->K, p->N, p->dtype,
+                      !whole_granules(p->M, p->K, p->N, p->dtype, false, true));
+}
+
+TilePlan plan_grad_weight(const flashblock_linear *p)
+{
+    return plan_tiles(p->N, p->K, p->M, p->dtype,
+                      !whole_granules(p->N, p->K, p->M, p->dtype, true, true));
+}
+
+template <int DT, bool AX, bool BX, int BM, int BN, int WM, int WN, int S>
+int launch_stream(Gemm &g, hipStream_t st)
+{
+    const void *fn = (const void *)linear_stream<DT, AX, BX, BM, BN, WM, WN, S>;
+    constexpr size_t lds = (size_t)S * (BM + BN) * 128;
+    g.tiles_m = (g.rows + BM - 1) / BM;
+    g.tiles_n = (g.cols + BN - 1) / BN;
+    const uint64_t items = (uint64_t)g.tiles_m * g.tiles_n * g.split;
+    if (items > 0x7fffffffull) return FLASHBEV_ERR_UNSUPPORTED;
+    constexpr uint64_t resident = kCus * (163840 / lds);
+    const uint64_t blocks = items < resident ? round_up(items, 8) : resident;
+    if (lds > 65536 &&
+        hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+        return FLASHBEV_ERR_HIP;
+    return launch_kernel(fn, blocks, WM * WN * 64, g, lds, st);
+}
+
+template <int DT, bool AX, bool BX>
+bool streamable(const Gemm &g)
+{
+    return g.red > 0 && !misaligned(g.a, 16) && !misaligned(g.b, 16) && g.lda % 16 == 0 &&
+           g.ldb % 16 == 0 && whole_granules(g.rows, g.cols, g.red, DT, AX, BX);
+}
+
+template <int DT, bool AX, bool BX, int TILE>
+int launch_checked(Gemm &g, hipStream_t st)
+{
+    g.tiles_m = (g.rows + TILE - 1) / TILE;
+    g.tiles_n = (g.cols + TILE - 1) / TILE;
+    return launch_kernel((const void *)linear_tiles<DT, AX, BX, TILE, TILE, 2, 2>,
+                         (uint64_t)g.tiles_m * g.tiles_n * g.split, 256, g, 0, st);
 }
 
 template <int DT, bool AX, bool BX>
 int launch_tiles(Gemm &g, const TilePlan &t, hipStream_t st)
 {
-    const uint64_t blocks = (uint64_t)g.tiles_m * g.tiles_n * g.split;
-    if (t.bm == 128)
-        return launch_kernel((const void *)linear_tiles<DT, AX, BX, 128, 128, 2, 2>, blocks, 256, g,
-                             0, st);
-    return launch_kernel((const void *)linear_tiles<DT, AX, BX, 64, 64, 2, 2>, blocks, 256, g, 0, st);
+    if (streamable<DT, AX, BX>(g)) {
+        if (t.tile == 256) return launch_stream<DT, AX, BX, 256, 256, 2, 4, 2>(g, st);
+        if (t.tile == 128) return launch_stream<DT, AX, BX, 128, 128, 2, 2, 2>(g, st);
+        return launch_stream<DT, AX, BX, 64, 64, 2, 2, 4>(g, st);
+    }
+    return t.tile == 64 ? launch_checked<DT, AX, BX, 64>(g, st) : launch_checked<DT, AX, BX, 128>(g, st);
 }
 
-// C = A B^T through the epilogue; `workspace` of plan_tiles(...).workspace bytes
+// C = A B^T through the epilogue; `workspace` of t.workspace bytes
 template <bool AX, bool BX>
-int product(int dt, const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows,
-            int64_t cols, int64_t red, const Epilogue &e, void *workspace, hipStream_t st)
+int product(const TilePlan &t, int dt, const void *a, int64_t lda, const void *b, int64_t ldb,
+            int64_t rows, int64_t cols, int64_t red, const Epilogue &e, void *workspace, hipStream_t st)
 {
     if (rows == 0 || cols == 0) return FLASHBEV_OK;
-    const TilePlan t = plan_tiles(rows, cols, red, dt);
     const int es = elem_size(dt);
     Gemm g{};
     g.a = static_cast<const char *>(a);
@@ -625,8 +1181,6 @@ int product(int dt, const void *a, int64_t lda, const void *b, int64_t ldb, int6
     g.rows = (int)rows;
     g.cols = (int)cols;
     g.red = (int)red;
-    g.tiles_m = (int)((rows + t.bm - 1) / t.bm);
-    g.tiles_n = (int)((cols + t.bn - 1) / t.bn);
     g.split = t.split;
     g.steps = t.steps;
     g.partial = static_cast<float *>(workspace);
@@ -709,9 +1263,9 @@ BackwardPlan plan_backward(const flashblock_linear *p, bool want_x, bool want_w,
     b.ranges = (int)((p->M + b.range_rows - 1) / b.range_rows);
     if (b.ranges < 1) b.ranges = 1;
     b.sum_bytes = want_b ? round_up((uint64_t)b.ranges * b.ldd * 4, 256) : 0;
-    if (want_w) b.partial_bytes = plan_tiles(p->N, p->K, p->M, p->dtype).workspace;
+    if (want_w) b.partial_bytes = plan_grad_weight(p).workspace;
     if (want_x) {
-        const uint64_t w = plan_tiles(p->M, p->K, p->N, p->dtype).workspace;
+        const uint64_t w = plan_grad_x(p).workspace;
         if (w > b.partial_bytes) b.partial_bytes = w;
     }
     b.total = b.d_bytes + b.sum_bytes + b.partial_bytes;
@@ -726,7 +1280,7 @@ int flashblock_linear_workspace_size(const flashblock_linear *p, uint64_t *bytes
 {
     if (!bytes) return FLASHBEV_ERR_NULLPTR;
     if (const int rc = check_sizes(p)) return rc;
-    *bytes = plan_tiles(p->M, p->N, p->K, p->dtype).workspace;
+    *bytes = p->M && p->N ? plan_forward(p).workspace : 0;
     return FLASHBEV_OK;
 }
 
@@ -745,7 +1299,8 @@ int flashblock_linear_forward(const flashblock_linear *p, const void *x, const v
     if (residual && (rc = check_rows(residual, p->M, p->ldr, p->N, os))) return rc;
     if (pre && (rc = check_rows(pre, p->M, p->ldp, p->N, es))) return rc;
     if (misaligned(bias, es)) return FLASHBEV_ERR_ALIGN;
-    const uint64_t need = plan_tiles(p->M, p->N, p->K, p->dtype).workspace;
+    const TilePlan plan = plan_forward(p);
+    const uint64_t need = plan.workspace;
     if ((rc = check_workspace(workspace, workspace_bytes, need))) return rc;
     const bool in_place = residual == out && p->ldr == p->ldo;
     const Range ins[] = {{x, span_bytes(p->M, p->ldx, p->K, es)},
@@ -765,7 +1320,7 @@ int flashblock_linear_forward(const flashblock_linear *p, const void *x, const v
     }
     Epilogue e{out, pre, bias, residual, p->ldo, p->ldp, p->ldr, p->scale, p->act,
                p->out_dtype == FLASHBEV_F32};
-    return product<false, false>(p->dtype, x, p->ldx, weight, p->ldw, p->M, p->N, p->K, e, workspace,
+    return product<false, false>(plan, p->dtype, x, p->ldx, weight, p->ldw, p->M, p->N, p->K, e, workspace,
                                  static_cast<hipStream_t>(stream));
 }
 
@@ -861,13 +1416,13 @@ int flashblock_linear_backward(const flashblock_linear *p, const void *grad_out,
     if (want_w) {
         Epilogue e{grad_weight, nullptr, nullptr, nullptr, ldgw, 0, 0, alpha, FLASHBLOCK_ACT_NONE,
                    dt == FLASHBEV_F32};
-        if ((rc = product<true, true>(dt, d, ldd, x, p->ldx, p->N, p->K, p->M, e, partial, st)))
+        if ((rc = product<true, true>(plan_grad_weight(p), dt, d, ldd, x, p->ldx, p->N, p->K, p->M, e, partial, st)))
             return rc;
     }
     if (want_x) {
         Epilogue e{grad_x, nullptr, nullptr, nullptr, ldgx, 0, 0, alpha, FLASHBLOCK_ACT_NONE,
                    dt == FLASHBEV_F32};
-        if ((rc = product<false, true>(dt, d, ldd, weight, p->ldw, p->M, p->K, p->N, e, partial, st)))
+        if ((rc = product<false, true>(plan_grad_x(p), dt, d, ldd, weight, p->ldw, p->M, p->K, p->N, e, partial, st)))
             return rc;
     }
     return FLASHBEV_OK;
