@@ -8,6 +8,7 @@ and gradient runs in the library's HIP kernels.
 from __future__ import annotations
 
 import ctypes
+import functools
 import struct
 
 from . import (FlashBevError, _dtype_code, _on_device, _one_device,
@@ -50,24 +51,32 @@ def _rows(t, name: str):
         raise ValueError(f"{name} must have at least one dimension")
     width = shape[-1]
     if t.is_contiguous():
+        if len(shape) == 2:
+            return shape[0], width
         return (t.numel() // width if width else _product(shape[:-1])), width
+    return _strided_rows(t, name)
+
+
+def _strided_rows(t, name: str):
+    shape, strides = t.shape, t.stride()
+    width = shape[-1]
     rows, ld = _product(shape[:-1]), width
-    if rows and width:
-        strides = t.stride()
-        if width > 1 and strides[-1] != 1:
-            raise ValueError(f"{name}'s last dimension must be contiguous")
-        step = None   # elements from one row to the next, and rows below it
-        for n, st in zip(reversed(shape[:-1]), reversed(strides[:-1])):
-            if n == 1:
-                continue
-            if step is None:
-                ld, step = st, st * n
-            elif st != step:
-                raise ValueError(f"{name}'s leading dimensions must be rows at one stride")
-            else:
-                step *= n
-        if step is not None and ld < width:
-            raise ValueError(f"{name}'s rows must not overlap")
+    if not rows or not width:
+        return rows, ld
+    if width > 1 and strides[-1] != 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    step = None   # elements from one row to the next, then over all rows so far
+    for n, st in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+        if n == 1:
+            continue
+        if step is None:
+            ld, step = st, st * n
+        elif st != step:
+            raise ValueError(f"{name}'s leading dimensions must be rows at one stride")
+        else:
+            step *= n
+    if ld < width:
+        raise ValueError(f"{name}'s rows must not overlap")
     return rows, ld
 
 
@@ -79,7 +88,7 @@ def _product(shape) -> int:
 
 
 def _same(t, name: str, dtype, shape) -> None:
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} [{', '.join(str(int(v)) for v in shape)}]")
 
 
@@ -89,9 +98,8 @@ def _vector(t, name: str, dtype, n: int) -> int:
         return 0
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    _same(t, name, dtype, (n,))
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+    if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} vector [{n}]")
     return t.data_ptr()
 
 
@@ -173,7 +181,7 @@ def linear_forward(x, weight, bias=None, activation="none", residual=None, scale
                              code if odt == x.dtype else 0, _act_code(activation), scale)
     dev = _one_device(x, weight, bias, residual, out, pre)
     s = _stream_handle(stream, dev)
-    need = _size("flashblock_linear_workspace_size", "PP", args)
+    need = _linear_need(M, K, N, code)
     ws = _workspace(need, dev, s) if need else None
     call = _packed_call("flashblock_linear_forward", "PPPPPPPPQP")
     with _on_device(dev):
@@ -191,6 +199,29 @@ def _size(name: str, kinds: str, *args) -> int:
     if rc != 0:
         raise FlashBevError(rc, name)
     return n.value
+
+
+# Workspace sizes depend on the sizes and types alone, which calls repeat.
+
+
+@functools.lru_cache(maxsize=4096)
+def _linear_need(M: int, K: int, N: int, code: int) -> int:
+    return _size("flashblock_linear_workspace_size", "PP",
+                 _PACK_LINEAR.pack(M, K, K, N, N, N, K, N, code, code, 0, 1.0))
+
+
+@functools.lru_cache(maxsize=4096)
+def _linear_backward_need(M: int, K: int, N: int, code: int, out_code: int, act: int, x: bool,
+                          weight: bool, bias: bool) -> int:
+    return _size("flashblock_linear_backward_workspace_size", "PiiiP",
+                 _PACK_LINEAR.pack(M, K, K, N, N, N, K, N, code, out_code, act, 1.0), x, weight, bias)
+
+
+@functools.lru_cache(maxsize=4096)
+def _norm_need(M: int, groups: int, C: int, flags) -> int:
+    return _size("flashblock_norm_backward_workspace_size", "PPP",
+                 _PACK_NORM.pack(M, C, C, C, C, groups, C, 0, 0, 0, 1, 1, 1.0, 1.0),
+                 _PACK_VECTORS.pack(*flags))
 
 
 def linear_backward(grad_out, x, weight, pre=None, activation="none", scale: float = 1.0,
@@ -230,7 +261,9 @@ def linear_backward(grad_out, x, weight, pre=None, activation="none", scale: flo
             if name == "bias" and not given.is_contiguous():
                 raise ValueError("grad_bias must be contiguous")
         elif name in want:
-            given = torch.empty(like, dtype=x.dtype, device=x.device)
+            given = (torch.empty(like, dtype=x.dtype, device=x.device) if name == "bias"
+                     else torch.empty_like(x if name == "x" else weight,
+                                           memory_format=torch.contiguous_format))
             ld[name] = K
         outs[name] = given
     if all(t is None for t in outs.values()):
@@ -239,8 +272,9 @@ def linear_backward(grad_out, x, weight, pre=None, activation="none", scale: flo
                              scale)
     dev = _one_device(grad_out, x, weight, pre if act else None, *outs.values())
     s = _stream_handle(stream, dev)
-    need = _size("flashblock_linear_backward_workspace_size", "PiiiP", args,
-                 *(int(outs[k] is not None) for k in ("x", "weight", "bias")))
+    need = _linear_backward_need(M, K, N, code, code if odt == x.dtype else 0, act,
+                                 outs["x"] is not None, outs["weight"] is not None,
+                                 outs["bias"] is not None)
     ws = _workspace(need, dev, s) if need else None
     call = _packed_call("flashblock_linear_backward", "PPPPPPQPQPPQP")
     with _on_device(dev):
@@ -253,6 +287,7 @@ def linear_backward(grad_out, x, weight, pre=None, activation="none", scale: flo
 
 
 _VECTORS = ("gate", "weight", "bias", "post_weight", "post_bias")
+_NORM_INPUTS = ("x", "residual", *_VECTORS)
 
 
 def _norm_code(kind, name: str) -> int:
@@ -345,12 +380,12 @@ def norm_forward(x, weight=None, bias=None, residual=None, gate=None, scale: flo
         _same(out_s, "out_s", sdt, x.shape)
         lds = _rows(out_s, "out_s")[1]
     elif not same:
-        out_s = torch.empty(x.shape, dtype=sdt, device=x.device)
+        out_s = torch.empty_like(x, dtype=sdt, memory_format=torch.contiguous_format)
     if not kind:
         if out is not None:
             raise ValueError("out needs a norm")
     elif out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
     else:
         _same(out, "out", x.dtype, x.shape)
         ldy = _rows(out, "out")[1]
@@ -402,9 +437,9 @@ def norm_backward(grad_y, grad_s, x, s, weight=None, gate=None, scale: float = 1
     outs = {}
     for k in want:
         if k == "x":
-            outs[k] = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            outs[k] = torch.empty_like(x, memory_format=torch.contiguous_format)
         elif k == "residual":
-            outs[k] = torch.empty(x.shape, dtype=sdt, device=x.device)
+            outs[k] = torch.empty_like(s, memory_format=torch.contiguous_format)
         elif k not in _VECTORS:
             raise ValueError(f"want takes 'x', 'residual' and {_VECTORS}")
         elif k == "gate":
@@ -418,7 +453,7 @@ def norm_backward(grad_y, grad_s, x, s, weight=None, gate=None, scale: float = 1
     grads = _PACK_VECTORS.pack(*(_addr(outs.get(k)) for k in _VECTORS))
     dev = _one_device(grad_y, grad_s, x, s, weight, gate, post_weight, post_bias)
     st = _stream_handle(stream, dev)
-    need = _size("flashblock_norm_backward_workspace_size", "PPP", args, grads)
+    need = _norm_need(M, groups, C, tuple(k in outs for k in _VECTORS))
     ws = _workspace(need, dev, st) if need else None
     call = _packed_call("flashblock_norm_backward", "PPPPPPPQPQPPQP")
     with _on_device(dev):
@@ -451,29 +486,46 @@ def _autograd_functions():
     import torch
     from torch.autograd.function import once_differentiable
 
+    def linear_grads(ctx, grad_out):
+        x, weight, pre = ctx.saved_tensors
+        activation, scale = ctx.meta
+        needs = ctx.needs_input_grad
+        want = tuple(k for k, n in zip(("x", "weight", "bias"), needs) if n)
+        residual = grad_out if needs[3] else None
+        if not want:
+            return None, None, None, residual, None, None, None
+        r = linear_backward(_as_rows(grad_out), x, weight, pre, activation, scale, want)
+        return r["x"], r["weight"], r["bias"], residual, None, None, None
+
+    def norm_grads(ctx, grad_y, grad_s):
+        x, s, weight, gate, post_weight, post_bias = ctx.saved_tensors
+        scale, norm, post_norm, eps = ctx.meta
+        want = tuple(k for k, n in zip(_NORM_INPUTS, ctx.needs_input_grad) if n)
+        r = {}
+        if grad_y is not None or grad_s is not None:
+            r = norm_backward(None if grad_y is None else _as_rows(grad_y),
+                              None if grad_s is None else _as_rows(grad_s), x, x if s is None else s,
+                              weight, gate, scale, norm, post_norm, post_weight, post_bias, eps, want)
+        return (*map(r.get, _NORM_INPUTS), None, None, None, None)
+
+    # the wrapper, which refuses a second derivative, only where a graph of the
+    # gradients is made (it takes some 10 us)
+    linear_once, norm_once = once_differentiable(linear_grads), once_differentiable(norm_grads)
+
     class _Linear(torch.autograd.Function):
         @staticmethod
         def forward(ctx, x, weight, bias, residual, activation, scale, out_dtype):
             pre = None
             if _act_code(activation) and any(ctx.needs_input_grad[:3]):
                 pre = torch.empty((*x.shape[:-1], weight.shape[0]), dtype=x.dtype, device=x.device)
-            out = linear_forward(x, weight, bias, activation, residual, scale, out_dtype=out_dtype,
-                                 pre=pre)
+            out = linear_forward(x, weight, bias, activation, residual, scale, None, out_dtype, pre)
             ctx.save_for_backward(x, weight, pre)
             ctx.meta = (activation, scale)
             return out
 
         @staticmethod
-        @once_differentiable
         def backward(ctx, grad_out):
-            x, weight, pre = ctx.saved_tensors
-            activation, scale = ctx.meta
-            needs = ctx.needs_input_grad
-            want = tuple(k for k, n in zip(("x", "weight", "bias"), needs) if n)
-            r = dict.fromkeys(("x", "weight", "bias"))
-            if want:
-                r = linear_backward(_as_rows(grad_out), x, weight, pre, activation, scale, want)
-            return (r["x"], r["weight"], r["bias"], grad_out if needs[3] else None, None, None, None)
+            return (linear_once if torch.is_grad_enabled() else linear_grads)(ctx, grad_out)
 
     class _Norm(torch.autograd.Function):
         @staticmethod
@@ -482,24 +534,15 @@ def _autograd_functions():
             ctx.set_materialize_grads(False)
             y, s = norm_forward(x, weight, bias, residual, gate, scale, norm, post_norm, post_weight,
                                 post_bias, eps)
-            same = s is x
-            ctx.save_for_backward(x, None if same else s, weight, gate, post_weight, post_bias)
+            if s is x:
+                s = None
+            ctx.save_for_backward(x, s, weight, gate, post_weight, post_bias)
             ctx.meta = (scale, norm, post_norm, eps)
-            return y, None if same else s
+            return y, s
 
         @staticmethod
-        @once_differentiable
         def backward(ctx, grad_y, grad_s):
-            x, s, weight, gate, post_weight, post_bias = ctx.saved_tensors
-            scale, norm, post_norm, eps = ctx.meta
-            names = ("x", "residual", "gate", "weight", "bias", "post_weight", "post_bias")
-            r = dict.fromkeys(names)
-            if grad_y is not None or grad_s is not None:
-                want = tuple(k for k, n in zip(names, ctx.needs_input_grad) if n)
-                grads = (None if g is None else _as_rows(g) for g in (grad_y, grad_s))
-                r.update(norm_backward(*grads, x, x if s is None else s, weight, gate, scale, norm,
-                                       post_norm, post_weight, post_bias, eps, want))
-            return (*(r[k] for k in names), None, None, None, None)
+            return (norm_once if torch.is_grad_enabled() else norm_grads)(ctx, grad_y, grad_s)
 
     _AUTOGRAD["linear"] = _Linear
     _AUTOGRAD["norm"] = _Norm
