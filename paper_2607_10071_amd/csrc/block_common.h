@@ -19,6 +19,19 @@ __device__ __forceinline__ u32x4 load16(const void *p)
     return *reinterpret_cast<const u32x4_any *>(p);
 }
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+
+__device__ __forceinline__ u32x2 load8(const void *p)
+{
+    return *reinterpret_cast<const u32x2_any *>(p);
+}
+
+__device__ __forceinline__ void store8(void *p, u32x2 v)
+{
+    *reinterpret_cast<u32x2_any *>(p) = v;
+}
+
 __device__ __forceinline__ void store16(void *p, u32x4 v)
 {
     *reinterpret_cast<u32x4_any *>(p) = v;
@@ -93,6 +106,18 @@ __device__ __forceinline__ void load_elems(const void *p, float (&v)[V])
     elems_of<DT>(raw, v);
 }
 
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    if constexpr (DT == FLASHBEV_BF16) {
+        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, b2{(__bf16)a, (__bf16)b});
+    } else {
+        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, h2{(_Float16)a, (_Float16)b});
+    }
+}
+
 template <int DT, int V>
 __device__ __forceinline__ void store_elems(void *p, const float (&v)[V])
 {
@@ -103,21 +128,63 @@ __device__ __forceinline__ void store_elems(void *p, const float (&v)[V])
         u32x4 r;
         if constexpr (DT == FLASHBEV_F32) {
             r = __builtin_bit_cast(u32x4, f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]});
-        } else if constexpr (DT == FLASHBEV_BF16) {
-            typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                r[e] = __builtin_bit_cast(uint32_t, b2{(__bf16)v[8 * q + 2 * e],
-                                                       (__bf16)v[8 * q + 2 * e + 1]});
         } else {
-            typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                r[e] = __builtin_bit_cast(uint32_t, h2{(_Float16)v[8 * q + 2 * e],
-                                                       (_Float16)v[8 * q + 2 * e + 1]});
+            for (int e = 0; e < 4; ++e) r[e] = pack2<DT>(v[8 * q + 2 * e], v[8 * q + 2 * e + 1]);
         }
         store16(static_cast<char *>(p) + 16 * q, r);
     }
+}
+
+// 16 bytes at element `i` of a row that ends at element `end`, zeros past it: the
+// row's last 16 bytes where they begin before `i`, shifted down.
+template <int DT>
+__device__ __forceinline__ u32x4 load_granule_edge(const char *row, int i, int end)
+{
+    constexpr int ES = elem_size(DT), E = 16 / ES;
+    u32x4 v = {0, 0, 0, 0};
+    if (end >= E) {
+        const int at = min(i, end - E);
+        v = load16(row + (int64_t)at * ES);
+        const int shift = (i - at) * ES * 8;   // bits
+        uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+        if (shift >= 64) {
+            lo = shift < 128 ? hi >> (shift - 64) : 0;
+            hi = 0;
+        } else if (shift > 0) {
+            lo = lo >> shift | hi << (64 - shift);
+            hi >>= shift;
+        }
+        v = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+    } else {
+#pragma unroll
+        for (int q = 0; q < E; ++q) {
+            if (i + q >= end) continue;
+            if constexpr (DT == FLASHBEV_F32) {
+                v[q] = reinterpret_cast<const uint32_t *>(row)[i + q];
+            } else {
+                v[q >> 1] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[i + q] << (16 * (q & 1));
+            }
+        }
+    }
+    return v;
+}
+
+// The same for 8 bytes of 16-bit elements.
+__device__ __forceinline__ u32x2 load_half_granule_edge(const char *row, int i, int end)
+{
+    uint64_t v = 0;
+    if (end >= 4) {
+        const int at = min(i, end - 4);
+        const u32x2 w = load8(row + (int64_t)at * 2);
+        const int shift = (i - at) * 16;
+        v = shift < 64 ? (w[0] | (uint64_t)w[1] << 32) >> shift : 0;
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (i + q < end) v |= (uint64_t)reinterpret_cast<const uint16_t *>(row)[i + q] << (16 * q);
+    }
+    return u32x2{(uint32_t)v, (uint32_t)(v >> 32)};
 }
 
 // ---------------------------------------------------------------------------

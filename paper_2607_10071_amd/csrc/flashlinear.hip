@@ -251,40 +251,6 @@ __device__ __forceinline__ void mma(f32x16 &c, const u32x4 &a, const u32x4 &b)
     }
 }
 
-// 16 bytes at element `i` of a row that ends at element `end`, zeros past it: the
-// row's last 16 bytes where they begin before `i`, shifted down.
-template <int DT>
-__device__ __forceinline__ u32x4 load_granule_edge(const char *row, int i, int end)
-{
-    constexpr int ES = elem_size(DT), E = 16 / ES;
-    u32x4 v = {0, 0, 0, 0};
-    if (end >= E) {
-        const int at = min(i, end - E);
-        v = load16(row + (int64_t)at * ES);
-        const int shift = (i - at) * ES * 8;   // bits
-        uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
-        if (shift >= 64) {
-            lo = shift < 128 ? hi >> (shift - 64) : 0;
-            hi = 0;
-        } else if (shift > 0) {
-            lo = lo >> shift | hi << (64 - shift);
-            hi >>= shift;
-        }
-        v = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
-    } else {
-#pragma unroll
-        for (int q = 0; q < E; ++q) {
-            if (i + q >= end) continue;
-            if constexpr (DT == FLASHBEV_F32) {
-                v[q] = reinterpret_cast<const uint32_t *>(row)[i + q];
-            } else {
-                v[q >> 1] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[i + q] << (16 * (q & 1));
-            }
-        }
-    }
-    return v;
-}
-
 // the place of an "along" row's granules (see above)
 __device__ __forceinline__ int along_swizzle(int row) { return row >> 1 & 7; }
 
@@ -907,7 +873,7 @@ __global__ void __launch_bounds__(WM *WN * 64, 2) linear_stream(Gemm p)
 // time they take.  A workgroup owns 16 output channels; its 8 wavefronts take the
 // K axis in turns of one 64-byte piece of each of the 16 weight rows (a 16x16x32 MFMA
 // of 16-bit elements, or four 16x16x4 of float32), from memory straight into the
-// operands, eight pieces in flight, and their sums are added through LDS in the
+// operands, 16 pieces in flight (8 for two blocks), and their sums are added through LDS in the
 // wavefronts' order.  One launch and no workspace: 1 x 4096 x 4096 bfloat16 takes 6.7 us
 // (33.6 MB, 5 TB/s) where parts of 64 x 64 tiles and their join took 14.6.
 constexpr int kFewRows = 32;
@@ -940,7 +906,7 @@ template <int DT, int MB>
 __global__ void __launch_bounds__(64 * kFewWaves) linear_few(Few p)
 {
     constexpr int ES = elem_size(DT), E = 16 / ES, KS = 4 * E;   // elements of a piece
-    constexpr int U = 8;
+    constexpr int U = MB == 1 ? 16 : 8;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int n0 = blockIdx.x * 16, k0 = (lane >> 4) * E;
     // rows and channels past the last repeat it; their sums are not stored
@@ -1026,6 +992,7 @@ __global__ void __launch_bounds__(256) linear_join(Join p)
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = 0.0f;
     const float *src = p.partial + m * p.pld + n;
+#pragma unroll 8
     for (int s = 0; s < p.split; ++s) {
         float w[V];
         load_elems<FLASHBEV_F32>(src + (int64_t)s * p.rows * p.pld, w);
@@ -1129,6 +1096,7 @@ __global__ void __launch_bounds__(256) column_join(ColumnJoin p)
     const int n = blockIdx.x * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
     float s = 0.0f;
     if (n < p.N)
+#pragma unroll 8
         for (int r = r0; r < p.ranges; r += 16) s += p.partial[(int64_t)r * p.pld + n];
     __shared__ float part[16][17];
     part[r0][threadIdx.x & 15] = s;

@@ -16,37 +16,80 @@
 namespace {
 
 // ---------------------------------------------------------------------------
-// a row over T lanes, NV vectors of 8 consecutive channels each
+// a row over T lanes, NV vectors of V consecutive channels each
 // ---------------------------------------------------------------------------
-// T = 8 to 64 lanes share a wavefront with other rows; T = 128 to 1024 are a
-// workgroup of their own.  Lane t holds channels 8 (v T + t) .. + 7 of vector v.
-template <int T, int NV>
+// T = 8 to 64 lanes share a wavefront with other rows; T = 128 takes half a
+// workgroup, T = 256 to 1024 one of their own.  Lane t holds channels
+// V (v T + t) .. + V - 1 of vector v.
+template <int T, int NV, int V>
 struct Row {
-    static constexpr int E = 8 * NV;                     // channels a lane holds
-    static constexpr int NT = T > 256 ? T : 256;         // threads of a workgroup
-    static constexpr int ROWS = T > 64 ? (T >= 256 ? 1 : 2) : NT / T;   // rows of a workgroup
-    static constexpr int WAVES = T / 64;                 // wavefronts of a row, 0: part of one
+    static constexpr int E = V * NV;                     // channels a lane holds
+    static constexpr int ROWS = T >= 256 ? 1 : 256 / T;  // rows of a workgroup
 
-    static __device__ __forceinline__ int col(int t, int v) { return 8 * (v * T + t); }
+    static __device__ __forceinline__ int col(int t, int v) { return V * (v * T + t); }
 
-    // channels past C read as 0
+    static __device__ __forceinline__ bool inside(int t, int e, int C)
+    {
+        return col(t, e / V) + e % V < C;
+    }
+
+    // a lane's channels as they are stored, 0 past C, in 16-byte pieces (8-byte ones
+    // for four 16-bit channels)
+    template <int DT>
+    struct Raw {
+        static constexpr int PIECES = V * elem_size(DT) >= 16 ? V * elem_size(DT) / 16 : 0;
+        u32x4 w[NV][PIECES ? PIECES : 1];
+        u32x2 h[NV];
+    };
+
+    template <int DT>
+    static __device__ __forceinline__ void fetch(const void *p, int64_t off, int t, int C, Raw<DT> &r)
+    {
+        constexpr int ES = elem_size(DT), G = 16 / ES;
+        const char *row = static_cast<const char *>(p) + off * ES;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            if constexpr (Raw<DT>::PIECES == 0) {
+                const int c = col(t, v);
+                if (c + 4 <= C) r.h[v] = load8(row + (int64_t)c * ES);
+                else r.h[v] = c < C ? load_half_granule_edge(row, c, C) : u32x2{0, 0};
+            } else {
+#pragma unroll
+                for (int k = 0; k < Raw<DT>::PIECES; ++k) {
+                    const int c = col(t, v) + k * G;
+                    if (c + G <= C) r.w[v][k] = load16(row + (int64_t)c * ES);
+                    else r.w[v][k] = c < C ? load_granule_edge<DT>(row, c, C) : u32x4{0, 0, 0, 0};
+                }
+            }
+        }
+    }
+
+    template <int DT>
+    static __device__ __forceinline__ void unpack(const Raw<DT> &raw, float (&r)[E])
+    {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            if constexpr (Raw<DT>::PIECES == 0) {
+                const u32x4 wide[1] = {{raw.h[v][0], raw.h[v][1], 0, 0}};
+                float w[8];
+                elems_of<DT>(wide, w);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[4 * v + e] = w[e];
+            } else {
+                float w[V];
+                elems_of<DT>(raw.w[v], w);
+#pragma unroll
+                for (int e = 0; e < V; ++e) r[V * v + e] = w[e];
+            }
+        }
+    }
+
     template <int DT>
     static __device__ __forceinline__ void load(const void *p, int64_t off, int t, int C, float (&r)[E])
     {
-        const char *row = static_cast<const char *>(p) + off * elem_size(DT);
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int c = col(t, v);
-            if (c + 8 <= C) {
-                float w[8];
-                load_elems<DT>(row + (int64_t)c * elem_size(DT), w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) r[8 * v + e] = w[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) r[8 * v + e] = c + e < C ? load_elem<DT>(row, c + e) : 0.0f;
-            }
-        }
+        Raw<DT> raw;
+        fetch<DT>(p, off, t, C, raw);
+        unpack<DT>(raw, r);
     }
 
     template <int DT>
@@ -56,15 +99,20 @@ struct Row {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = col(t, v);
-            if (c + 8 <= C) {
-                float w[8];
+            if (c + V <= C) {
+                char *q = row + (int64_t)c * elem_size(DT);
+                if constexpr (V * elem_size(DT) == 8) {
+                    store8(q, u32x2{pack2<DT>(r[4 * v], r[4 * v + 1]), pack2<DT>(r[4 * v + 2], r[4 * v + 3])});
+                } else {
+                    float w[V];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = r[8 * v + e];
-                store_elems<DT>(row + (int64_t)c * elem_size(DT), w);
+                    for (int e = 0; e < V; ++e) w[e] = r[V * v + e];
+                    store_elems<DT>(q, w);
+                }
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (c + e < C) store_elem<DT>(row, c + e, r[8 * v + e]);
+                for (int e = 0; e < V; ++e)
+                    if (c + e < C) store_elem<DT>(row, c + e, r[V * v + e]);
             }
         }
     }
@@ -82,11 +130,6 @@ struct Row {
         } else {
             load<DT>(p, off, t, C, r);
         }
-    }
-
-    static __device__ __forceinline__ bool inside(int t, int e, int C)
-    {
-        return col(t, e / 8) + e % 8 < C;
     }
 
     // differences from the mean, 0 past C so that they add nothing
@@ -181,7 +224,7 @@ struct Norm {
 template <int DT, int SDT, int T, int NV, bool POST>
 __global__ void __launch_bounds__(T > 256 ? T : 256) norm_forward(Norm p)
 {
-    using R = Row<T, NV>;
+    using R = Row<T, NV, 8>;
     constexpr int E = R::E;
     __shared__ float slots[T > 64 ? 4 * kSlot : 1];
     const int t = threadIdx.x % T;
@@ -275,10 +318,11 @@ struct NormBackward {
 template <int DT, int SDT, int T, int NV, bool POST>
 __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward p)
 {
-    using R = Row<T, NV>;
+    constexpr int V = 4;
+    using R = Row<T, NV, V>;
     constexpr int E = R::E;
     __shared__ float slots[T > 64 ? 3 * kSlot : 1];
-    __shared__ float lanes[R::ROWS > 1 ? R::ROWS * T * 8 : 1];   // one vector's sums at a time
+    __shared__ float lanes[R::ROWS > 1 ? R::ROWS * T * V : 1];   // one vector's sums at a time
     const int t = threadIdx.x % T, lane_row = threadIdx.x / T;
     const int64_t group = blockIdx.x / p.ranges_per_group, range = blockIdx.x % p.ranges_per_group;
     const int64_t m0 = group * p.per_group + range * p.range;
@@ -287,34 +331,59 @@ __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward 
     const float inv = 1.0f / (float)p.C;
     const bool norm = p.norm != FLASHBLOCK_NORM_NONE && p.grad_y;
     const bool reads_x = POST || p.partial[kGate];
+    // the vectors of this sample, and their gradients over the range
+    float weight[E], gate[E], post_weight[E], post_bias[E];
+    R::template params<DT>(p.weight, 0, p.params_f32, t, p.C, 1.0f, weight);
+    R::template params<DT>(p.gate, group * p.C, p.params_f32, t, p.C, 1.0f, gate);
+    if constexpr (POST) {
+        R::template params<DT>(p.post_weight, 0, p.params_f32, t, p.C, 1.0f, post_weight);
+        R::template params<DT>(p.post_bias, 0, p.params_f32, t, p.C, 0.0f, post_bias);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) gate[e] *= p.scale;
     float acc[kVectors][E];
 #pragma unroll
     for (int k = 0; k < kVectors; ++k)
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[k][e] = 0.0f;
 
+    // The next row's loads are in flight while a row's three sums are formed (a row
+    // at a time, 8331 x 771 half took 82 us).  Rows of more than 4096 channels have no
+    // registers for that.
+    constexpr bool AHEAD = T < 1024 || NV == 1;
+    typename R::template Raw<SDT> raw_ds, raw_s;
+    typename R::template Raw<DT> raw_x, raw_g;
+    auto fetch = [&](int64_t first) {
+        const int64_t m = first + lane_row < m1 ? first + lane_row : m1 - 1;
+        if (p.grad_s) R::template fetch<SDT>(p.grad_s, m * p.ldgs, t, p.C, raw_ds);
+        if (reads_x) R::template fetch<DT>(p.x, m * p.ldx, t, p.C, raw_x);
+        if (norm) {
+            R::template fetch<SDT>(p.s, m * p.lds, t, p.C, raw_s);
+            R::template fetch<DT>(p.grad_y, m * p.ldgy, t, p.C, raw_g);
+        }
+    };
+    if (m0 < m1) fetch(m0);
     for (int64_t first = m0; first < m1; first += R::ROWS) {
         // lanes past the range take its last row again and add and store nothing
         const bool in = first + lane_row < m1;
         const int64_t m = in ? first + lane_row : m1 - 1;
-        float ds[E], x[E], a[E];
+        float ds[E], x[E], s[E], g[E];
         if (p.grad_s) {
-            R::template load<SDT>(p.grad_s, m * p.ldgs, t, p.C, ds);
+            R::template unpack<SDT>(raw_ds, ds);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) ds[e] = 0.0f;
         }
-        if (reads_x) R::template load<DT>(p.x, m * p.ldx, t, p.C, x);
-        float s[E], g[E];
+        if (reads_x) R::template unpack<DT>(raw_x, x);
         if (norm) {
-            R::template load<SDT>(p.s, m * p.lds, t, p.C, s);
-            R::template load<DT>(p.grad_y, m * p.ldgy, t, p.C, g);
+            R::template unpack<SDT>(raw_s, s);
+            R::template unpack<DT>(raw_g, g);
         }
+        if (AHEAD && first + R::ROWS < m1) fetch(first + R::ROWS);
         float one[3] = {0.0f, 0.0f, 0.0f};
         if (norm) {
-            R::template params<DT>(p.weight, 0, p.params_f32, t, p.C, 1.0f, a);
             one[0] = R::sum(s);
-            one[1] = R::dot(g, a);
+            one[1] = R::dot(g, weight);
         }
         if constexpr (POST) one[2] = R::sum(x);
         row_sum<T>(one, slots);
@@ -323,7 +392,7 @@ __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward 
             R::centre(s, p.norm == FLASHBLOCK_NORM_LAYER ? one[0] * inv : 0.0f, t, p.C, s);
             two[0] = R::dot(s, s);
 #pragma unroll
-            for (int e = 0; e < E; ++e) two[1] = __builtin_fmaf(g[e] * a[e], s[e], two[1]);
+            for (int e = 0; e < E; ++e) two[1] = __builtin_fmaf(g[e] * weight[e], s[e], two[1]);
         }
         if constexpr (POST) {
             R::centre(x, p.post == FLASHBLOCK_NORM_LAYER ? one[2] * inv : 0.0f, t, p.C, x);
@@ -341,38 +410,31 @@ __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward 
                     acc[kWeight][e] = __builtin_fmaf(g[e], sh, acc[kWeight][e]);
                     acc[kBias][e] += g[e];
                 }
-                ds[e] = __builtin_fmaf(r, g[e] * a[e] - mg - sh * mgs, ds[e]);
+                ds[e] = __builtin_fmaf(r, g[e] * weight[e] - mg - sh * mgs, ds[e]);
             }
         }
         if (in && p.grad_residual)
             R::template store<SDT>(p.grad_residual, m * p.ldgr, t, p.C, ds);
-        if (!reads_x && !p.grad_x) continue;
+        if (!reads_x && !p.grad_x) {
+            if (!AHEAD && first + R::ROWS < m1) fetch(first + R::ROWS);
+            continue;
+        }
         float rx = 0.0f;
         if constexpr (POST) {
             rx = 1.0f / sqrtf(two[2] * inv + p.eps);
 #pragma unroll
             for (int e = 0; e < E; ++e) x[e] *= rx;
         }
-        float pw[E];
-        if constexpr (POST) R::template params<DT>(p.post_weight, 0, p.params_f32, t, p.C, 1.0f, pw);
         if (p.partial[kGate]) {
-            if constexpr (POST)
-                R::template params<DT>(p.post_bias, 0, p.params_f32, t, p.C, 0.0f, a);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 float u = x[e];
-                if constexpr (POST) u = __builtin_fmaf(u, pw[e], a[e]);
+                if constexpr (POST) u = __builtin_fmaf(u, post_weight[e], post_bias[e]);
                 if (in) acc[kGate][e] = __builtin_fmaf(ds[e], u, acc[kGate][e]);
             }
         }
-        if (p.gate) {
-            R::template params<DT>(p.gate, group * p.C, p.params_f32, t, p.C, 1.0f, a);
 #pragma unroll
-            for (int e = 0; e < E; ++e) ds[e] *= p.scale * a[e];
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) ds[e] *= p.scale;
-        }
+        for (int e = 0; e < E; ++e) ds[e] *= gate[e];
         if constexpr (POST) {
             float three[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -382,7 +444,7 @@ __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward 
                     acc[kPostBias][e] += ds[e];
                 }
                 // ds past C is -r mean(g), not 0
-                ds[e] = R::inside(t, e, p.C) ? ds[e] * pw[e] : 0.0f;
+                ds[e] = R::inside(t, e, p.C) ? ds[e] * post_weight[e] : 0.0f;
                 three[0] += ds[e];
                 three[1] = __builtin_fmaf(ds[e], x[e], three[1]);
             }
@@ -393,6 +455,7 @@ __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward 
             for (int e = 0; e < E; ++e) ds[e] = rx * (ds[e] - mh - x[e] * mhx);
         }
         if (in && p.grad_x) R::template store<DT>(p.grad_x, m * p.ldgx, t, p.C, ds);
+        if (!AHEAD && first + R::ROWS < m1) fetch(first + R::ROWS);
     }
 
 #pragma unroll
@@ -402,24 +465,24 @@ __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward 
         float *dst = p.partial[k] + (int64_t)blockIdx.x * p.pld;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            float w[8];
+            float w[V];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = acc[k][8 * v + e];
+            for (int e = 0; e < V; ++e) w[e] = acc[k][V * v + e];
             if constexpr (R::ROWS > 1) {
                 __syncthreads();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) lanes[(lane_row * T + t) * 8 + e] = w[e];
+                for (int e = 0; e < V; ++e) lanes[(lane_row * T + t) * V + e] = w[e];
                 __syncthreads();
                 if (lane_row == 0) {
                     for (int q = 1; q < R::ROWS; ++q)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) w[e] += lanes[(q * T + t) * 8 + e];
+                        for (int e = 0; e < V; ++e) w[e] += lanes[(q * T + t) * V + e];
                 }
             }
             const int c = R::col(t, v);
             if (lane_row == 0 && c < p.C) {   // pld is a multiple of 8
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] *= f;
+                for (int e = 0; e < V; ++e) w[e] *= f;
                 store_elems<FLASHBEV_F32>(dst + c, w);
             }
         }
@@ -450,7 +513,7 @@ __global__ void __launch_bounds__(256) norm_join(NormJoin p)
     float s = 0.0f;
     if (n < p.C) {
         const float *src = p.partial[k] + b * p.ranges[k] * p.pld + n;
-#pragma unroll 4
+#pragma unroll 8
         for (int64_t r = r0; r < p.ranges[k]; r += 16) s += src[r * p.pld];
     }
     __shared__ float part[16][17];
@@ -467,15 +530,18 @@ __global__ void __launch_bounds__(256) norm_join(NormJoin p)
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
-// The lanes of a row: one vector of 8 channels each up to 8192 channels.
+// The lanes of a row: a vector of `v` channels each, up to 1024 lanes.  Forward, 8
+// channels; backward, 4, for its five sums and four vectors in registers (with 8, at
+// 145 to 200 of them, two or three wavefronts fit a SIMD: 40000 x 256 bfloat16 52 us,
+// 16384 x 4096 303).
 struct Shape {
     int lanes, rows, threads;   // of a row; rows and threads of a workgroup
 };
 
-Shape shape_of(int C)
+Shape shape_of(int C, int v)
 {
     int t = 8;
-    while (t < 1024 && 8 * t < C) t *= 2;
+    while (t < 1024 && v * t < C) t *= 2;
     return {t, t >= 256 ? 1 : 256 / t, t > 256 ? t : 256};
 }
 
@@ -483,7 +549,7 @@ template <int DT, int SDT, bool POST>
 const void *forward_kernel(int C)
 {
     if (C > 8192) return (const void *)norm_forward<DT, SDT, 1024, 2, POST>;
-    switch (shape_of(C).lanes) {
+    switch (shape_of(C, 8).lanes) {
     case 8: return (const void *)norm_forward<DT, SDT, 8, 1, POST>;
     case 16: return (const void *)norm_forward<DT, SDT, 16, 1, POST>;
     case 32: return (const void *)norm_forward<DT, SDT, 32, 1, POST>;
@@ -498,8 +564,9 @@ const void *forward_kernel(int C)
 template <int DT, int SDT, bool POST>
 const void *backward_kernel(int C)
 {
-    if (C > 8192) return (const void *)norm_backward<DT, SDT, 1024, 2, POST>;
-    switch (shape_of(C).lanes) {
+    if (C > 8192) return (const void *)norm_backward<DT, SDT, 1024, 4, POST>;
+    if (C > 4096) return (const void *)norm_backward<DT, SDT, 1024, 2, POST>;
+    switch (shape_of(C, 4).lanes) {
     case 8: return (const void *)norm_backward<DT, SDT, 8, 1, POST>;
     case 16: return (const void *)norm_backward<DT, SDT, 16, 1, POST>;
     case 32: return (const void *)norm_backward<DT, SDT, 32, 1, POST>;
@@ -584,7 +651,7 @@ struct NormRanges {
 NormRanges plan_ranges(const flashblock_norm *p)
 {
     NormRanges r;
-    const Shape s = shape_of(p->C);
+    const Shape s = shape_of(p->C, 4);
     r.per_group = p->M / p->groups;
     const int64_t want = (int64_t)256 * 4 * 256 / s.threads;
     int64_t per = (want + p->groups - 1) / p->groups;
@@ -659,7 +726,7 @@ int flashblock_norm_forward(const flashblock_norm *p, const flashblock_norm_para
     Norm n{x, residual, v->gate, v->weight, v->bias, v->post_weight, v->post_bias, s, y,
            p->ldx, p->ldr, p->lds, p->ldy, p->M, p->M / p->groups, p->C, p->norm,
            p->param_dtype == FLASHBEV_F32, p->post_norm, p->eps, p->scale};
-    const Shape h = shape_of(p->C);
+    const Shape h = shape_of(p->C, 8);
     const void *fn = p->post_norm != FLASHBLOCK_NORM_NONE
                          ? kernel_of<false, true>(p->dtype, p->stream_dtype, p->C)
                          : kernel_of<false, false>(p->dtype, p->stream_dtype, p->C);
@@ -787,7 +854,7 @@ int flashblock_norm_backward(const flashblock_norm *p, const flashblock_norm_par
         out_rows += j.rows[k];
     }
     if (p->M > 0) {
-        const Shape h = shape_of(p->C);
+        const Shape h = shape_of(p->C, 4);
         const void *fn = p->post_norm != FLASHBLOCK_NORM_NONE
                              ? kernel_of<true, true>(p->dtype, p->stream_dtype, p->C)
                              : kernel_of<true, false>(p->dtype, p->stream_dtype, p->C);
