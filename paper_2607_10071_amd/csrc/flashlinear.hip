@@ -871,10 +871,10 @@ __global__ void __launch_bounds__(WM *WN * 64, 2) linear_stream(Gemm p)
 // ---------------------------------------------------------------------------
 // Up to 32 rows (one or two blocks of 16) read every weight once, which is all the
 // time they take.  A workgroup owns 16 output channels; its 8 wavefronts take the
-// K axis in turns of one 64-byte piece of each of the 16 weight rows (a 16x16x32 MFMA
-// of 16-bit elements, or four 16x16x4 of float32), from memory straight into the
-// operands, 16 pieces in flight (8 for two blocks), and their sums are added through LDS in the
-// wavefronts' order.  One launch and no workspace: 1 x 4096 x 4096 bfloat16 takes 6.7 us
+// K axis in turns of 16 (for two blocks 8) 64-byte pieces of each of the 16 weight
+// rows (a piece: a 16x16x32 MFMA of 16-bit elements, or four 16x16x4 of float32), all
+// in flight, from memory straight into the operands; their sums are added through LDS in the
+XX
 // (33.6 MB, 5 TB/s) where parts of 64 x 64 tiles and their join took 14.6.
 constexpr int kFewRows = 32;
 constexpr int kFewWaves = 8;
@@ -918,12 +918,12 @@ __global__ void __launch_bounds__(64 * kFewWaves) linear_few(Few p)
 #pragma unroll
     for (int b = 0; b < MB; ++b) acc[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const int whole = p.K / KS;
-    int s = wave;
-    for (; s + kFewWaves * (U - 1) < whole; s += kFewWaves * U) {
+    int done = 0;
+    for (; done + kFewWaves * U <= whole; done += kFewWaves * U) {
         u32x4 fw[U], fx[U][MB];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t at = (int64_t)((s + u * kFewWaves) * KS + k0) * ES;
+            const int64_t at = (int64_t)((done + wave * U + u) * KS + k0) * ES;
             fw[u] = load16(w + at);
 #pragma unroll
             for (int b = 0; b < MB; ++b) fx[u][b] = load16(x[b] + at);
@@ -933,6 +933,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) linear_few(Few p)
 #pragma unroll
             for (int b = 0; b < MB; ++b) mma16<DT>(acc[b], fw[u], fx[u][b]);
     }
+    int s = done + wave;
     for (; s < whole; s += kFewWaves) {
         const int64_t at = (int64_t)(s * KS + k0) * ES;
         const u32x4 fw = load16(w + at);
@@ -979,26 +980,41 @@ struct Join {
     Epilogue e;
 };
 
+// 64 vectors of columns to a workgroup; its four wavefronts take the parts in turns,
+// and their sums are added in the wavefronts' order.
 template <int DT>
 __global__ void __launch_bounds__(256) linear_join(Join p)
 {
-    constexpr int V = 16 / elem_size(DT);
+    constexpr int V = 8;
     const int per_row = (p.cols + V - 1) / V;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t i = (int64_t)blockIdx.x * 64 + lane;
     const int64_t m = i / per_row;
-    if (m >= p.rows) return;
     const int n = (int)(i % per_row) * V;
     float v[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = 0.0f;
-    const float *src = p.partial + m * p.pld + n;
-#pragma unroll 8
-    for (int s = 0; s < p.split; ++s) {
-        float w[V];
-        load_elems<FLASHBEV_F32>(src + (int64_t)s * p.rows * p.pld, w);
+    if (m < p.rows) {
+        const float *src = p.partial + m * p.pld + n;
+#pragma unroll 4
+        for (int s = wave; s < p.split; s += 4) {
+            float w[V];
+            load_elems<FLASHBEV_F32>(src + (int64_t)s * p.rows * p.pld, w);
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] += w[e];
+            for (int e = 0; e < V; ++e) v[e] += w[e];
+        }
     }
+    __shared__ float part[3][V][64];
+    if (wave > 0) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) part[wave - 1][e][lane] = v[e];
+    }
+    __syncthreads();
+    if (wave > 0 || m >= p.rows) return;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] += part[w][e][lane];
     epilogue<DT>(p.e, m, n, p.cols, v);
 }
 
@@ -1033,6 +1049,7 @@ __global__ void __launch_bounds__(256) linear_slope(Slope p)
     for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
     if (n < p.N) {
         const bool whole = n + 8 <= p.N;
+#pragma unroll 2
         for (int64_t m = r0 + (threadIdx.x >> 5); m < r1; m += 8) {
             float g[8], v[8];
             const char *gp = static_cast<const char *>(p.grad) + (m * p.ldg + n) * (p.grad_f32 ? 4 : es);
@@ -1263,11 +1280,11 @@ int product(const TilePlan &t, int dt, const void *a, int64_t lda, const void *b
                                   : launch_tiles<FLASHBEV_BF16, AX, BX>(g, t, st);
     if (rc || t.split == 1) return rc;
     Join j{g.partial, g.pld, g.rows, g.cols, t.split, e};
-    const uint64_t vecs = (uint64_t)rows * ((cols + 16 / es - 1) / (16 / es));
+    const uint64_t vecs = (uint64_t)rows * ((cols + 7) / 8);
     const void *fn = dt == FLASHBEV_F32   ? (const void *)linear_join<FLASHBEV_F32>
                      : dt == FLASHBEV_F16 ? (const void *)linear_join<FLASHBEV_F16>
                                           : (const void *)linear_join<FLASHBEV_BF16>;
-    return launch_kernel(fn, (vecs + 255) / 256, 256, j, 0, st);
+    return launch_kernel(fn, (vecs + 63) / 64, 256, j, 0, st);
 }
 
 int check_sizes(const flashblock_linear *p)

@@ -221,8 +221,11 @@ struct Norm {
     float eps, scale;
 };
 
+// Eight wavefronts a SIMD (64 registers) where 16-bit rows allow it: with 66, a row of
+// 4096 left room for three workgroups of four (124 us for 4 x 4096 x 4096, 112 with it).
 template <int DT, int SDT, int T, int NV, bool POST>
-__global__ void __launch_bounds__(T > 256 ? T : 256) norm_forward(Norm p)
+__global__ void __launch_bounds__(T > 256 ? T : 256, DT != FLASHBEV_F32 && NV == 1 ? 8 : 1)
+    norm_forward(Norm p)
 {
     using R = Row<T, NV, 8>;
     constexpr int E = R::E;
@@ -331,16 +334,28 @@ __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward 
     const float inv = 1.0f / (float)p.C;
     const bool norm = p.norm != FLASHBLOCK_NORM_NONE && p.grad_y;
     const bool reads_x = POST || p.partial[kGate];
-    // the vectors of this sample, and their gradients over the range
+    // The vectors of this sample, in registers over the range (read again for each
+    // row where a lane holds more than four channels), and their gradients.
+    constexpr bool HOLD = NV == 1;
     float weight[E], gate[E], post_weight[E], post_bias[E];
-    R::template params<DT>(p.weight, 0, p.params_f32, t, p.C, 1.0f, weight);
-    R::template params<DT>(p.gate, group * p.C, p.params_f32, t, p.C, 1.0f, gate);
-    if constexpr (POST) {
-        R::template params<DT>(p.post_weight, 0, p.params_f32, t, p.C, 1.0f, post_weight);
-        R::template params<DT>(p.post_bias, 0, p.params_f32, t, p.C, 0.0f, post_bias);
-    }
+    auto read_weight = [&] { R::template params<DT>(p.weight, 0, p.params_f32, t, p.C, 1.0f, weight); };
+    auto read_gate = [&] {
+        R::template params<DT>(p.gate, group * p.C, p.params_f32, t, p.C, 1.0f, gate);
 #pragma unroll
-    for (int e = 0; e < E; ++e) gate[e] *= p.scale;
+        for (int e = 0; e < E; ++e) gate[e] *= p.scale;
+    };
+    auto read_post_weight = [&] {
+        if constexpr (POST) R::template params<DT>(p.post_weight, 0, p.params_f32, t, p.C, 1.0f, post_weight);
+    };
+    auto read_post_bias = [&] {
+        if constexpr (POST) R::template params<DT>(p.post_bias, 0, p.params_f32, t, p.C, 0.0f, post_bias);
+    };
+    if constexpr (HOLD) {
+        read_weight();
+        read_gate();
+        read_post_weight();
+        read_post_bias();
+    }
     float acc[kVectors][E];
 #pragma unroll
     for (int k = 0; k < kVectors; ++k)
@@ -350,7 +365,7 @@ __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward 
     // The next row's loads are in flight while a row's three sums are formed (a row
     // at a time, 8331 x 771 half took 82 us).  Rows of more than 4096 channels have no
     // registers for that.
-    constexpr bool AHEAD = T < 1024 || NV == 1;
+    constexpr bool AHEAD = NV == 1;
     typename R::template Raw<SDT> raw_ds, raw_s;
     typename R::template Raw<DT> raw_x, raw_g;
     auto fetch = [&](int64_t first) {
@@ -382,6 +397,7 @@ __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward 
         if (AHEAD && first + R::ROWS < m1) fetch(first + R::ROWS);
         float one[3] = {0.0f, 0.0f, 0.0f};
         if (norm) {
+            if constexpr (!HOLD) read_weight();
             one[0] = R::sum(s);
             one[1] = R::dot(g, weight);
         }
@@ -425,7 +441,9 @@ __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward 
 #pragma unroll
             for (int e = 0; e < E; ++e) x[e] *= rx;
         }
+        if constexpr (!HOLD) read_post_weight();
         if (p.partial[kGate]) {
+            if constexpr (!HOLD) read_post_bias();
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 float u = x[e];
@@ -433,6 +451,7 @@ __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward 
                 if (in) acc[kGate][e] = __builtin_fmaf(ds[e], u, acc[kGate][e]);
             }
         }
+        if constexpr (!HOLD) read_gate();
 #pragma unroll
         for (int e = 0; e < E; ++e) ds[e] *= gate[e];
         if constexpr (POST) {
@@ -532,8 +551,10 @@ __global__ void __launch_bounds__(256) norm_join(NormJoin p)
 // ---------------------------------------------------------------------------
 // The lanes of a row: a vector of `v` channels each, up to 1024 lanes.  Forward, 8
 // channels; backward, 4, for its five sums and four vectors in registers (with 8, at
-// 145 to 200 of them, two or three wavefronts fit a SIMD: 40000 x 256 bfloat16 52 us,
-// 16384 x 4096 303).
+// 145 to 200 of them, two or three wavefronts fit a SIMD: 40000 x 256 bfloat16 took 52
+// us and takes 34, 16384 x 4096 303 and 197).  Wider rows of the backward spill: up to
+// 8192 channels 512 lanes with 256 registers do it less than 1024 with 128 (8192 x 8192
+// with both norms 483 us and 749, without a post norm 261 and 244).
 struct Shape {
     int lanes, rows, threads;   // of a row; rows and threads of a workgroup
 };
@@ -542,6 +563,7 @@ Shape shape_of(int C, int v)
 {
     int t = 8;
     while (t < 1024 && v * t < C) t *= 2;
+    if (v == 4 && C > 4096 && C <= 8192) t = 512;
     return {t, t >= 256 ? 1 : 256 / t, t > 256 ? t : 256};
 }
 
@@ -565,7 +587,7 @@ template <int DT, int SDT, bool POST>
 const void *backward_kernel(int C)
 {
     if (C > 8192) return (const void *)norm_backward<DT, SDT, 1024, 4, POST>;
-    if (C > 4096) return (const void *)norm_backward<DT, SDT, 1024, 2, POST>;
+    if (C > 4096) return (const void *)norm_backward<DT, SDT, 512, 4, POST>;
     switch (shape_of(C, 4).lanes) {
     case 8: return (const void *)norm_backward<DT, SDT, 8, 1, POST>;
     case 16: return (const void *)norm_backward<DT, SDT, 16, 1, POST>;
