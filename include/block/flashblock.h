@@ -55,6 +55,8 @@
 extern "C" {
 #endif
 
+/* Largest number of rows. */
+#define FLASHBLOCK_ROWS_MAX 2147483392
 /* Largest row width (K or N) and row stride, in elements. */
 #define FLASHBLOCK_WIDTH_MAX 262144
 #define FLASHBLOCK_LD_MAX 1048576

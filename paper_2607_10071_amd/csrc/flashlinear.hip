@@ -1294,7 +1294,7 @@ int check_sizes(const flashblock_linear *p)
         return FLASHBEV_ERR_DTYPE;
     if (p->act < FLASHBLOCK_ACT_NONE || p->act > FLASHBLOCK_ACT_SILU || !finite_value(p->scale))
         return FLASHBEV_ERR_VALUE;
-    if (p->M > 0x7fffffff || p->K > FLASHBLOCK_WIDTH_MAX || p->N > FLASHBLOCK_WIDTH_MAX)
+    if (p->M > FLASHBLOCK_ROWS_MAX || p->K > FLASHBLOCK_WIDTH_MAX || p->N > FLASHBLOCK_WIDTH_MAX)
         return FLASHBEV_ERR_UNSUPPORTED;
     return FLASHBEV_OK;
 }

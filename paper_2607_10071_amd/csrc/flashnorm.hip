@@ -628,7 +628,7 @@ int check_norm(const flashblock_norm *p)
         (p->norm == FLASHBLOCK_NORM_NONE && p->post_norm == FLASHBLOCK_NORM_NONE) ||
         !finite_value(p->scale) || !finite_value(p->eps) || !(p->eps > 0.0f))
         return FLASHBEV_ERR_VALUE;
-    if (p->M > 0x7fffffff || p->C > FLASHBLOCK_NORM_MAX) return FLASHBEV_ERR_UNSUPPORTED;
+    if (p->M > FLASHBLOCK_ROWS_MAX || p->C > FLASHBLOCK_NORM_MAX) return FLASHBEV_ERR_UNSUPPORTED;
     return FLASHBEV_OK;
 }
 

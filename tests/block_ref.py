@@ -26,9 +26,10 @@ def act(name, v):
     if name == "relu":
         return v.clamp(min=0)
     if name == "gelu":
-        return 0.5 * v * (1 + torch.erf(v / math.sqrt(2)))
-    if name == "gelu_tanh":
-        return 0.5 * v * (1 + torch.tanh(math.sqrt(2 / math.pi) * (v + 0.044715 * v ** 3)))
+        # (1 + erf(x) cancels for negative x, in float64 too)
+        return 0.5 * v * torch.erfc(-v / math.sqrt(2))
+    if name == "gelu_tanh":   # (1 + tanh z) / 2 = 1 / (1 + exp(-2 z))
+        return v / (1 + torch.exp(-2 * math.sqrt(2 / math.pi) * (v + 0.044715 * v ** 3)))
     if name == "silu":
         return v / (1 + torch.exp(-v))
     return v
@@ -38,7 +39,7 @@ def slope(name, v):
     if name == "relu":
         return (v > 0).double()
     if name == "gelu":
-        return 0.5 * (1 + torch.erf(v / math.sqrt(2))) + v * torch.exp(-v * v / 2) / math.sqrt(2 * math.pi)
+        return 0.5 * torch.erfc(-v / math.sqrt(2)) + v * torch.exp(-v * v / 2) / math.sqrt(2 * math.pi)
     if name == "gelu_tanh":
         c = math.sqrt(2 / math.pi)
         t = torch.tanh(c * (v + 0.044715 * v ** 3))

@@ -118,12 +118,13 @@ def passes(fb, seed=0, dtype=torch.bfloat16, M=600, C=256):
     rand = lambda *s: torch.randn(s, generator=gen, device="cuda").to(dtype)
     ins = {"x": rand(M, C), "w": rand(512, C), "b": rand(512), "g": rand(M, 512), "pre": rand(M, 512),
            "r": rand(M, C), "gate": rand(C), "n": rand(C), "long": rand(96, 8192), "wl": rand(64, 8192),
-           "one": rand(1, C)}
+           "one": rand(1, C), "many": rand(4096, 512), "wide": rand(4096, 512)}
 
     def run():
         i = ins
         out = [fb.linear_forward(i["x"], i["w"], i["b"], "gelu"),
                fb.linear_forward(i["long"], i["wl"]), fb.linear_forward(i["one"], i["w"], i["b"])]
+        out.append(fb.linear_forward(i["many"], i["wide"]))   # 256 x 256 tiles
         out += fb.linear_backward(i["g"], i["x"], i["w"], i["pre"], "gelu", 0.5).values()
         y, s = fb.norm_forward(i["x"], i["n"], None, i["r"], i["gate"], 0.5, "rms", "layer")
         out += [y, s]

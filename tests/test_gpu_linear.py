@@ -114,6 +114,44 @@ def test_forward_leading_dimensions(fb, device):
                                                                            w[:, :8].contiguous()))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu", "relu"])
+def test_activations_of_extreme_values(fb, device, act, dtype):
+    """Each activation over its whole range, through a product with the identity:
+    tails, values far past them, both infinities and NaN; and its slope."""
+    dt = ref.DTYPES[dtype]
+    big = float(torch.finfo(dt).max) / 4
+    v = torch.cat([torch.linspace(-30, 30, 4801), torch.tensor([-big, big, -1e4, 1e4, -100.0, 100.0, 0.0])])
+    v = v.to(dt)
+    x = torch.zeros(v.numel(), 8, dtype=dt)
+    x[:, 0] = v
+    w = torch.zeros(8, 8, dtype=dt)
+    w[0, 0] = 1
+    got = fb.linear_forward(x.cuda(), w.cuda(), None, act)[:, 0]
+    d = v.double()
+    # relative to the result in the tails as well: an exponential's float32 exponent t
+    # (v^2 / 2; 0.08 |v|^3 + 1.6 |v|; |v|) is off by a few |t| 2^-24, and the exponential
+    # by that share of itself; below 2^-126 it is 0, times |v| at most 2^-120
+    a = d.abs().clamp(max=40)
+    t = {"gelu": a * a / 2, "gelu_tanh": 0.08 * a ** 3 + 1.6 * a, "silu": a, "relu": 0 * a}[act]
+    want = torch.where(d.abs() < 40, ref.act(act, d), d.clamp(min=0))
+    ref.close(got, want, (16 + 4 * t) * ref.F32 * want.abs() + 2.0 ** -120)
+    pre = torch.zeros_like(x)
+    pre[:, 0] = v
+    g = torch.zeros_like(x)
+    g[:, 0] = 1
+    slope = fb.linear_backward(g.cuda(), x.cuda(), w.cuda(), pre.cuda(), act, want=("x",))["x"][:, 0]
+    want = torch.where(d.abs() < 40, ref.slope(act, d), (d > 0).double())
+    ref.close(slope, want, 24 * ref.F32 * (1 + d.abs().clamp(max=40)) * torch.ones_like(d))
+    inf = torch.zeros(3, 8, dtype=dt, device=device)
+    inf[:, 0] = torch.tensor([float("inf"), -float("inf"), float("nan")])
+    eye = torch.zeros(1, 8, dtype=dt, device=device)
+    eye[0, 0] = 1
+    got = fb.linear_forward(inf, eye, None, act)[:, 0]
+    assert got[0] == float("inf") and got[2].isnan()
+    assert got[1] == 0 or (act in ("silu", "gelu_tanh") and got[1].isnan())   # -inf times 0
+
+
 def test_nan_and_infinity_stay_in_their_rows(fb, device):
     """A row of NaN or infinities reaches its own row of the output alone, and a
     channel of the weight its own channel, whatever shares their tiles."""
@@ -249,7 +287,7 @@ def test_autograd_second_derivative_is_refused(fb, device):
 
 def test_empty(fb, device):
     for dt in ref.DTYPES.values():
-        for M, K, N in ((0, 8, 8), (8, 8, 0), (3, 0, 5), (0, 0, 0)):
+        for M, K, N in ((0, 8, 8), (8, 8, 0), (3, 0, 5), (40, 0, 16), (0, 0, 0), (40, 8, 0)):
             x, w, b = (torch.ones(s, dtype=dt, device=device) for s in ((M, K), (N, K), (N,)))
             out = fb.linear_forward(x, w, b, "relu")
             assert out.shape == (M, N) and (out == 1).all()
@@ -265,8 +303,11 @@ def test_long_rows_past_32_bits(fb, device):
     x[-5:] = torch.randn(5, K, device=device).to(torch.bfloat16)
     w = torch.randn(N, K, device=device).to(torch.bfloat16)
     out = fb.linear_forward(x, w)
-    assert torch.equal(out[-5:], fb.linear_forward(x[-5:], w)) or torch.allclose(
-        out[-5:].float(), fb.linear_forward(x[-5:], w).float(), rtol=2.0 ** -7, atol=2.0 ** -7)
+    # five rows take another kernel: the same sums in another order, each rounded
+    mag = x[-5:].double().abs() @ w.double().abs().t()
+    exact = x[-5:].double() @ w.double().t()
+    for got in (out[-5:], fb.linear_forward(x[-5:], w)):
+        assert ((got.double() - exact).abs() <= 2.0 ** -8 * exact.abs() * 1.01 + K * 2.0 ** -24 * mag).all()
     assert (out[:-5] == 0).all()
     g = torch.ones(M, N, dtype=torch.bfloat16, device=device)
     r = fb.linear_backward(g, x, w)

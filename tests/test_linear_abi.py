@@ -72,6 +72,7 @@ def test_packed_structure_is_the_c_one():
     (dict(dtype=3), "ERR_DTYPE"), (dict(dtype=-1), "ERR_DTYPE"), (dict(out_dtype=1), "ERR_DTYPE"),
     (dict(act=5), "ERR_VALUE"), (dict(act=-1), "ERR_VALUE"), (dict(scale=float("nan")), "ERR_VALUE"),
     (dict(scale=float("inf")), "ERR_VALUE"), (dict(M=1 << 31), "ERR_UNSUPPORTED"),
+    (dict(M=(1 << 31) - 255), "ERR_UNSUPPORTED"),
     (dict(K=(1 << 18) + 1, ldx=1 << 19, ldw=1 << 19), "ERR_UNSUPPORTED"),
     (dict(N=(1 << 18) + 1), "ERR_UNSUPPORTED"), (dict(ldx=(1 << 20) + 1), "ERR_UNSUPPORTED"),
 ])
@@ -152,11 +153,11 @@ def test_backward_reads_only_what_its_gradients_need():
 
 def test_sizes_do_not_wrap():
     n = ctypes.c_uint64()
-    big = pack(M=(1 << 31) - 1, K=1 << 18, N=1 << 18, ldx=1 << 18, ldw=1 << 18, act=2, ldp=1 << 18,
+    big = pack(M=(1 << 31) - 256, K=1 << 18, N=1 << 18, ldx=1 << 18, ldw=1 << 18, act=2, ldp=1 << 18,
                ldo=1 << 18)
     call = fb._packed_call("flashblock_linear_backward_workspace_size", "PiiiP")
     assert call(big, 1, 1, 1, ctypes.byref(n)) == 0
-    assert n.value >= ((1 << 31) - 1) * (1 << 18) * 2
+    assert n.value >= ((1 << 31) - 256) * (1 << 18) * 2
 
 
 class _Cuda:
