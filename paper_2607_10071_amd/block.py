@@ -155,6 +155,11 @@ def linear_forward(x, weight, bias=None, activation="none", residual=None, scale
     Sums are float32, each output is rounded once.  Returns ``out``; the call is
     asynchronous.
     """
+    return _linear_forward(x, weight, bias, activation, residual, scale, out, out_dtype, pre, stream)[0]
+
+
+def _linear_forward(x, weight, bias, activation, residual, scale, out, out_dtype, pre, stream):
+    """linear_forward's (out, sizes for _linear_gradients)."""
     import torch
 
     M, ldx = _rows(x, "x")
@@ -177,8 +182,8 @@ def linear_forward(x, weight, bias=None, activation="none", residual=None, scale
         _same(pre, "pre", x.dtype, shape)
         ldp = _rows(pre, "pre")[1]
     b = _vector(bias, "bias", x.dtype, N)
-    args = _PACK_LINEAR.pack(M, ldx, ldw, ldr, ldo, ldp, K, N, code,
-                             code if odt == x.dtype else 0, _act_code(activation), scale)
+    act, out_code = _act_code(activation), code if odt == x.dtype else 0
+    args = _PACK_LINEAR.pack(M, ldx, ldw, ldr, ldo, ldp, K, N, code, out_code, act, scale)
     dev = _one_device(x, weight, bias, residual, out, pre)
     s = _stream_handle(stream, dev)
     need = _linear_need(M, K, N, code)
@@ -189,7 +194,7 @@ def linear_forward(x, weight, bias=None, activation="none", residual=None, scale
                   _addr(pre), _addr(ws), need, s)
     if rc != 0:
         raise FlashBevError(rc, "flashblock_linear_forward")
-    return out
+    return out, (M, ldx, ldw, K, N, code, out_code, act, scale, dev)
 
 
 def _size(name: str, kinds: str, *args) -> int:
@@ -268,22 +273,28 @@ def linear_backward(grad_out, x, weight, pre=None, activation="none", scale: flo
         outs[name] = given
     if all(t is None for t in outs.values()):
         return outs
-    args = _PACK_LINEAR.pack(M, ldx, ldw, N, ldo, ldp, K, N, code, code if odt == x.dtype else 0, act,
-                             scale)
     dev = _one_device(grad_out, x, weight, pre if act else None, *outs.values())
+    sizes = (M, ldx, ldw, K, N, code, code if odt == x.dtype else 0, act, scale, dev)
+    _linear_gradients(sizes, grad_out, ldo, x, weight, pre if act else None, ldp, outs["x"],
+                      ld.get("x", K), outs["weight"], ld.get("weight", K), outs["bias"], stream)
+    return outs
+
+
+def _linear_gradients(sizes, grad_out, ldo, x, weight, pre, ldp, grad_x, ldgx, grad_weight, ldgw,
+                      grad_bias, stream):
+    """The backward call on checked tensors."""
+    M, ldx, ldw, K, N, code, out_code, act, scale, dev = sizes
+    args = _PACK_LINEAR.pack(M, ldx, ldw, N, ldo, ldp, K, N, code, out_code, act, scale)
     s = _stream_handle(stream, dev)
-    need = _linear_backward_need(M, K, N, code, code if odt == x.dtype else 0, act,
-                                 outs["x"] is not None, outs["weight"] is not None,
-                                 outs["bias"] is not None)
+    need = _linear_backward_need(M, K, N, code, out_code, act, grad_x is not None,
+                                 grad_weight is not None, grad_bias is not None)
     ws = _workspace(need, dev, s) if need else None
     call = _packed_call("flashblock_linear_backward", "PPPPPPQPQPPQP")
     with _on_device(dev):
-        rc = call(args, grad_out.data_ptr(), x.data_ptr(), weight.data_ptr(),
-                  pre.data_ptr() if act else 0, _addr(outs["x"]), ld.get("x", K),
-                  _addr(outs["weight"]), ld.get("weight", K), _addr(outs["bias"]), _addr(ws), need, s)
+        rc = call(args, grad_out.data_ptr(), x.data_ptr(), weight.data_ptr(), _addr(pre),
+                  _addr(grad_x), ldgx, _addr(grad_weight), ldgw, _addr(grad_bias), _addr(ws), need, s)
     if rc != 0:
         raise FlashBevError(rc, "flashblock_linear_backward")
-    return outs
 
 
 _VECTORS = ("gate", "weight", "bias", "post_weight", "post_bias")
@@ -361,6 +372,13 @@ def norm_forward(x, weight=None, bias=None, residual=None, gate=None, scale: flo
     N(s) reads s as it is stored.  Returns (y, s); s is x itself where nothing
     changes it.  Asynchronous.
     """
+    return _norm_forward(x, weight, bias, residual, gate, scale, norm, post_norm, post_weight, post_bias,
+                         eps, out, out_s, stream)[:2]
+
+
+def _norm_forward(x, weight, bias, residual, gate, scale, norm, post_norm, post_weight, post_bias, eps,
+                  out, out_s, stream):
+    """norm_forward's (y, s, sizes for _norm_gradients)."""
     import torch
 
     M, ldx = _rows(x, "x")
@@ -389,8 +407,9 @@ def norm_forward(x, weight=None, bias=None, residual=None, gate=None, scale: flo
     else:
         _same(out, "out", x.dtype, x.shape)
         ldy = _rows(out, "out")[1]
-    args = _PACK_NORM.pack(M, ldx, ldr, lds, ldy, groups, C, code, code if sdt == x.dtype else 0,
-                           code if pdt is None or pdt == x.dtype else 0, kind, post, eps, scale)
+    types = (code, code if sdt == x.dtype else 0, code if pdt is None or pdt == x.dtype else 0, kind, post,
+             eps, scale)
+    args = _PACK_NORM.pack(M, ldx, ldr, lds, ldy, groups, C, *types)
     dev = _one_device(x, weight, bias, residual, gate, post_weight, post_bias, out, out_s)
     s = _stream_handle(stream, dev)
     call = _packed_call("flashblock_norm_forward", "PPPPPPP")
@@ -398,7 +417,7 @@ def norm_forward(x, weight=None, bias=None, residual=None, gate=None, scale: flo
         rc = call(args, vectors, x.data_ptr(), _addr(residual), _addr(out_s), _addr(out), s)
     if rc != 0:
         raise FlashBevError(rc, "flashblock_norm_forward")
-    return out, x if same else out_s
+    return out, x if same else out_s, (M, ldx, ldx if same else lds, groups, C, types, dev)
 
 
 def norm_backward(grad_y, grad_s, x, s, weight=None, gate=None, scale: float = 1.0, norm="layer",
@@ -434,26 +453,35 @@ def norm_backward(grad_y, grad_s, x, s, weight=None, gate=None, scale: float = 1
     if grad_s is not None:
         _same(grad_s, "grad_s", sdt, x.shape)
         ldgs = _rows(grad_s, "grad_s")[1]
+    for k in want:
+        if k not in _NORM_INPUTS:
+            raise ValueError(f"want takes {_NORM_INPUTS}")
+    if not want:
+        return {}
+    dev = _one_device(grad_y, grad_s, x, s, weight, gate, post_weight, post_bias)
+    types = (code, code if sdt == x.dtype else 0, code if pdt == x.dtype else 0, kind, post, eps, scale)
+    return _norm_gradients((M, ldx, lds, groups, C, types, dev), grad_y, ldgy, grad_s, ldgs, x, s, gate,
+                           vectors, pdt, want, stream)
+
+
+def _norm_gradients(sizes, grad_y, ldgy, grad_s, ldgs, x, s, gate, vectors, pdt, want, stream):
+    """The backward call on checked tensors: a dict of the gradients in ``want``."""
+    import torch
+
+    M, ldx, lds, groups, C, types, dev = sizes
     outs = {}
     for k in want:
         if k == "x":
             outs[k] = torch.empty_like(x, memory_format=torch.contiguous_format)
         elif k == "residual":
             outs[k] = torch.empty_like(s, memory_format=torch.contiguous_format)
-        elif k not in _VECTORS:
-            raise ValueError(f"want takes 'x', 'residual' and {_VECTORS}")
-        elif k == "gate":
-            outs[k] = torch.empty((C,) if gate is None else gate.shape, dtype=pdt, device=x.device)
         else:
-            outs[k] = torch.empty(C, dtype=pdt, device=x.device)
-    if not outs:
-        return outs
-    args = _PACK_NORM.pack(M, ldx, ldgs, lds, ldgy, groups, C, code, code if sdt == x.dtype else 0,
-                           code if pdt == x.dtype else 0, kind, post, eps, scale)
-    grads = _PACK_VECTORS.pack(*(_addr(outs.get(k)) for k in _VECTORS))
-    dev = _one_device(grad_y, grad_s, x, s, weight, gate, post_weight, post_bias)
+            outs[k] = torch.empty((C,) if k != "gate" or gate is None else gate.shape, dtype=pdt,
+                                  device=dev)
+    args = _PACK_NORM.pack(M, ldx, ldgs, lds, ldgy, groups, C, *types)
+    grads = _PACK_VECTORS.pack(*[_addr(outs.get(k)) for k in _VECTORS])
     st = _stream_handle(stream, dev)
-    need = _norm_need(M, groups, C, tuple(k in outs for k in _VECTORS))
+    need = _norm_need(M, groups, C, tuple([k in outs for k in _VECTORS]))
     ws = _workspace(need, dev, st) if need else None
     call = _packed_call("flashblock_norm_backward", "PPPPPPPQPQPPQP")
     with _on_device(dev):
@@ -470,13 +498,15 @@ def norm_backward(grad_y, grad_s, x, s, weight=None, gate=None, scale: float = 1
 _AUTOGRAD = {}
 
 
-def _as_rows(t):
-    """A gradient as it came where its rows are at one stride, else a copy."""
-    try:
-        _rows(t, "gradient")
-        return t
-    except ValueError:
-        return t.contiguous()
+def _as_rows(t, width: int):
+    """(a gradient as it came, its row stride) where its rows are at one stride,
+    else of a copy."""
+    if not t.is_contiguous():
+        try:
+            return t, _strided_rows(t, "gradient")[1]
+        except ValueError:
+            t = t.contiguous()
+    return t, width
 
 
 def _autograd_functions():
@@ -486,26 +516,41 @@ def _autograd_functions():
     import torch
     from torch.autograd.function import once_differentiable
 
+    # The gradients that autograd hands over fit the forward's outputs, so only
+    # their strides are looked at.
+
     def linear_grads(ctx, grad_out):
         x, weight, pre = ctx.saved_tensors
-        activation, scale = ctx.meta
         needs = ctx.needs_input_grad
-        want = tuple(k for k, n in zip(("x", "weight", "bias"), needs) if n)
         residual = grad_out if needs[3] else None
-        if not want:
+        if not (needs[0] or needs[1] or needs[2]):
             return None, None, None, residual, None, None, None
-        r = linear_backward(_as_rows(grad_out), x, weight, pre, activation, scale, want)
-        return r["x"], r["weight"], r["bias"], residual, None, None, None
+        M, K, N, *rest = ctx.sizes
+        g, ldo = _as_rows(grad_out, N)
+        # (hooks on saved tensors may have moved them: their strides are read here)
+        x, ldx = _as_rows(x, K)
+        weight, ldw = _as_rows(weight, K)
+        gx = torch.empty_like(x, memory_format=torch.contiguous_format) if needs[0] else None
+        gw = torch.empty_like(weight, memory_format=torch.contiguous_format) if needs[1] else None
+        gb = torch.empty(N, dtype=x.dtype, device=x.device) if needs[2] else None
+        _linear_gradients((M, ldx, ldw, K, N, *rest), g, ldo, x, weight, pre, N, gx, K, gw, K, gb, None)
+        return gx, gw, gb, residual, None, None, None
 
     def norm_grads(ctx, grad_y, grad_s):
         x, s, weight, gate, post_weight, post_bias = ctx.saved_tensors
-        scale, norm, post_norm, eps = ctx.meta
-        want = tuple(k for k, n in zip(_NORM_INPUTS, ctx.needs_input_grad) if n)
-        r = {}
-        if grad_y is not None or grad_s is not None:
-            r = norm_backward(None if grad_y is None else _as_rows(grad_y),
-                              None if grad_s is None else _as_rows(grad_s), x, x if s is None else s,
-                              weight, gate, scale, norm, post_norm, post_weight, post_bias, eps, want)
+        if grad_y is None and grad_s is None:
+            return (None,) * 11
+        (M, groups, C, types, dev), want, pdt = ctx.sizes
+        ldgy = ldgs = C
+        x, ldx = _as_rows(x, C)
+        s, lds = (x, ldx) if s is None else _as_rows(s, C)
+        if grad_y is not None:
+            grad_y, ldgy = _as_rows(grad_y, C)
+        if grad_s is not None:
+            grad_s, ldgs = _as_rows(grad_s, C)
+        vectors = _PACK_VECTORS.pack(_addr(gate), _addr(weight), 0, _addr(post_weight), _addr(post_bias))
+        r = _norm_gradients((M, ldx, lds, groups, C, types, dev), grad_y, ldgy, grad_s, ldgs, x, s, gate,
+                            vectors, pdt, want, None)
         return (*map(r.get, _NORM_INPUTS), None, None, None, None)
 
     # the wrapper, which refuses a second derivative, only where a graph of the
@@ -518,9 +563,10 @@ def _autograd_functions():
             pre = None
             if _act_code(activation) and any(ctx.needs_input_grad[:3]):
                 pre = torch.empty((*x.shape[:-1], weight.shape[0]), dtype=x.dtype, device=x.device)
-            out = linear_forward(x, weight, bias, activation, residual, scale, None, out_dtype, pre)
+            out, sizes = _linear_forward(x, weight, bias, activation, residual, scale, None, out_dtype,
+                                         pre, None)
+            ctx.sizes = sizes[:1] + sizes[3:]   # without the strides
             ctx.save_for_backward(x, weight, pre)
-            ctx.meta = (activation, scale)
             return out
 
         @staticmethod
@@ -532,12 +578,18 @@ def _autograd_functions():
         def forward(ctx, x, residual, gate, weight, bias, post_weight, post_bias, scale, norm,
                     post_norm, eps):
             ctx.set_materialize_grads(False)
-            y, s = norm_forward(x, weight, bias, residual, gate, scale, norm, post_norm, post_weight,
-                                post_bias, eps)
+            y, s, sizes = _norm_forward(x, weight, bias, residual, gate, scale, norm, post_norm,
+                                        post_weight, post_bias, eps, None, None, None)
             if s is x:
                 s = None
             ctx.save_for_backward(x, s, weight, gate, post_weight, post_bias)
-            ctx.meta = (scale, norm, post_norm, eps)
+            pdt = x.dtype
+            for t in (gate, weight, bias, post_weight, post_bias):
+                if t is not None:
+                    pdt = t.dtype
+                    break
+            want = [k for k, n in zip(_NORM_INPUTS, ctx.needs_input_grad) if n]
+            ctx.sizes = sizes[:1] + sizes[3:], want, pdt   # without the strides
             return y, s
 
         @staticmethod

@@ -712,7 +712,7 @@ __device__ __forceinline__ void write_any(const Gemm &p, int part, int m, int n,
 }
 
 template <int DT, bool AX, bool BX, int BM, int BN, int WM, int WN, int S>
-__global__ void __launch_bounds__(WM *WN * 64, 2) linear_stream(Gemm p)
+__global__ void __launch_bounds__(WM *WN * 64, BM == 64 ? 4 : 2) linear_stream(Gemm p)
 {
     constexpr int NT = WM * WN * 64;
     constexpr int TM = BM / WM, TN = BN / WN;

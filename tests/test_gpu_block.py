@@ -111,6 +111,26 @@ def test_a_block_around_flashsca(fb, device):
     assert all(torch.isfinite(t.grad).all() and t.grad.abs().max() > 0 for t in (q, feats))
 
 
+def test_saved_tensors_moved_by_hooks(fb, device):
+    """Inputs that are rows inside wider tensors, packed to contiguous copies: the
+    backward goes by the strides of what it gets."""
+    gen = torch.Generator().manual_seed(3)
+    big, w = leaf(gen, 50, 90), leaf(gen, 64, 40)
+    gate = leaf(gen, 64)
+    g = torch.randn(50, 64, generator=gen).cuda()
+
+    def step():
+        x = big[:, 5:45]
+        h = fb.linear_autograd(x, w, None, "silu")
+        y, s = fb.norm_autograd(big[:, 20:84], gate, None, h, gate, post_norm="rms")
+        return torch.autograd.grad([y, s], [big, w, gate], [g, g])
+
+    want = step()
+    with torch.autograd.graph.save_on_cpu():
+        got = step()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def passes(fb, seed=0, dtype=torch.bfloat16, M=600, C=256):
     """A few calls of each kind with workspaces among them, as functions of inputs
     that stay where they are."""
