@@ -562,7 +562,7 @@ __device__ __forceinline__ void columns_of(const f32x16 &acc, int q, float (&v)[
 // (of all, where there are two), each further one before its predecessor's stores.
 // The scheduling barriers keep the compiler from working on all vectors at once, which
 // spilled.
-template <int DT, int ODT, int ACT, bool FULL, int FM, int FN>
+template <int DT, int ODT, int ACT, bool FULL, bool ENDS, int FM, int FN>
 __device__ __forceinline__ void write_tile(const Gemm &p, int m, int n, int lane,
                                            const f32x16 (&acc)[FM][FN])
 {
@@ -579,7 +579,7 @@ __device__ __forceinline__ void write_tile(const Gemm &p, int m, int n, int lane
             for (int g = 0; g < FN; ++g)
 #pragma unroll
                 for (int q = 0; q < 2; ++q)
-                    if (n0 + g * 32 + q * 16 < p.cols) {
+                    if (n0 + g * 32 + q * 16 + 8 <= p.cols) {
 #pragma unroll
                         for (int w = 0; w < OW; ++w)
                             res[f % AHEAD][g][q][w] = load16(r + (g * 32 + q * 16) * OS + w * 16);
@@ -596,7 +596,7 @@ __device__ __forceinline__ void write_tile(const Gemm &p, int m, int n, int lane
         for (int g = 0; g < FN; ++g)
 #pragma unroll
             for (int q = 0; q < 2; ++q)
-                if (n0 + g * 32 + q * 16 < p.cols) {
+                if (n0 + g * 32 + q * 16 + 8 <= p.cols) {
 #pragma unroll
                     for (int w = 0; w < BW; ++w)
                         bias[g][q][w] = load16(b + (g * 32 + q * 16) * ES + w * 16);
@@ -606,18 +606,28 @@ __device__ __forceinline__ void write_tile(const Gemm &p, int m, int n, int lane
     for (int f = 0; f < FM; ++f) {
         const int64_t row = m0 + f * 32;
         float v[FN][2][8];
+        [[maybe_unused]] float end[8];
+        [[maybe_unused]] int at = -1;   // first column of the vector that holds C's last columns, if here
 #pragma unroll
         for (int g = 0; g < FN; ++g)
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
                 float b[8];
                 columns_of(acc[f][g], q, v[g][q]);
+                if constexpr (ENDS) {
+                    const int n1 = n0 + g * 32 + q * 16;
+                    if (n1 < p.cols && n1 + 8 > p.cols) {
+                        at = n1;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) end[i] = v[g][q][i];
+                    }
+                }
                 if (FULL && e.bias) {
                     elems_of<DT>(bias[g][q], b);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) v[g][q][i] += b[i];
                 }
-                if (FULL && e.pre && row < p.rows && n0 + g * 32 + q * 16 < p.cols)
+                if (FULL && e.pre && row < p.rows && n0 + g * 32 + q * 16 + 8 <= p.cols)
                     store_elems<DT>(static_cast<char *>(e.pre) +
                                         (row * e.ldp + n0 + g * 32 + q * 16) * ES, v[g][q]);
 #pragma unroll
@@ -650,8 +660,11 @@ __device__ __forceinline__ void write_tile(const Gemm &p, int m, int n, int lane
         for (int g = 0; g < FN; ++g)
 #pragma unroll
             for (int q = 0; q < 2; ++q)
-                if (row < p.rows && n0 + g * 32 + q * 16 < p.cols)
+                if (row < p.rows && n0 + g * 32 + q * 16 + 8 <= p.cols)
                     store_elems<ODT>(o + (g * 32 + q * 16) * OS, v[g][q]);
+        if constexpr (ENDS) {
+            if (at >= 0 && row < p.rows) epilogue<DT>(e, row, at, p.cols, end);
+        }
         __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -678,8 +691,9 @@ __device__ __forceinline__ void write_part(const Gemm &p, int part, int m, int n
 }
 
 // FULL: the forward, with every activation and type of output; else a gradient
-// in the inputs' type.
-template <int DT, bool FULL, int FM, int FN>
+// in the inputs' type.  ENDS: a forward whose rows end inside a vector of 8 (in
+// kernels of their own: its code in the others cost the value projection 15 us of 55).
+template <int DT, bool FULL, bool ENDS, int FM, int FN>
 __device__ __forceinline__ void write_any(const Gemm &p, int part, int m, int n, int lane,
                                           const f32x16 (&acc)[FM][FN])
 {
@@ -689,29 +703,29 @@ __device__ __forceinline__ void write_any(const Gemm &p, int part, int m, int n,
     if (p.split > 1) return write_part(p, part, m, n, lane, acc);
     constexpr int F32 = FLASHBEV_F32;
     if constexpr (!FULL) {
-        write_tile<DT, DT, FLASHBLOCK_ACT_NONE, FULL>(p, m, n, lane, acc);
+        write_tile<DT, DT, FLASHBLOCK_ACT_NONE, FULL, ENDS>(p, m, n, lane, acc);
     } else if (DT == F32 || !p.e.out_f32) {
         switch (p.e.act) {
-        case FLASHBLOCK_ACT_RELU: return write_tile<DT, DT, FLASHBLOCK_ACT_RELU, FULL>(p, m, n, lane, acc);
-        case FLASHBLOCK_ACT_GELU: return write_tile<DT, DT, FLASHBLOCK_ACT_GELU, FULL>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_RELU: return write_tile<DT, DT, FLASHBLOCK_ACT_RELU, FULL, ENDS>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_GELU: return write_tile<DT, DT, FLASHBLOCK_ACT_GELU, FULL, ENDS>(p, m, n, lane, acc);
         case FLASHBLOCK_ACT_GELU_TANH:
-            return write_tile<DT, DT, FLASHBLOCK_ACT_GELU_TANH, FULL>(p, m, n, lane, acc);
-        case FLASHBLOCK_ACT_SILU: return write_tile<DT, DT, FLASHBLOCK_ACT_SILU, FULL>(p, m, n, lane, acc);
-        default: return write_tile<DT, DT, FLASHBLOCK_ACT_NONE, FULL>(p, m, n, lane, acc);
+            return write_tile<DT, DT, FLASHBLOCK_ACT_GELU_TANH, FULL, ENDS>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_SILU: return write_tile<DT, DT, FLASHBLOCK_ACT_SILU, FULL, ENDS>(p, m, n, lane, acc);
+        default: return write_tile<DT, DT, FLASHBLOCK_ACT_NONE, FULL, ENDS>(p, m, n, lane, acc);
         }
     } else {
         switch (p.e.act) {
-        case FLASHBLOCK_ACT_RELU: return write_tile<DT, F32, FLASHBLOCK_ACT_RELU, FULL>(p, m, n, lane, acc);
-        case FLASHBLOCK_ACT_GELU: return write_tile<DT, F32, FLASHBLOCK_ACT_GELU, FULL>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_RELU: return write_tile<DT, F32, FLASHBLOCK_ACT_RELU, FULL, ENDS>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_GELU: return write_tile<DT, F32, FLASHBLOCK_ACT_GELU, FULL, ENDS>(p, m, n, lane, acc);
         case FLASHBLOCK_ACT_GELU_TANH:
-            return write_tile<DT, F32, FLASHBLOCK_ACT_GELU_TANH, FULL>(p, m, n, lane, acc);
-        case FLASHBLOCK_ACT_SILU: return write_tile<DT, F32, FLASHBLOCK_ACT_SILU, FULL>(p, m, n, lane, acc);
-        default: return write_tile<DT, F32, FLASHBLOCK_ACT_NONE, FULL>(p, m, n, lane, acc);
+            return write_tile<DT, F32, FLASHBLOCK_ACT_GELU_TANH, FULL, ENDS>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_SILU: return write_tile<DT, F32, FLASHBLOCK_ACT_SILU, FULL, ENDS>(p, m, n, lane, acc);
+        default: return write_tile<DT, F32, FLASHBLOCK_ACT_NONE, FULL, ENDS>(p, m, n, lane, acc);
         }
     }
 }
 
-template <int DT, bool AX, bool BX, int BM, int BN, int WM, int WN, int S>
+template <int DT, bool AX, bool BX, int BM, int BN, int WM, int WN, int S, bool ENDS>
 __global__ void __launch_bounds__(WM *WN * 64, BM == 64 ? 4 : 2) linear_stream(Gemm p)
 {
     constexpr int NT = WM * WN * 64;
@@ -854,7 +868,7 @@ __global__ void __launch_bounds__(WM *WN * 64, BM == 64 ? 4 : 2) linear_stream(G
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        write_any<DT, !BX>(p, it.part, it.m0 + wm * TM, it.n0 + wn * TN, lane, acc);
+        write_any<DT, !BX, ENDS>(p, it.part, it.m0 + wm * TM, it.n0 + wn * TN, lane, acc);
         // what the lanes' addresses are made of is computed again rather than kept
         // in registers through the epilogue (where it spilled, the ring's loads
         // waited for its way back)
@@ -1184,11 +1198,12 @@ TilePlan plan_tiles(int64_t rows, int64_t cols, int64_t red, int dt, bool checke
 
 // What the sizes alone say about linear_stream's layout (linear_stream also needs
 // its strides and addresses): widths of whole granules, the reduction axis of an
-// operand along it or the columns of one across it, and outputs of whole vectors.
+// operand along it or the columns of one across it, and a gradient's rows of whole
+// vectors.
 bool whole_granules(int64_t rows, int64_t cols, int64_t red, int dt, bool ax, bool bx)
 {
     const int e = 16 / elem_size(dt);
-    return (ax ? rows : red) % e == 0 && (bx ? cols : red) % e == 0 && cols % 8 == 0;
+    return (ax ? rows : red) % e == 0 && (bx ? cols % 8 : red % e) == 0;
 }
 
 TilePlan plan_forward(const flashblock_linear *p)
@@ -1213,7 +1228,10 @@ TilePlan plan_grad_weight(const flashblock_linear *p)
 template <int DT, bool AX, bool BX, int BM, int BN, int WM, int WN, int S>
 int launch_stream(Gemm &g, hipStream_t st)
 {
-    const void *fn = (const void *)linear_stream<DT, AX, BX, BM, BN, WM, WN, S>;
+    const void *fn = (const void *)linear_stream<DT, AX, BX, BM, BN, WM, WN, S, false>;
+    if constexpr (!BX) {
+        if (g.cols % 8) fn = (const void *)linear_stream<DT, AX, BX, BM, BN, WM, WN, S, true>;
+    }
     constexpr size_t lds = (size_t)S * (BM + BN) * 128;
     g.tiles_m = (g.rows + BM - 1) / BM;
     g.tiles_n = (g.cols + BN - 1) / BN;
