@@ -225,6 +225,7 @@ struct Gemm {
     int64_t lda, ldb;          // bytes
     int rows, cols;            // of C
     int red;                   // length of the reduction axis
+    int padded;                // A's rows end in zeros up to a multiple of 8 elements
     int tiles_m, tiles_n;
     int split;                 // workgroups that share a tile's reduction axis
     int steps;                 // reduction steps for each of them
@@ -788,7 +789,7 @@ __global__ void __launch_bounds__(WM *WN * 64, BM == 64 ? 4 : 2) linear_stream(G
     const char *pa = nullptr, *pb = nullptr;
     bool loading = li < mine;
     auto offsets = [&] {
-        SA::offsets(oa, p.lda, load.m0, p.rows, tid);
+        SA::offsets(oa, p.lda, load.m0, AX && p.padded ? (p.rows + 7) & ~7 : p.rows, tid);
         SB::offsets(ob, p.ldb, load.n0, p.cols, tid);
     };
     auto open = [&] {
@@ -1047,6 +1048,7 @@ struct Slope {
     int M, N, rows;         // rows of a range
     int col_blocks;
     int act, grad_f32;
+    int copy;               // d is grad_out itself: without the scale, which the products take
     float scale;
 };
 
@@ -1083,21 +1085,14 @@ __global__ void __launch_bounds__(256) linear_slope(Slope p)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) g[e] *= act_slope(p.act, v[e]);
             }
+            const float scale = p.copy ? 1.0f : p.scale;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                g[e] *= p.scale;
+                g[e] *= scale;
                 sum[e] += g[e];
             }
-            if (p.d) {
-                char *dp = static_cast<char *>(p.d) + (m * p.ldd + n) * es;
-                if (whole) {
-                    store_elems<DT>(dp, g);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (n + e < p.N) store_elem<DT>(dp, e, g[e]);
-                }
-            }
+            // whole vectors, with zeros past N (ldd is a multiple of 8)
+            if (p.d) store_elems<DT>(static_cast<char *>(p.d) + (m * p.ldd + n) * es, g);
         }
     }
     if (!p.partial) return;
@@ -1109,7 +1104,7 @@ __global__ void __launch_bounds__(256) linear_slope(Slope p)
     float s = 0.0f;
 #pragma unroll
     for (int r = 0; r < 8; ++r) s += part[r][threadIdx.x];
-    if (c < p.N) p.partial[(int64_t)range * p.pld + c] = s;
+    if (c < p.N) p.partial[(int64_t)range * p.pld + c] = p.copy ? s * p.scale : s;
 }
 
 // out[n] = sum over ranges of partial[range][n], in `DT`; 16 columns per workgroup
@@ -1200,29 +1195,39 @@ TilePlan plan_tiles(int64_t rows, int64_t cols, int64_t red, int dt, bool checke
 // its strides and addresses): widths of whole granules, the reduction axis of an
 // operand along it or the columns of one across it, and a gradient's rows of whole
 // vectors.
-bool whole_granules(int64_t rows, int64_t cols, int64_t red, int dt, bool ax, bool bx)
+// `padded`: A's rows end in zeros up to a multiple of 8 (B, whose rows run along the
+// reduction axis then, is checked against its end).
+bool whole_granules(int64_t rows, int64_t cols, int64_t red, int dt, bool ax, bool bx, bool padded)
 {
     const int e = 16 / elem_size(dt);
-    return (ax ? rows : red) % e == 0 && (bx ? cols % 8 : red % e) == 0;
+    return (padded || (ax ? rows : red) % e == 0) && (bx ? cols % 8 : red % e) == 0;
+}
+
+// Whether the backward makes d a tensor of its own (rows padded with zeros): where
+// an activation or a type makes it another one than grad_out, and where grad_out's rows
+// alone would keep both products from streaming (a copy: 150278 x 80 -> 333 bfloat16).
+bool forms_d(const flashblock_linear *p)
+{
+    return p->act != FLASHBLOCK_ACT_NONE || p->out_dtype != p->dtype || (p->N % 8 && p->K % 8 == 0);
 }
 
 TilePlan plan_forward(const flashblock_linear *p)
 {
     if (p->M <= kFewRows) return {0, 1, 0, 0};   // linear_few
     return plan_tiles(p->M, p->N, p->K, p->dtype,
-                      !whole_granules(p->M, p->N, p->K, p->dtype, false, false));
+                      !whole_granules(p->M, p->N, p->K, p->dtype, false, false, false));
 }
 
 TilePlan plan_grad_x(const flashblock_linear *p)
 {
     return plan_tiles(p->M, p->K, p->N, p->dtype,
-                      !whole_granules(p->M, p->K, p->N, p->dtype, false, true));
+                      !whole_granules(p->M, p->K, p->N, p->dtype, false, true, forms_d(p)));
 }
 
 TilePlan plan_grad_weight(const flashblock_linear *p)
 {
     return plan_tiles(p->N, p->K, p->M, p->dtype,
-                      !whole_granules(p->N, p->K, p->M, p->dtype, true, true));
+                      !whole_granules(p->N, p->K, p->M, p->dtype, true, true, forms_d(p)));
 }
 
 template <int DT, bool AX, bool BX, int BM, int BN, int WM, int WN, int S>
@@ -1249,7 +1254,7 @@ template <int DT, bool AX, bool BX>
 bool streamable(const Gemm &g)
 {
     return g.red > 0 && !misaligned(g.a, 16) && !misaligned(g.b, 16) && g.lda % 16 == 0 &&
-           g.ldb % 16 == 0 && whole_granules(g.rows, g.cols, g.red, DT, AX, BX);
+           g.ldb % 16 == 0 && whole_granules(g.rows, g.cols, g.red, DT, AX, BX, g.padded);
 }
 
 template <int DT, bool AX, bool BX, int TILE>
@@ -1275,7 +1280,8 @@ int launch_tiles(Gemm &g, const TilePlan &t, hipStream_t st)
 // C = A B^T through the epilogue; `workspace` of t.workspace bytes
 template <bool AX, bool BX>
 int product(const TilePlan &t, int dt, const void *a, int64_t lda, const void *b, int64_t ldb,
-            int64_t rows, int64_t cols, int64_t red, const Epilogue &e, void *workspace, hipStream_t st)
+            int64_t rows, int64_t cols, int64_t red, bool padded, const Epilogue &e, void *workspace,
+            hipStream_t st)
 {
     if (rows == 0 || cols == 0) return FLASHBEV_OK;
     const int es = elem_size(dt);
@@ -1287,6 +1293,7 @@ int product(const TilePlan &t, int dt, const void *a, int64_t lda, const void *b
     g.rows = (int)rows;
     g.cols = (int)cols;
     g.red = (int)red;
+    g.padded = padded;
     g.split = t.split;
     g.steps = t.steps;
     g.partial = static_cast<float *>(workspace);
@@ -1354,7 +1361,7 @@ BackwardPlan plan_backward(const flashblock_linear *p, bool want_x, bool want_w,
 {
     BackwardPlan b{};
     const int es = elem_size(p->dtype);
-    b.slope = (want_x || want_w) && (p->act != FLASHBLOCK_ACT_NONE || p->out_dtype != p->dtype);
+    b.slope = (want_x || want_w) && forms_d(p);
     b.column_sums = want_b;
     b.ldd = (int64_t)round_up((uint64_t)p->N, 8);
     b.d_bytes = b.slope ? round_up((uint64_t)p->M * b.ldd * es, 256) : 0;
@@ -1440,8 +1447,8 @@ int flashblock_linear_forward(const flashblock_linear *p, const void *x, const v
         return launch_kernel(fn, (uint64_t)(p->N + 15) / 16, 64 * kFewWaves, f, 0,
                              static_cast<hipStream_t>(stream));
     }
-    return product<false, false>(plan, p->dtype, x, p->ldx, weight, p->ldw, p->M, p->N, p->K, e, workspace,
-                                 static_cast<hipStream_t>(stream));
+    return product<false, false>(plan, p->dtype, x, p->ldx, weight, p->ldw, p->M, p->N, p->K, false, e,
+                                 workspace, static_cast<hipStream_t>(stream));
 }
 
 int flashblock_linear_backward_workspace_size(const flashblock_linear *p, int32_t want_x,
@@ -1513,6 +1520,7 @@ int flashblock_linear_backward(const flashblock_linear *p, const void *grad_out,
         s.act = p->act;
         s.grad_f32 = p->out_dtype == FLASHBEV_F32;
         s.scale = p->scale;
+        s.copy = p->act == FLASHBLOCK_ACT_NONE && p->out_dtype == p->dtype;
         s.d = b.slope ? ws : nullptr;
         s.partial = b.column_sums ? reinterpret_cast<float *>(ws + b.d_bytes) : nullptr;
         const void *fn = dt == FLASHBEV_F32   ? (const void *)linear_slope<FLASHBEV_F32>
@@ -1522,7 +1530,7 @@ int flashblock_linear_backward(const flashblock_linear *p, const void *grad_out,
         if (b.slope) {
             d = ws;
             ldd = b.ldd;
-            alpha = 1.0f;
+            if (!s.copy) alpha = 1.0f;
         }
         if (b.column_sums) {
             ColumnJoin c{s.partial, b.ldd, b.ranges, p->N, grad_bias};
@@ -1536,13 +1544,15 @@ int flashblock_linear_backward(const flashblock_linear *p, const void *grad_out,
     if (want_w) {
         Epilogue e{grad_weight, nullptr, nullptr, nullptr, ldgw, 0, 0, alpha, FLASHBLOCK_ACT_NONE,
                    dt == FLASHBEV_F32};
-        if ((rc = product<true, true>(plan_grad_weight(p), dt, d, ldd, x, p->ldx, p->N, p->K, p->M, e, partial, st)))
+        if ((rc = product<true, true>(plan_grad_weight(p), dt, d, ldd, x, p->ldx, p->N, p->K, p->M, b.slope, e, partial,
+                                      st)))
             return rc;
     }
     if (want_x) {
         Epilogue e{grad_x, nullptr, nullptr, nullptr, ldgx, 0, 0, alpha, FLASHBLOCK_ACT_NONE,
                    dt == FLASHBEV_F32};
-        if ((rc = product<false, true>(plan_grad_x(p), dt, d, ldd, weight, p->ldw, p->M, p->K, p->N, e, partial, st)))
+        if ((rc = product<false, true>(plan_grad_x(p), dt, d, ldd, weight, p->ldw, p->M, p->K, p->N, b.slope, e,
+                                       partial, st)))
             return rc;
     }
     return FLASHBEV_OK;

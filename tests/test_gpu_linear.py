@@ -175,7 +175,7 @@ def test_nan_and_infinity_stay_in_their_rows(fb, device):
 @pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("bf16", "f32")])
 @pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
 @pytest.mark.parametrize("M,K,N", [(1, 8, 8), (1, 70, 3), (13, 33, 65), (130, 256, 129), (515, 40, 777),
-                                   (3000, 72, 48)])
+                                   (3000, 72, 48), (600, 264, 1), (2000, 520, 333), (700, 16, 2049)])
 def test_backward(fb, device, M, K, N, act, dtype, out):
     dt, odt = ref.DTYPES[dtype], ref.DTYPES[out]
     x, w, _, g = make(M + K, M, K, N, dt, odt)
