@@ -25,6 +25,7 @@ __all__ = [
     "sample_vt_autograd", "sca_autograd",
     "linear_forward", "linear_backward", "linear_autograd",
     "norm_forward", "norm_backward", "norm_autograd",
+    "prepare_linear_forward", "prepare_norm_forward",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -1172,4 +1173,5 @@ def sca_autograd(value, lidar2img, anchors, grid: BevGrid, img_hw: Tuple[int, in
 # the operators around FlashSCA in an encoder block (include/block/flashblock.h)
 # ---------------------------------------------------------------------------
 from .block import (linear_autograd, linear_backward, linear_forward,  # noqa: E402
-                    norm_autograd, norm_backward, norm_forward)
+                    norm_autograd, norm_backward, norm_forward, prepare_linear_forward,
+                    prepare_norm_forward)

@@ -11,7 +11,7 @@ import ctypes
 import functools
 import struct
 
-from . import (FlashBevError, _dtype_code, _on_device, _one_device,
+from . import (FlashBevError, _dtype_code, _on_device, _one_device, _Prepared,
                _packed_call, _stream_handle, _workspace)
 
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
@@ -160,6 +160,30 @@ def linear_forward(x, weight, bias=None, activation="none", residual=None, scale
 
 def _linear_forward(x, weight, bias, activation, residual, scale, out, out_dtype, pre, stream):
     """linear_forward's (out, sizes for _linear_gradients)."""
+    call, args, _, out, sizes = _linear_call(x, weight, bias, activation, residual, scale, out,
+                                             out_dtype, pre, stream)
+    with _on_device(sizes[-1]):
+        rc = call(*args)
+    if rc != 0:
+        raise FlashBevError(rc, "flashblock_linear_forward")
+    return out, sizes
+
+
+def prepare_linear_forward(x, weight, bias=None, activation="none", residual=None, scale: float = 1.0,
+                           out=None, pre=None, stream=None) -> _Prepared:
+    """``linear_forward`` with every argument fixed (``out`` given): a callable that
+    enqueues the same call again (same tensors, same stream).  A workspace, where the
+    sizes need one, is allocated once, here."""
+    if out is None:
+        raise ValueError("a prepared call needs out")
+    call, args, ws, _, sizes = _linear_call(x, weight, bias, activation, residual, scale, out, None, pre,
+                                            stream)
+    return _Prepared(call, args, (x, weight, bias, residual, out, pre, ws), "flashblock_linear_forward",
+                     sizes[-1])
+
+
+def _linear_call(x, weight, bias, activation, residual, scale, out, out_dtype, pre, stream):
+    """(C call, its arguments, workspace, out, sizes for _linear_gradients)."""
     import torch
 
     M, ldx = _rows(x, "x")
@@ -188,13 +212,9 @@ def _linear_forward(x, weight, bias, activation, residual, scale, out, out_dtype
     s = _stream_handle(stream, dev)
     need = _linear_need(M, K, N, code)
     ws = _workspace(need, dev, s) if need else None
-    call = _packed_call("flashblock_linear_forward", "PPPPPPPPQP")
-    with _on_device(dev):
-        rc = call(args, x.data_ptr(), weight.data_ptr(), b, _addr(residual), out.data_ptr(),
-                  _addr(pre), _addr(ws), need, s)
-    if rc != 0:
-        raise FlashBevError(rc, "flashblock_linear_forward")
-    return out, (M, ldx, ldw, K, N, code, out_code, act, scale, dev)
+    return (_packed_call("flashblock_linear_forward", "PPPPPPPPQP"),
+            (args, x.data_ptr(), weight.data_ptr(), b, _addr(residual), out.data_ptr(), _addr(pre),
+             _addr(ws), need, s), ws, out, (M, ldx, ldw, K, N, code, out_code, act, scale, dev))
 
 
 def _size(name: str, kinds: str, *args) -> int:
@@ -379,6 +399,33 @@ def norm_forward(x, weight=None, bias=None, residual=None, gate=None, scale: flo
 def _norm_forward(x, weight, bias, residual, gate, scale, norm, post_norm, post_weight, post_bias, eps,
                   out, out_s, stream):
     """norm_forward's (y, s, sizes for _norm_gradients)."""
+    call, args, y, s, sizes = _norm_call(x, weight, bias, residual, gate, scale, norm, post_norm,
+                                         post_weight, post_bias, eps, out, out_s, stream)
+    with _on_device(sizes[-1]):
+        rc = call(*args)
+    if rc != 0:
+        raise FlashBevError(rc, "flashblock_norm_forward")
+    return y, s, sizes
+
+
+def prepare_norm_forward(x, weight=None, bias=None, residual=None, gate=None, scale: float = 1.0,
+                         norm="layer", post_norm=None, post_weight=None, post_bias=None,
+                         eps: float = 1e-5, out=None, out_s=None, stream=None) -> _Prepared:
+    """``norm_forward`` with every argument fixed (``out`` given with a norm, ``out_s``
+    where anything is added or there is no norm): a callable that enqueues the same call
+    again (same tensors, same stream)."""
+    if (out is None and _norm_code(norm, "norm")) or (out_s is None and not _adds_nothing(
+            x, residual, gate, scale, post_norm, out_s)):
+        raise ValueError("a prepared call needs out and out_s")
+    call, args, _, _, sizes = _norm_call(x, weight, bias, residual, gate, scale, norm, post_norm,
+                                         post_weight, post_bias, eps, out, out_s, stream)
+    keep = (x, weight, bias, residual, gate, post_weight, post_bias, out, out_s)
+    return _Prepared(call, args, keep, "flashblock_norm_forward", sizes[-1])
+
+
+def _norm_call(x, weight, bias, residual, gate, scale, norm, post_norm, post_weight, post_bias, eps, out,
+               out_s, stream):
+    """(C call, its arguments, y, s, sizes for _norm_gradients)."""
     import torch
 
     M, ldx = _rows(x, "x")
@@ -412,12 +459,9 @@ def _norm_forward(x, weight, bias, residual, gate, scale, norm, post_norm, post_
     args = _PACK_NORM.pack(M, ldx, ldr, lds, ldy, groups, C, *types)
     dev = _one_device(x, weight, bias, residual, gate, post_weight, post_bias, out, out_s)
     s = _stream_handle(stream, dev)
-    call = _packed_call("flashblock_norm_forward", "PPPPPPP")
-    with _on_device(dev):
-        rc = call(args, vectors, x.data_ptr(), _addr(residual), _addr(out_s), _addr(out), s)
-    if rc != 0:
-        raise FlashBevError(rc, "flashblock_norm_forward")
-    return out, x if same else out_s, (M, ldx, ldx if same else lds, groups, C, types, dev)
+    return (_packed_call("flashblock_norm_forward", "PPPPPPP"),
+            (args, vectors, x.data_ptr(), _addr(residual), _addr(out_s), _addr(out), s), out,
+            x if same else out_s, (M, ldx, ldx if same else lds, groups, C, types, dev))
 
 
 def norm_backward(grad_y, grad_s, x, s, weight=None, gate=None, scale: float = 1.0, norm="layer",
@@ -605,7 +649,8 @@ def linear_autograd(x, weight, bias=None, activation="none", residual=None, scal
                     out_dtype=None):
     """``linear_forward`` as a differentiable function of x, weight, bias and
     residual; the gradients are ``linear_backward``'s, computed only for the inputs
-    that need them."""
+    that need them.  (In a HIP graph capture forward and gradients together, by
+    torch.autograd.grad, with no eager graph of the same leaves alive.)"""
     return _autograd_functions()["linear"].apply(x, weight, bias, residual, activation, scale,
                                                  out_dtype)
 

@@ -1,6 +1,6 @@
-// Helpers of the encoder block's operators (flashlinear.hip, flashnorm.hip): 16-byte vectors at any element
-// alignment, conversion of stored elements to float32 and back, and on the host
-// the byte ranges of strided tensors.
+// Helpers of the encoder block's operators (flashlinear.hip, flashnorm.hip): 8- and
+// 16-byte vectors at any element alignment, conversion of stored elements to
+// float32 and back, and on the host the byte ranges of strided tensors.
 #pragma once
 
 #include "block/flashblock.h"

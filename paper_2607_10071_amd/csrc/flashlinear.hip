@@ -26,9 +26,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // activations
 // ---------------------------------------------------------------------------
 // On the hardware's exp2 and reciprocal (one unit in the last place each): an
-// output of 40000 x 1024 gelus is 41 M of them, and the library's erff, expf and
-// IEEE division took longer than the product before them (119 us of the whole
-// call, and 80 with these).
+// output of 40000 x 1024 gelus is 41 M of them, and with the library's erff, expf and
+// IEEE division its product took 109 us where it takes 75 with these.
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSqrt2OverPi = 0.79788456080286536f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
@@ -92,8 +91,8 @@ __device__ __forceinline__ float act_slope(int act, float v)
     case FLASHBLOCK_ACT_GELU_TANH: {
         const float p = sigmoid(2.0f * kSqrt2OverPi * v * __builtin_fmaf(0.044715f, v * v, 1.0f));
         const float w = within(v, 20.0f);
-        return __builtin_fmaf(w * p * (1.0f - p), 2.0f * kSqrt2OverPi * __builtin_fmaf(0.134145f, w * w, 1.0f),
-                              p);
+        const float dz = 2.0f * kSqrt2OverPi * __builtin_fmaf(0.134145f, w * w, 1.0f);
+        return __builtin_fmaf(w * p * (1.0f - p), dz, p);
     }
     case FLASHBLOCK_ACT_SILU: {
         const float p = sigmoid(v);
@@ -702,28 +701,31 @@ __device__ __forceinline__ void write_any(const Gemm &p, int part, int m, int n,
     // whose registers are short
     asm volatile("" : "+v"(lane));
     if (p.split > 1) return write_part(p, part, m, n, lane, acc);
-    constexpr int F32 = FLASHBEV_F32;
+    // One activation's code per call.  (The branches in this order: with the types
+    // inside the activations' cases the 256 x 256 forward spilled beside the ring's
+    // loads, 536 -> 765 us for the large product.)
+#define FLASHBLOCK_WRITE(OUT, ACT) \
+    return write_tile<DT, OUT, ACT, FULL, ENDS>(p, m, n, lane, acc)
     if constexpr (!FULL) {
         write_tile<DT, DT, FLASHBLOCK_ACT_NONE, FULL, ENDS>(p, m, n, lane, acc);
-    } else if (DT == F32 || !p.e.out_f32) {
+    } else if (DT == FLASHBEV_F32 || !p.e.out_f32) {
         switch (p.e.act) {
-        case FLASHBLOCK_ACT_RELU: return write_tile<DT, DT, FLASHBLOCK_ACT_RELU, FULL, ENDS>(p, m, n, lane, acc);
-        case FLASHBLOCK_ACT_GELU: return write_tile<DT, DT, FLASHBLOCK_ACT_GELU, FULL, ENDS>(p, m, n, lane, acc);
-        case FLASHBLOCK_ACT_GELU_TANH:
-            return write_tile<DT, DT, FLASHBLOCK_ACT_GELU_TANH, FULL, ENDS>(p, m, n, lane, acc);
-        case FLASHBLOCK_ACT_SILU: return write_tile<DT, DT, FLASHBLOCK_ACT_SILU, FULL, ENDS>(p, m, n, lane, acc);
-        default: return write_tile<DT, DT, FLASHBLOCK_ACT_NONE, FULL, ENDS>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_RELU: FLASHBLOCK_WRITE(DT, FLASHBLOCK_ACT_RELU);
+        case FLASHBLOCK_ACT_GELU: FLASHBLOCK_WRITE(DT, FLASHBLOCK_ACT_GELU);
+        case FLASHBLOCK_ACT_GELU_TANH: FLASHBLOCK_WRITE(DT, FLASHBLOCK_ACT_GELU_TANH);
+        case FLASHBLOCK_ACT_SILU: FLASHBLOCK_WRITE(DT, FLASHBLOCK_ACT_SILU);
+        default: FLASHBLOCK_WRITE(DT, FLASHBLOCK_ACT_NONE);
         }
     } else {
         switch (p.e.act) {
-        case FLASHBLOCK_ACT_RELU: return write_tile<DT, F32, FLASHBLOCK_ACT_RELU, FULL, ENDS>(p, m, n, lane, acc);
-        case FLASHBLOCK_ACT_GELU: return write_tile<DT, F32, FLASHBLOCK_ACT_GELU, FULL, ENDS>(p, m, n, lane, acc);
-        case FLASHBLOCK_ACT_GELU_TANH:
-            return write_tile<DT, F32, FLASHBLOCK_ACT_GELU_TANH, FULL, ENDS>(p, m, n, lane, acc);
-        case FLASHBLOCK_ACT_SILU: return write_tile<DT, F32, FLASHBLOCK_ACT_SILU, FULL, ENDS>(p, m, n, lane, acc);
-        default: return write_tile<DT, F32, FLASHBLOCK_ACT_NONE, FULL, ENDS>(p, m, n, lane, acc);
+        case FLASHBLOCK_ACT_RELU: FLASHBLOCK_WRITE(FLASHBEV_F32, FLASHBLOCK_ACT_RELU);
+        case FLASHBLOCK_ACT_GELU: FLASHBLOCK_WRITE(FLASHBEV_F32, FLASHBLOCK_ACT_GELU);
+        case FLASHBLOCK_ACT_GELU_TANH: FLASHBLOCK_WRITE(FLASHBEV_F32, FLASHBLOCK_ACT_GELU_TANH);
+        case FLASHBLOCK_ACT_SILU: FLASHBLOCK_WRITE(FLASHBEV_F32, FLASHBLOCK_ACT_SILU);
+        default: FLASHBLOCK_WRITE(FLASHBEV_F32, FLASHBLOCK_ACT_NONE);
         }
     }
+#undef FLASHBLOCK_WRITE
 }
 
 template <int DT, bool AX, bool BX, int BM, int BN, int WM, int WN, int S, bool ENDS>
@@ -1311,6 +1313,12 @@ int product(const TilePlan &t, int dt, const void *a, int64_t lda, const void *b
     return launch_kernel(fn, (vecs + 63) / 64, 256, j, 0, st);
 }
 
+template <int DT>
+const void *few_kernel(bool two)
+{
+    return two ? (const void *)linear_few<DT, 2> : (const void *)linear_few<DT, 1>;
+}
+
 int check_sizes(const flashblock_linear *p)
 {
     if (!p) return FLASHBEV_ERR_NULLPTR;
@@ -1436,14 +1444,10 @@ int flashblock_linear_forward(const flashblock_linear *p, const void *x, const v
     if (p->M <= kFewRows) {
         Few f{static_cast<const char *>(x), static_cast<const char *>(weight), p->ldx * es,
               p->ldw * es, (int)p->M, p->N, p->K, e};
-        const void *fn = nullptr;
         const bool two = p->M > 16;
-        if (p->dtype == FLASHBEV_F32)
-            fn = two ? (const void *)linear_few<FLASHBEV_F32, 2> : (const void *)linear_few<FLASHBEV_F32, 1>;
-        else if (p->dtype == FLASHBEV_F16)
-            fn = two ? (const void *)linear_few<FLASHBEV_F16, 2> : (const void *)linear_few<FLASHBEV_F16, 1>;
-        else
-            fn = two ? (const void *)linear_few<FLASHBEV_BF16, 2> : (const void *)linear_few<FLASHBEV_BF16, 1>;
+        const void *fn = p->dtype == FLASHBEV_F32   ? few_kernel<FLASHBEV_F32>(two)
+                         : p->dtype == FLASHBEV_F16 ? few_kernel<FLASHBEV_F16>(two)
+                                                    : few_kernel<FLASHBEV_BF16>(two);
         return launch_kernel(fn, (uint64_t)(p->N + 15) / 16, 64 * kFewWaves, f, 0,
                              static_cast<hipStream_t>(stream));
     }
@@ -1544,15 +1548,15 @@ int flashblock_linear_backward(const flashblock_linear *p, const void *grad_out,
     if (want_w) {
         Epilogue e{grad_weight, nullptr, nullptr, nullptr, ldgw, 0, 0, alpha, FLASHBLOCK_ACT_NONE,
                    dt == FLASHBEV_F32};
-        if ((rc = product<true, true>(plan_grad_weight(p), dt, d, ldd, x, p->ldx, p->N, p->K, p->M, b.slope, e, partial,
-                                      st)))
+        if ((rc = product<true, true>(plan_grad_weight(p), dt, d, ldd, x, p->ldx, p->N, p->K, p->M,
+                                      b.slope, e, partial, st)))
             return rc;
     }
     if (want_x) {
         Epilogue e{grad_x, nullptr, nullptr, nullptr, ldgx, 0, 0, alpha, FLASHBLOCK_ACT_NONE,
                    dt == FLASHBEV_F32};
-        if ((rc = product<false, true>(plan_grad_x(p), dt, d, ldd, weight, p->ldw, p->M, p->K, p->N, b.slope, e,
-                                       partial, st)))
+        if ((rc = product<false, true>(plan_grad_x(p), dt, d, ldd, weight, p->ldw, p->M, p->K, p->N,
+                                       b.slope, e, partial, st)))
             return rc;
     }
     return FLASHBEV_OK;

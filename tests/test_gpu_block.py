@@ -251,6 +251,39 @@ def test_a_training_pass_in_a_graph(fb, device):
         assert all(torch.equal(a, b.detach()) for a, b in zip(got, want)), k
 
 
+def test_prepared_calls(fb, device):
+    """The same calls again on the same tensors, with new values in them, on their
+    stream and in a graph."""
+    ins, _ = passes(fb)
+    i = ins
+    outs = {"long": torch.empty(96, 64, dtype=torch.bfloat16, device=device),
+            "one": torch.empty(1, 512, device=device), "y": torch.empty_like(i["x"]),
+            "s": torch.empty_like(i["x"]), "n": torch.empty_like(i["x"])}
+    calls = [fb.prepare_linear_forward(i["long"], i["wl"], out=outs["long"]),
+             fb.prepare_linear_forward(i["one"], i["w"], i["b"], "silu", out=outs["one"]),
+             fb.prepare_norm_forward(i["x"], i["n"], None, i["r"], i["gate"], 0.5, "rms", out=outs["y"],
+                                     out_s=outs["s"]),
+             fb.prepare_norm_forward(i["x"], i["n"], out=outs["n"])]
+
+    def want():
+        y, s = fb.norm_forward(i["x"], i["n"], None, i["r"], i["gate"], 0.5, "rms")
+        return {"long": fb.linear_forward(i["long"], i["wl"]),
+                "one": fb.linear_forward(i["one"], i["w"], i["b"], "silu", out_dtype=torch.float32),
+                "y": y, "s": s, "n": fb.norm_forward(i["x"], i["n"])[0]}
+
+    for k in range(3):
+        refill(ins, k)
+        for call in calls:
+            call()
+        torch.cuda.synchronize()
+        w = want()
+        assert all(torch.equal(outs[n], w[n]) for n in w)
+    with pytest.raises(ValueError):
+        fb.prepare_linear_forward(i["x"], i["w"])
+    with pytest.raises(ValueError):
+        fb.prepare_norm_forward(i["x"], i["n"], residual=i["r"], out=outs["y"])
+
+
 def test_threads(fb, device):
     ins, run = passes(fb)
     want = [t.clone() for t in run()]
