@@ -27,8 +27,8 @@
  *     float32); statistics, gates and sums are float32; each output is rounded
  *     once, to nearest even;
  *   - widths (K, N) are at most FLASHBLOCK_WIDTH_MAX, a norm's (C)
- *     FLASHBLOCK_NORM_MAX, and row strides at most
- *     FLASHBLOCK_LD_MAX elements; M < 2^31 rows;
+ *     FLASHBLOCK_NORM_MAX, row strides at most FLASHBLOCK_LD_MAX elements, and
+ *     rows at most FLASHBLOCK_ROWS_MAX;
  *   - an output must not overlap an input or another output, except where
  *     stated (byte ranges from a tensor's first to its last element are
  *     compared);
@@ -36,13 +36,15 @@
  *     NULL.
  *
  * Results are bitwise reproducible: no atomics, sums in a fixed order that
- * depends on the sizes alone.
+ * depends on sizes, types, strides and alignment alone.
  *
  * Thread safety: no state; calls are asynchronous on the given stream and may
  * come from several threads.  No allocation, no printing, no abort.  Kernels
  * run on the calling thread's current HIP device, which must hold every buffer
- * of the call and the stream.  Status codes are flashbev.h's; argument errors
- * are reported before any HIP call.
+ * of the call and the stream.  A product of large tiles needs more than 64 KiB of
+ * LDS per workgroup and first raises that kernel's dynamic-LDS limit with
+ * hipFuncSetAttribute, a per-process setting that is idempotent.  Status codes
+ * are flashbev.h's; argument errors are reported before any HIP call.
  */
 #ifndef FLASHBLOCK_H
 #define FLASHBLOCK_H
