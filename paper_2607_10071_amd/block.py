@@ -553,6 +553,16 @@ def _as_rows(t, width: int):
     return t, width
 
 
+def _restored(t, name: str, dtype, shape, device):
+    """A saved tensor as it came back.  Hooks on saved tensors hand over anything:
+    the kernels read it as what was saved, so another type, size or place is refused.
+    Its strides are its own."""
+    if t.dtype != dtype or t.shape != shape or t.device != device:
+        raise ValueError(f"{name} was saved as {dtype} {tuple(shape)} on {device} and came back as "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    return t
+
+
 def _autograd_functions():
     """The torch.autograd.Function classes, made on first use."""
     if _AUTOGRAD:
@@ -569,29 +579,37 @@ def _autograd_functions():
         residual = grad_out if needs[3] else None
         if not (needs[0] or needs[1] or needs[2]):
             return None, None, None, residual, None, None, None
-        M, K, N, *rest = ctx.sizes
+        (M, K, N, *rest), shape, dtype = ctx.sizes
+        dev = rest[-1]
         g, ldo = _as_rows(grad_out, N)
-        # (hooks on saved tensors may have moved them: their strides are read here)
-        x, ldx = _as_rows(x, K)
-        weight, ldw = _as_rows(weight, K)
+        x, ldx = _as_rows(_restored(x, "x", dtype, shape, dev), K)
+        weight, ldw = _as_rows(_restored(weight, "weight", dtype, (N, K), dev), K)
+        ldp = N
+        if pre is not None:
+            pre, ldp = _as_rows(_restored(pre, "pre", dtype, (*shape[:-1], N), dev), N)
         gx = torch.empty_like(x, memory_format=torch.contiguous_format) if needs[0] else None
         gw = torch.empty_like(weight, memory_format=torch.contiguous_format) if needs[1] else None
         gb = torch.empty(N, dtype=x.dtype, device=x.device) if needs[2] else None
-        _linear_gradients((M, ldx, ldw, K, N, *rest), g, ldo, x, weight, pre, N, gx, K, gw, K, gb, None)
+        _linear_gradients((M, ldx, ldw, K, N, *rest), g, ldo, x, weight, pre, ldp, gx, K, gw, K, gb, None)
         return gx, gw, gb, residual, None, None, None
 
     def norm_grads(ctx, grad_y, grad_s):
         x, s, weight, gate, post_weight, post_bias = ctx.saved_tensors
         if grad_y is None and grad_s is None:
             return (None,) * 11
-        (M, groups, C, types, dev), want, pdt = ctx.sizes
+        (M, groups, C, types, dev), want, shape, gate_shape, (dt, sdt, pdt) = ctx.sizes
         ldgy = ldgs = C
-        x, ldx = _as_rows(x, C)
-        s, lds = (x, ldx) if s is None else _as_rows(s, C)
+        x, ldx = _as_rows(_restored(x, "x", dt, shape, dev), C)
+        s, lds = (x, ldx) if s is None else _as_rows(_restored(s, "s", sdt, shape, dev), C)
         if grad_y is not None:
             grad_y, ldgy = _as_rows(grad_y, C)
         if grad_s is not None:
             grad_s, ldgs = _as_rows(grad_s, C)
+        # (contiguous for the call, and alive until it is enqueued)
+        gate, weight, post_weight, post_bias = [
+            None if t is None else _restored(t, name, pdt, like, dev).contiguous()
+            for t, name, like in ((gate, "gate", gate_shape), (weight, "weight", (C,)),
+                                  (post_weight, "post_weight", (C,)), (post_bias, "post_bias", (C,)))]
         vectors = _PACK_VECTORS.pack(_addr(gate), _addr(weight), 0, _addr(post_weight), _addr(post_bias))
         r = _norm_gradients((M, ldx, lds, groups, C, types, dev), grad_y, ldgy, grad_s, ldgs, x, s, gate,
                             vectors, pdt, want, None)
@@ -609,7 +627,7 @@ def _autograd_functions():
                 pre = torch.empty((*x.shape[:-1], weight.shape[0]), dtype=x.dtype, device=x.device)
             out, sizes = _linear_forward(x, weight, bias, activation, residual, scale, None, out_dtype,
                                          pre, None)
-            ctx.sizes = sizes[:1] + sizes[3:]   # without the strides
+            ctx.sizes = sizes[:1] + sizes[3:], x.shape, x.dtype   # without the strides
             ctx.save_for_backward(x, weight, pre)
             return out
 
@@ -624,6 +642,7 @@ def _autograd_functions():
             ctx.set_materialize_grads(False)
             y, s, sizes = _norm_forward(x, weight, bias, residual, gate, scale, norm, post_norm,
                                         post_weight, post_bias, eps, None, None, None)
+            sdt = s.dtype
             if s is x:
                 s = None
             ctx.save_for_backward(x, s, weight, gate, post_weight, post_bias)
@@ -633,7 +652,8 @@ def _autograd_functions():
                     pdt = t.dtype
                     break
             want = [k for k, n in zip(_NORM_INPUTS, ctx.needs_input_grad) if n]
-            ctx.sizes = sizes[:1] + sizes[3:], want, pdt   # without the strides
+            ctx.sizes = (sizes[:1] + sizes[3:], want, x.shape, None if gate is None else gate.shape,
+                         (x.dtype, sdt, pdt))   # without the strides
             return y, s
 
         @staticmethod
