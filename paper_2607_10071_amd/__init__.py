@@ -1145,8 +1145,8 @@ def _autograd_functions():
                               None, "auto", value.dtype)
             return r["value"], None, r["offsets"], r["logits"], None, None, None, None, None, None
 
-    _AUTOGRAD["sample_vt"] = _SampleVT
-    _AUTOGRAD["sca"] = _SCA
+    # both at once: another thread takes what it finds here as the whole
+    _AUTOGRAD.update({"sample_vt": _SampleVT, "sca": _SCA})
     return _AUTOGRAD
 
 

@@ -660,8 +660,8 @@ def _autograd_functions():
         def backward(ctx, grad_y, grad_s):
             return (norm_once if torch.is_grad_enabled() else norm_grads)(ctx, grad_y, grad_s)
 
-    _AUTOGRAD["linear"] = _Linear
-    _AUTOGRAD["norm"] = _Norm
+    # both at once: another thread takes what it finds here as the whole
+    _AUTOGRAD.update({"linear": _Linear, "norm": _Norm})
     return _AUTOGRAD
 
 
