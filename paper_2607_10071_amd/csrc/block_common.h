@@ -39,6 +39,12 @@ __device__ __forceinline__ void store16(void *p, u32x4 v)
 
 constexpr int elem_size(int dt) { return dt == FLASHBEV_F32 ? 4 : 2; }
 
+// The workgroups of a row of the grid (2^31 threads at most), and a workgroup's number
+// over all rows.
+constexpr uint32_t kGridRow = 1u << 21;
+
+__device__ __forceinline__ uint32_t block_index() { return blockIdx.y * kGridRow + blockIdx.x; }
+
 // One stored element as float32 (exact) and a float32 rounded to it.
 template <int DT>
 __device__ __forceinline__ float load_elem(const void *p, int64_t i)
@@ -209,14 +215,27 @@ inline bool known_dtype(int dt) { return dt >= FLASHBEV_F32 && dt <= FLASHBEV_BF
 
 inline bool misaligned(const void *p, int a) { return ((uintptr_t)p & (uintptr_t)(a - 1)) != 0; }
 
+// An axis of a grid holds fewer than 2^32 threads: past them HIP launches what is left
+// modulo 2^32, without an error.
 template <class P>
-int launch_kernel(const void *fn, uint64_t blocks, int threads, P &p, size_t lds, hipStream_t st)
+int launch_kernel(const void *fn, uint64_t blocks, int threads, P &p, size_t lds, hipStream_t st,
+                  unsigned grid_rows = 1)
 {
     if (blocks == 0) return FLASHBEV_OK;
-    if (blocks > 0x7fffffffull) return FLASHBEV_ERR_UNSUPPORTED;
+    if (blocks > 0x7fffffffull || blocks * threads > 0xffffffffull) return FLASHBEV_ERR_UNSUPPORTED;
     void *args[] = {&p};
-    return hipLaunchKernel(fn, dim3((unsigned)blocks), dim3(threads), args, lds, st) == hipSuccess
+    return hipLaunchKernel(fn, dim3((unsigned)blocks, grid_rows), dim3(threads), args, lds, st) == hipSuccess
                ? FLASHBEV_OK : FLASHBEV_ERR_HIP;
+}
+
+// For kernels that go by block_index() and leave at once past their last workgroup: more
+// workgroups than one row of the grid takes go over several.
+template <class P>
+int launch_rows(const void *fn, uint64_t blocks, int threads, P &p, hipStream_t st)
+{
+    if (blocks > 0x7fffffffull) return FLASHBEV_ERR_UNSUPPORTED;
+    if (blocks <= kGridRow) return launch_kernel(fn, blocks, threads, p, 0, st);
+    return launch_kernel(fn, kGridRow, threads, p, 0, st, (unsigned)((blocks + kGridRow - 1) / kGridRow));
 }
 
 }  // namespace

@@ -364,7 +364,8 @@ __global__ void __launch_bounds__(WM *WN * 64) linear_tiles(Gemm p)
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int wm = wave / WN, wn = wave % WN;
-    const int tile = blockIdx.x / p.split, part = blockIdx.x % p.split;
+    const int tile = block_index() / p.split, part = block_index() % p.split;
+    if (tile >= p.tiles_m * p.tiles_n) return;
     const int m0 = tile / p.tiles_n * BM, n0 = tile % p.tiles_n * BN;
 
     f32x16 acc[FM][FN];
@@ -1264,8 +1265,8 @@ int launch_checked(Gemm &g, hipStream_t st)
 {
     g.tiles_m = (g.rows + TILE - 1) / TILE;
     g.tiles_n = (g.cols + TILE - 1) / TILE;
-    return launch_kernel((const void *)linear_tiles<DT, AX, BX, TILE, TILE, 2, 2>,
-                         (uint64_t)g.tiles_m * g.tiles_n * g.split, 256, g, 0, st);
+    return launch_rows((const void *)linear_tiles<DT, AX, BX, TILE, TILE, 2, 2>,
+                       (uint64_t)g.tiles_m * g.tiles_n * g.split, 256, g, st);
 }
 
 template <int DT, bool AX, bool BX>

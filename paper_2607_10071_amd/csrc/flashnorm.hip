@@ -231,10 +231,12 @@ __global__ void __launch_bounds__(T > 256 ? T : 256, DT != FLASHBEV_F32 && NV ==
     constexpr int E = R::E;
     __shared__ float slots[T > 64 ? 4 * kSlot : 1];
     const int t = threadIdx.x % T;
-    const int64_t row = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / T;
+    const int64_t row0 = (int64_t)block_index() * R::ROWS;
+    if (row0 >= p.M) return;
+    const int64_t row = R::ROWS > 1 ? row0 + threadIdx.x / T : row0;
     // lanes past the last row take it again (the sums' barriers need every
     // wavefront) and store nothing
-    const bool in = row < p.M;
+    const bool in = R::ROWS == 1 || row < p.M;
     const int64_t m = in ? row : p.M - 1;
     const float inv = 1.0f / (float)p.C;
     float u[E], a[E], b[E];
@@ -327,8 +329,9 @@ __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward 
     __shared__ float slots[T > 64 ? 3 * kSlot : 1];
     __shared__ float lanes[R::ROWS > 1 ? R::ROWS * T * V : 1];   // one vector's sums at a time
     const int t = threadIdx.x % T, lane_row = threadIdx.x / T;
-    const int64_t group = blockIdx.x / p.ranges_per_group, range = blockIdx.x % p.ranges_per_group;
+    const int64_t group = block_index() / p.ranges_per_group, range = block_index() % p.ranges_per_group;
     const int64_t m0 = group * p.per_group + range * p.range;
+    if (m0 >= p.M) return;
     int64_t m1 = m0 + p.range;
     if (m1 > (group + 1) * p.per_group) m1 = (group + 1) * p.per_group;
     const float inv = 1.0f / (float)p.C;
@@ -481,7 +484,7 @@ __global__ void __launch_bounds__(T > 256 ? T : 256) norm_backward(NormBackward 
     for (int k = 0; k < kVectors; ++k) {
         if (!p.partial[k]) continue;
         const float f = k == kGate ? p.scale : 1.0f;
-        float *dst = p.partial[k] + (int64_t)blockIdx.x * p.pld;
+        float *dst = p.partial[k] + (int64_t)block_index() * p.pld;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             float w[V];
@@ -519,16 +522,18 @@ struct NormJoin {
     int which[kVectors];        // vectors in use, in order
     int col_blocks, C;
     int out_f32;
+    uint32_t blocks;
 };
 
 template <int DT>
 __global__ void __launch_bounds__(256) norm_join(NormJoin p)
 {
-    int64_t b = blockIdx.x / p.col_blocks;
+    if (block_index() >= p.blocks) return;
+    int64_t b = block_index() / p.col_blocks;
     int k = 0;
     while (b >= p.rows[p.which[k]]) b -= p.rows[p.which[k++]];
     k = p.which[k];
-    const int n = (int)(blockIdx.x % p.col_blocks) * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
+    const int n = (int)(block_index() % p.col_blocks) * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
     float s = 0.0f;
     if (n < p.C) {
         const float *src = p.partial[k] + b * p.ranges[k] * p.pld + n;
@@ -752,8 +757,8 @@ int flashblock_norm_forward(const flashblock_norm *p, const flashblock_norm_para
     const void *fn = p->post_norm != FLASHBLOCK_NORM_NONE
                          ? kernel_of<false, true>(p->dtype, p->stream_dtype, p->C)
                          : kernel_of<false, false>(p->dtype, p->stream_dtype, p->C);
-    return launch_kernel(fn, (uint64_t)(p->M + h.rows - 1) / h.rows, h.threads, n, 0,
-                         static_cast<hipStream_t>(stream));
+    return launch_rows(fn, (uint64_t)(p->M + h.rows - 1) / h.rows, h.threads, n,
+                       static_cast<hipStream_t>(stream));
 }
 
 int flashblock_norm_backward_workspace_size(const flashblock_norm *p,
@@ -880,7 +885,7 @@ int flashblock_norm_backward(const flashblock_norm *p, const flashblock_norm_par
         const void *fn = p->post_norm != FLASHBLOCK_NORM_NONE
                              ? kernel_of<true, true>(p->dtype, p->stream_dtype, p->C)
                              : kernel_of<true, false>(p->dtype, p->stream_dtype, p->C);
-        if ((rc = launch_kernel(fn, (uint64_t)p->groups * q.per, h.threads, n, 0, st))) return rc;
+        if ((rc = launch_rows(fn, (uint64_t)p->groups * q.per, h.threads, n, st))) return rc;
     } else {
         for (int k = 0; k < kVectors; ++k) j.ranges[k] = 0;   // sums of nothing
     }
@@ -888,7 +893,9 @@ int flashblock_norm_backward(const flashblock_norm *p, const flashblock_norm_par
     const void *fn = p->dtype == FLASHBEV_F32   ? (const void *)norm_join<FLASHBEV_F32>
                      : p->dtype == FLASHBEV_F16 ? (const void *)norm_join<FLASHBEV_F16>
                                                 : (const void *)norm_join<FLASHBEV_BF16>;
-    return launch_kernel(fn, (uint64_t)out_rows * j.col_blocks, 256, j, 0, st);
+    const uint64_t blocks = (uint64_t)out_rows * j.col_blocks;
+    j.blocks = (uint32_t)blocks;   // (more than 32 bits are refused below)
+    return launch_rows(fn, blocks, 256, j, st);
 }
 
 }  // extern "C"
