@@ -420,6 +420,17 @@ def _backward_workspace_bytes(f, g, zb, args) -> int:
     return int(out.value)
 
 
+def _on_stream(device, s: int):
+    """Makes the stream ``s`` torch's current one on ``device``."""
+    import torch
+
+    if s == torch._C._cuda_getCurrentRawStream(device.index):
+        return _HERE_ALREADY
+    # (ExternalStream(0) would be a stream of torch's own)
+    return torch.cuda.stream(torch.cuda.ExternalStream(s, device=device) if s
+                             else torch.cuda.default_stream(device))
+
+
 def _workspace(size: int, device, s: int):
     """``size`` bytes of device memory from the pool of the stream ``s``, so
     that what the allocator gives out before and after a call on ``s`` is in
@@ -427,11 +438,7 @@ def _workspace(size: int, device, s: int):
     there, and would go back to that stream while the call runs on ``s``.)"""
     import torch
 
-    if s == torch._C._cuda_getCurrentRawStream(device.index):
-        return torch.empty(size, dtype=torch.uint8, device=device)
-    # (ExternalStream(0) would be a stream of torch's own)
-    stream = torch.cuda.ExternalStream(s, device=device) if s else torch.cuda.default_stream(device)
-    with torch.cuda.stream(stream):
+    with _on_stream(device, s):
         return torch.empty(size, dtype=torch.uint8, device=device)
 
 

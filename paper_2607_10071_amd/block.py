@@ -11,11 +11,12 @@ import ctypes
 import functools
 import struct
 
-from . import (FlashBevError, _dtype_code, _on_device, _one_device, _Prepared,
+from . import (FlashBevError, _dtype_code, _on_device, _on_stream, _one_device, _Prepared,
                _packed_call, _stream_handle, _workspace)
 
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 NORMS = {"none": 0, "layer": 1, "rms": 2}
+LD_MAX = 1 << 20   # FLASHBLOCK_LD_MAX
 
 # The C structures as packed bytes (see the package's other calls).
 _PACK_LINEAR = struct.Struct("@6q5if")
@@ -80,6 +81,20 @@ def _strided_rows(t, name: str):
     return rows, ld
 
 
+def _near(t, ld: int, device, s: int):
+    """(t, its row stride), or a copy, made on the stream ``s`` of the call that reads
+    it, where the library does not take rows so far apart."""
+    if ld <= LD_MAX:
+        return t, ld
+    with _on_stream(device, s):
+        return t.contiguous(), t.shape[-1]
+
+
+def _no_copies(*lds) -> None:
+    if max(lds) > LD_MAX:
+        raise ValueError(f"a prepared call takes rows at most {LD_MAX} elements apart")
+
+
 def _product(shape) -> int:
     n = 1
     for v in shape:
@@ -139,7 +154,9 @@ def linear_forward(x, weight, bias=None, activation="none", residual=None, scale
     """residual + scale * act(x weight^T + bias) on the GPU.
 
     x           CUDA tensor [..., K] (float32, float16 or bfloat16): rows of
-                contiguous elements, at any one row stride.
+                contiguous elements, at any one row stride.  (Of inputs whose rows
+                lie more than LD_MAX = 2^20 elements apart a copy is read; outputs
+                must lie closer.)
     weight      [N, K] in x's dtype, rows likewise.
     bias        optional [N] in x's dtype.
     activation  "none", "relu", "gelu" (erf), "gelu_tanh" or "silu".
@@ -160,8 +177,8 @@ def linear_forward(x, weight, bias=None, activation="none", residual=None, scale
 
 def _linear_forward(x, weight, bias, activation, residual, scale, out, out_dtype, pre, stream):
     """linear_forward's (out, sizes for _linear_gradients)."""
-    call, args, _, out, sizes = _linear_call(x, weight, bias, activation, residual, scale, out,
-                                             out_dtype, pre, stream)
+    call, args, keep, out, sizes = _linear_call(x, weight, bias, activation, residual, scale, out,
+                                                out_dtype, pre, stream, False)
     with _on_device(sizes[-1]):
         rc = call(*args)
     if rc != 0:
@@ -176,14 +193,14 @@ def prepare_linear_forward(x, weight, bias=None, activation="none", residual=Non
     sizes need one, is allocated once, here."""
     if out is None:
         raise ValueError("a prepared call needs out")
-    call, args, ws, _, sizes = _linear_call(x, weight, bias, activation, residual, scale, out, None, pre,
-                                            stream)
-    return _Prepared(call, args, (x, weight, bias, residual, out, pre, ws), "flashblock_linear_forward",
-                     sizes[-1])
+    call, args, keep, _, sizes = _linear_call(x, weight, bias, activation, residual, scale, out, None, pre,
+                                              stream, True)
+    return _Prepared(call, args, keep, "flashblock_linear_forward", sizes[-1])
 
 
-def _linear_call(x, weight, bias, activation, residual, scale, out, out_dtype, pre, stream):
-    """(C call, its arguments, workspace, out, sizes for _linear_gradients)."""
+def _linear_call(x, weight, bias, activation, residual, scale, out, out_dtype, pre, stream, again):
+    """(C call, its arguments, the tensors they point into, out, sizes for
+    _linear_gradients).  ``again``: the call may be made more than once."""
     import torch
 
     M, ldx = _rows(x, "x")
@@ -207,14 +224,22 @@ def _linear_call(x, weight, bias, activation, residual, scale, out, out_dtype, p
         ldp = _rows(pre, "pre")[1]
     b = _vector(bias, "bias", x.dtype, N)
     act, out_code = _act_code(activation), code if odt == x.dtype else 0
-    args = _PACK_LINEAR.pack(M, ldx, ldw, ldr, ldo, ldp, K, N, code, out_code, act, scale)
     dev = _one_device(x, weight, bias, residual, out, pre)
     s = _stream_handle(stream, dev)
+    if ldx > LD_MAX or ldw > LD_MAX or (ldr > LD_MAX and residual is not out):
+        if again:
+            _no_copies(ldx, ldw, ldr)
+        x, ldx = _near(x, ldx, dev, s)
+        weight, ldw = _near(weight, ldw, dev, s)
+        if residual is not None:
+            residual, ldr = _near(residual, ldr, dev, s)
+    args = _PACK_LINEAR.pack(M, ldx, ldw, ldr, ldo, ldp, K, N, code, out_code, act, scale)
     need = _linear_need(M, K, N, code)
     ws = _workspace(need, dev, s) if need else None
     return (_packed_call("flashblock_linear_forward", "PPPPPPPPQP"),
             (args, x.data_ptr(), weight.data_ptr(), b, _addr(residual), out.data_ptr(), _addr(pre),
-             _addr(ws), need, s), ws, out, (M, ldx, ldw, K, N, code, out_code, act, scale, dev))
+             _addr(ws), need, s), (x, weight, bias, residual, out, pre, ws), out,
+            (M, ldx, ldw, K, N, code, out_code, act, scale, dev))
 
 
 def _size(name: str, kinds: str, *args) -> int:
@@ -294,6 +319,13 @@ def linear_backward(grad_out, x, weight, pre=None, activation="none", scale: flo
     if all(t is None for t in outs.values()):
         return outs
     dev = _one_device(grad_out, x, weight, pre if act else None, *outs.values())
+    if max(ldo, ldx, ldw, ldp) > LD_MAX:
+        s = _stream_handle(stream, dev)
+        grad_out, ldo = _near(grad_out, ldo, dev, s)
+        x, ldx = _near(x, ldx, dev, s)
+        weight, ldw = _near(weight, ldw, dev, s)
+        if act:
+            pre, ldp = _near(pre, ldp, dev, s)
     sizes = (M, ldx, ldw, K, N, code, code if odt == x.dtype else 0, act, scale, dev)
     _linear_gradients(sizes, grad_out, ldo, x, weight, pre if act else None, ldp, outs["x"],
                       ld.get("x", K), outs["weight"], ld.get("weight", K), outs["bias"], stream)
@@ -374,7 +406,8 @@ def norm_forward(x, weight=None, bias=None, residual=None, gate=None, scale: flo
         y = N(s) weight + bias                       (None without ``norm``)
 
     x            CUDA tensor [..., C] (float32, float16 or bfloat16): a block's
-                 output, rows at any one row stride.
+                 output, rows at any one row stride (far ones as in
+                 ``linear_forward``).
     weight, bias, post_weight, post_bias
                  optional [C], in x's dtype or float32 (one for all vectors).
     residual     optional [..., C] in x's dtype or float32: the stream that the
@@ -399,8 +432,8 @@ def norm_forward(x, weight=None, bias=None, residual=None, gate=None, scale: flo
 def _norm_forward(x, weight, bias, residual, gate, scale, norm, post_norm, post_weight, post_bias, eps,
                   out, out_s, stream):
     """norm_forward's (y, s, sizes for _norm_gradients)."""
-    call, args, y, s, sizes = _norm_call(x, weight, bias, residual, gate, scale, norm, post_norm,
-                                         post_weight, post_bias, eps, out, out_s, stream)
+    call, args, y, s, sizes, keep = _norm_call(x, weight, bias, residual, gate, scale, norm, post_norm,
+                                               post_weight, post_bias, eps, out, out_s, stream, False)
     with _on_device(sizes[-1]):
         rc = call(*args)
     if rc != 0:
@@ -417,15 +450,15 @@ def prepare_norm_forward(x, weight=None, bias=None, residual=None, gate=None, sc
     if (out is None and _norm_code(norm, "norm")) or (out_s is None and not _adds_nothing(
             x, residual, gate, scale, post_norm, out_s)):
         raise ValueError("a prepared call needs out and out_s")
-    call, args, _, _, sizes = _norm_call(x, weight, bias, residual, gate, scale, norm, post_norm,
-                                         post_weight, post_bias, eps, out, out_s, stream)
-    keep = (x, weight, bias, residual, gate, post_weight, post_bias, out, out_s)
+    call, args, _, _, sizes, keep = _norm_call(x, weight, bias, residual, gate, scale, norm, post_norm,
+                                               post_weight, post_bias, eps, out, out_s, stream, True)
     return _Prepared(call, args, keep, "flashblock_norm_forward", sizes[-1])
 
 
 def _norm_call(x, weight, bias, residual, gate, scale, norm, post_norm, post_weight, post_bias, eps, out,
-               out_s, stream):
-    """(C call, its arguments, y, s, sizes for _norm_gradients)."""
+               out_s, stream, again):
+    """(C call, its arguments, y, s, sizes for _norm_gradients, the tensors that the
+    arguments point into).  ``again``: the call may be made more than once."""
     import torch
 
     M, ldx = _rows(x, "x")
@@ -456,12 +489,20 @@ def _norm_call(x, weight, bias, residual, gate, scale, norm, post_norm, post_wei
         ldy = _rows(out, "out")[1]
     types = (code, code if sdt == x.dtype else 0, code if pdt is None or pdt == x.dtype else 0, kind, post,
              eps, scale)
-    args = _PACK_NORM.pack(M, ldx, ldr, lds, ldy, groups, C, *types)
     dev = _one_device(x, weight, bias, residual, gate, post_weight, post_bias, out, out_s)
     s = _stream_handle(stream, dev)
+    stays = x if same else out_s
+    if ldx > LD_MAX or (ldr > LD_MAX and residual is not out_s):
+        if again:
+            _no_copies(ldx, ldr)
+        x, ldx = _near(x, ldx, dev, s)
+        if residual is not None:
+            residual, ldr = _near(residual, ldr, dev, s)
+    args = _PACK_NORM.pack(M, ldx, ldr, lds, ldy, groups, C, *types)
     return (_packed_call("flashblock_norm_forward", "PPPPPPP"),
-            (args, vectors, x.data_ptr(), _addr(residual), _addr(out_s), _addr(out), s), out,
-            x if same else out_s, (M, ldx, ldx if same else lds, groups, C, types, dev))
+            (args, vectors, x.data_ptr(), _addr(residual), _addr(out_s), _addr(out), s), out, stays,
+            (M, ldx, ldx if same else lds, groups, C, types, dev),
+            (x, weight, bias, residual, gate, post_weight, post_bias, out, out_s))
 
 
 def norm_backward(grad_y, grad_s, x, s, weight=None, gate=None, scale: float = 1.0, norm="layer",
@@ -503,6 +544,14 @@ def norm_backward(grad_y, grad_s, x, s, weight=None, gate=None, scale: float = 1
     if not want:
         return {}
     dev = _one_device(grad_y, grad_s, x, s, weight, gate, post_weight, post_bias)
+    if max(ldx, lds, ldgy, ldgs) > LD_MAX:
+        st = _stream_handle(stream, dev)
+        x, ldx = _near(x, ldx, dev, st)
+        s, lds = _near(s, lds, dev, st)
+        if grad_y is not None:
+            grad_y, ldgy = _near(grad_y, ldgy, dev, st)
+        if grad_s is not None:
+            grad_s, ldgs = _near(grad_s, ldgs, dev, st)
     types = (code, code if sdt == x.dtype else 0, code if pdt == x.dtype else 0, kind, post, eps, scale)
     return _norm_gradients((M, ldx, lds, groups, C, types, dev), grad_y, ldgy, grad_s, ldgs, x, s, gate,
                            vectors, pdt, want, stream)
@@ -543,13 +592,16 @@ _AUTOGRAD = {}
 
 
 def _as_rows(t, width: int):
-    """(a gradient as it came, its row stride) where its rows are at one stride,
-    else of a copy."""
+    """(a gradient as it came, its row stride) where its rows are at one stride that
+    the library takes, else of a copy."""
     if not t.is_contiguous():
         try:
-            return t, _strided_rows(t, "gradient")[1]
+            ld = _strided_rows(t, "gradient")[1]
+            if ld <= LD_MAX:
+                return t, ld
         except ValueError:
-            t = t.contiguous()
+            pass
+        t = t.contiguous()
     return t, width
 
 
