@@ -122,6 +122,17 @@ def _addr(t) -> int:
     return 0 if t is None else t.data_ptr()
 
 
+_LINEAR_GRADS = ("x", "weight", "bias")
+_VECTORS = ("gate", "weight", "bias", "post_weight", "post_bias")
+_NORM_INPUTS = ("x", "residual", *_VECTORS)
+
+
+def _wanted(want, names) -> None:
+    for k in want:
+        if k not in names:
+            raise ValueError(f"want takes {names}")
+
+
 def _act_code(activation) -> int:
     try:
         return ACTIVATIONS[activation or "none"]
@@ -275,7 +286,7 @@ def _norm_need(M: int, groups: int, C: int, flags) -> int:
 
 
 def linear_backward(grad_out, x, weight, pre=None, activation="none", scale: float = 1.0,
-                    want=("x", "weight", "bias"), grad_x=None, grad_weight=None, grad_bias=None,
+                    want=_LINEAR_GRADS, grad_x=None, grad_weight=None, grad_bias=None,
                     stream=None):
     """The gradients of ``linear_forward`` for ``grad_out`` [..., N] (in the
     output's dtype): a dict with "x", "weight" and "bias", in x's dtype, None for
@@ -288,6 +299,7 @@ def linear_backward(grad_out, x, weight, pre=None, activation="none", scale: flo
     """
     import torch
 
+    _wanted(want, _LINEAR_GRADS)
     M, ldx = _rows(x, "x")
     code = _dtype_code(x)
     N, ldw = _weight(weight, x)
@@ -347,10 +359,6 @@ def _linear_gradients(sizes, grad_out, ldo, x, weight, pre, ldp, grad_x, ldgx, g
                   _addr(grad_x), ldgx, _addr(grad_weight), ldgw, _addr(grad_bias), _addr(ws), need, s)
     if rc != 0:
         raise FlashBevError(rc, "flashblock_linear_backward")
-
-
-_VECTORS = ("gate", "weight", "bias", "post_weight", "post_bias")
-_NORM_INPUTS = ("x", "residual", *_VECTORS)
 
 
 def _norm_code(kind, name: str) -> int:
@@ -538,9 +546,7 @@ def norm_backward(grad_y, grad_s, x, s, weight=None, gate=None, scale: float = 1
     if grad_s is not None:
         _same(grad_s, "grad_s", sdt, x.shape)
         ldgs = _rows(grad_s, "grad_s")[1]
-    for k in want:
-        if k not in _NORM_INPUTS:
-            raise ValueError(f"want takes {_NORM_INPUTS}")
+    _wanted(want, _NORM_INPUTS)
     if not want:
         return {}
     dev = _one_device(grad_y, grad_s, x, s, weight, gate, post_weight, post_bias)
