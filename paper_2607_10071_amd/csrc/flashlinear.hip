@@ -469,13 +469,13 @@ __device__ const uint32_t kZeros[4] = {0, 0, 0, 0};
 __device__ __forceinline__ void to_lds(const void *base, uint32_t off, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                 :: "s"(lds), "v"(off), "s"(base) : "memory");
+                 :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 
 __device__ __forceinline__ void to_lds(const void *p, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                 :: "s"(lds), "v"(p) : "memory");
+                 :: "s"(lds), "v"(p) : "memory", "m0");
 }
 
 // Until at most N vector memory operations are in flight: s_waitcnt with vmcnt N
