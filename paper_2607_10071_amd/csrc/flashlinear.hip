@@ -461,7 +461,7 @@ __global__ void __launch_bounds__(WM *WN * 64) linear_tiles(Gemm p)
 // consecutive ones, which need no pass through LDS.
 //
 // Granules past the reduction axis's end come from 16 bytes of zeros.
-__device__ const uint32_t kZeros[4] = {0, 0, 0, 0};
+__device__ const __attribute__((aligned(16))) uint32_t kZeros[4] = {0, 0, 0, 0};
 
 // 16 bytes of each lane to LDS at `lds` + 16 lane.  Written in assembly, without
 // registers to be written: the compiler would wait for every load in flight before
