@@ -465,17 +465,18 @@ __device__ const __attribute__((aligned(16))) uint32_t kZeros[4] = {0, 0, 0, 0};
 
 // 16 bytes of each lane to LDS at `lds` + 16 lane.  Written in assembly, without
 // registers to be written: the compiler would wait for every load in flight before
-// the next LDS read, whichever stage it reads.
+// the next LDS read, whichever stage it reads.  m0, which holds the place in LDS, is an
+// operand, so that the compiler knows it (s_nop: the wait between its write and the load).
 __device__ __forceinline__ void to_lds(const void *base, uint32_t off, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                 :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :: "{m0}"(lds), "v"(off), "s"(base) : "memory");
 }
 
 __device__ __forceinline__ void to_lds(const void *p, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                 :: "s"(lds), "v"(p) : "memory", "m0");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :: "{m0}"(lds), "v"(p) : "memory");
 }
 
 // Until at most N vector memory operations are in flight: s_waitcnt with vmcnt N
