@@ -68,7 +68,7 @@ typedef enum {
     FLASHBEV_ERR_SHAPE = -2,       /* a dimension is negative or zero where >= 1 is needed */
     FLASHBEV_ERR_DTYPE = -3,       /* unknown feature dtype                      */
     FLASHBEV_ERR_ALIGN = -4,       /* a device pointer is not element-aligned    */
-    FLASHBEV_ERR_UNSUPPORTED = -5, /* beyond a documented limit (Z, N, row, 2 GiB) */
+    FLASHBEV_ERR_UNSUPPORTED = -5, /* beyond a documented limit (Z, N, row, 2 GiB, 2^32 threads) */
     FLASHBEV_ERR_ALIAS = -6,       /* out overlaps an input                      */
     FLASHBEV_ERR_VALUE = -7,       /* non-finite grid spec or bad reduce mode    */
     FLASHBEV_ERR_HIP = -8,         /* the kernel launch failed                   */

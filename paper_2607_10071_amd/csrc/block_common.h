@@ -215,14 +215,12 @@ inline bool known_dtype(int dt) { return dt >= FLASHBEV_F32 && dt <= FLASHBEV_BF
 
 inline bool misaligned(const void *p, int a) { return ((uintptr_t)p & (uintptr_t)(a - 1)) != 0; }
 
-// An axis of a grid holds fewer than 2^32 threads: past them HIP launches what is left
-// modulo 2^32, without an error.
 template <class P>
 int launch_kernel(const void *fn, uint64_t blocks, int threads, P &p, size_t lds, hipStream_t st,
                   unsigned grid_rows = 1)
 {
     if (blocks == 0) return FLASHBEV_OK;
-    if (blocks > 0x7fffffffull || blocks * threads > 0xffffffffull) return FLASHBEV_ERR_UNSUPPORTED;
+    if (blocks > 0x7fffffffull || !grid_fits((int64_t)blocks, threads)) return FLASHBEV_ERR_UNSUPPORTED;
     void *args[] = {&p};
     return hipLaunchKernel(fn, dim3((unsigned)blocks, grid_rows), dim3(threads), args, lds, st) == hipSuccess
                ? FLASHBEV_OK : FLASHBEV_ERR_HIP;

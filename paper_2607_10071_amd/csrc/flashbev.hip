@@ -2391,8 +2391,8 @@ int make_plan(const flashbev_features *f, const float *l2i, const flashbev_bev_g
     for (int k = 0; k < zb->Z; ++k) p.z[k] = zb->z[k];
 
     pl->workgroups = empty ? 0 : (int64_t)f->B * p.tiles_per_b;
-    if (pl->workgroups > 0x7FFFFFFFll) return FLASHBEV_ERR_UNSUPPORTED;
     pl->threads = waves * kWave;
+    if (!grid_fits(pl->workgroups, pl->threads)) return FLASHBEV_ERR_UNSUPPORTED;
     pl->lds = lay.total;
     pl->lw = lw;
     pl->vpl = vpl;
@@ -2643,8 +2643,8 @@ int make_bwd_plan(const flashbev_features *f, const float *l2i, const flashbev_b
     for (int k = 0; k < zb->Z; ++k) p.z[k] = zb->z[k];
 
     pl->workgroups = scatter ? (int64_t)f->B * p.tiles_per_b : 0;
-    if (pl->workgroups > 0x7FFFFFFFll) return FLASHBEV_ERR_UNSUPPORTED;
     pl->threads = (tiled ? t_waves : waves) * kWave;
+    if (!grid_fits(pl->workgroups, pl->threads)) return FLASHBEV_ERR_UNSUPPORTED;
     pl->lds = tiled ? l_total : lay.total;
     pl->kpl = kpl;
     pl->tiled = tiled;
@@ -2836,7 +2836,8 @@ int make_bwd_gather_plan(const flashbev_features *f, const float *l2i,
 
     pl->prep_wgs = (gelems > 0) ? (int64_t)f->B * p.prep_tiles_per_b * p.prep_cblocks : 0;
     pl->gather_wgs = (gelems > 0) ? (p.groups + kGatherWaves - 1) / kGatherWaves : 0;
-    if (pl->prep_wgs > 0x7FFFFFFFll || pl->gather_wgs > 0x7FFFFFFFll) return FLASHBEV_ERR_UNSUPPORTED;
+    if (!grid_fits(pl->prep_wgs, 256) || !grid_fits(pl->gather_wgs, kGatherWaves * kWave))
+        return FLASHBEV_ERR_UNSUPPORTED;
     pl->lds = (size_t)p.lds_wave * kGatherWaves;
     if (pl->lds > kLdsBudget) return FLASHBEV_ERR_UNSUPPORTED;
     pl->lw = lw;

@@ -2155,8 +2155,8 @@ int make_sca_plan(const flashsca_value *v, const flashbev_bev_grid_spec *s,
     else p.ord_blocks = 0;
 
     pl->workgroups = empty ? 0 : (int64_t)v->B * p.tiles_per_b;
-    if (pl->workgroups > 0x7FFFFFFFll) return FLASHBEV_ERR_UNSUPPORTED;
     pl->threads = waves * kScaWave;
+    if (!grid_fits(pl->workgroups, pl->threads)) return FLASHBEV_ERR_UNSUPPORTED;
     pl->lds = lay.total;
     pl->lw = lw;
     pl->empty = empty;
@@ -2352,7 +2352,7 @@ int launch_fn(ScaFn fn, ScaParams &p, uint64_t workgroups, int threads, size_t l
               hipStream_t st)
 {
     if (workgroups == 0) return FLASHBEV_OK;
-    if (workgroups > 0x7FFFFFFFull) return FLASHBEV_ERR_UNSUPPORTED;
+    if (!grid_fits((int64_t)workgroups, threads)) return FLASHBEV_ERR_UNSUPPORTED;
     if (lds > kScaLdsBudget &&
         hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
         return FLASHBEV_ERR_HIP;

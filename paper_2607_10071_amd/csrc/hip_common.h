@@ -1,7 +1,7 @@
 // Helpers shared by the library's kernels (flashbev.hip, flashsca.hip):
 // 16/8/4/2-byte buffer loads, exact conversion of stored elements to
 // float32, wavefront-local LDS ordering, a small exact integer division, and
-// on the host a size product that cannot wrap.
+// on the host a size product that cannot wrap and the size limit of a grid.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -98,6 +98,13 @@ inline uint64_t size_prod(std::initializer_list<uint64_t> factors)
         p *= v;
     }
     return p;
+}
+
+// Whether an axis of a grid takes so many workgroups.  It holds fewer than 2^32 threads:
+// past them HIP launches what is left modulo 2^32, without an error.
+inline bool grid_fits(int64_t workgroups, int threads)
+{
+    return workgroups <= 0x7fffffffll && workgroups * threads <= 0xffffffffll;
 }
 
 }  // namespace
