@@ -730,6 +730,10 @@ __device__ __forceinline__ void write_any(const Gemm &p, int part, int m, int n,
 #undef FLASHBLOCK_WRITE
 }
 
+// LDS lets two workgroups of 64 x 64 or 128 x 128 tiles onto a CU, or one of 256 x 256: two
+// wavefronts a SIMD.  The compiler's bound of four for 64 x 64 tiles is for its choice of
+// registers alone (at most 128): with two 40000 x 256 x 256 float32 takes 62 us, with four 58;
+// other products are the same to 2%.
 template <int DT, bool AX, bool BX, int BM, int BN, int WM, int WN, int S, bool ENDS>
 __global__ void __launch_bounds__(WM *WN * 64, BM == 64 ? 4 : 2) linear_stream(Gemm p)
 {
@@ -887,13 +891,13 @@ __global__ void __launch_bounds__(WM *WN * 64, BM == 64 ? 4 : 2) linear_stream(G
 // ---------------------------------------------------------------------------
 // few rows: one pass over the weight
 // ---------------------------------------------------------------------------
-// Up to 32 rows (one or two blocks of 16) read every weight once, which is all the
+// Up to 32 rows (one or two blocks of 16) read every weight once, which is nearly all the
 // time they take.  A workgroup owns 16 output channels; its 8 wavefronts take the
 // K axis in turns of 16 (for two blocks 8) 64-byte pieces of each of the 16 weight
 // rows (a piece: a 16x16x32 MFMA of 16-bit elements, or four 16x16x4 of float32), all
 // in flight, from memory straight into the operands; their sums are added through LDS in the
 // wavefronts' order.  One launch and no workspace: 1 x 4096 x 4096 bfloat16 takes 8.5 us
-// (33.6 MB, 4 TB/s) where parts of 64 x 64 tiles and their join took 14.6.
+// (33.6 MB, 4 TB/s) where parts of 64 x 64 tiles and their join take 11.3.
 constexpr int kFewRows = 32;
 constexpr int kFewWaves = 8;
 
@@ -1089,6 +1093,11 @@ __global__ void __launch_bounds__(256) linear_slope(Slope p)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) g[e] *= act_slope(p.act, v[e]);
             }
+            // d is rounded to the inputs' type, in which the matrix units read it (its column
+            // sums are not); pre was rounded to it as the forward wrote it.  On 4000 x 256 x 1024
+            // bfloat16 with gelu the products' gradients are 0.00241 off float64 (norms of the
+            // difference and the value) where their own rounding alone is 0.00166: 0.00235 for
+            // d alone, 0.00175 for pre alone.
             const float scale = p.copy ? 1.0f : p.scale;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -1150,7 +1159,12 @@ uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 // products: in 256, 128 and 64 tiles, bfloat16, 8192 x 8192 over 4096 takes 461, 536 and
 // 937; 184950 x 256 over 256 51, 57 and 86; 40000 x 512 over 256 with a float32 output
 // 41, 27 and 38; 1024 x 256 over 40000 (in parts) 57, 57 and 74; float32
-// 40000 x 256 over 256 75, 60 and 55.
+// 40000 x 256 over 256 77, 58 and 58.  float32 tiles of 256 and 128 are close where both fill the
+// card (8192 cubed 7687 and 7550, 16384 x 4096 over 4096 3879 and 3796, gradient 512 x 512
+// over 65536 270 and 278) and up to 18% apart where the estimate takes 256 for a short axis
+// (40001 x 520 over 72 71 and 60).  Checked tiles of 128 and 64: half 3331 x 777 over 515 22 and 16,
+// bfloat16 40001 x 72 over 129 12.8 and 14.6, 40001 x 520 over 129 46 and 42, 8191 x 4095 over 4095
+// 416 and 659, 200 x 72 over 129 10.1 and 5.6.  `estimate` gets the least time.
 struct TilePlan {
     int tile, split, steps;
     uint64_t workspace;    // bytes of partial sums
@@ -1167,7 +1181,8 @@ constexpr TileCost kStream32[] = {{256, kCus, 7.4f, 7.5f}, {128, 2 * kCus, 3.8f,
 // linear_tiles, which widths of other than whole granules take
 constexpr TileCost kChecked[] = {{128, 2 * kCus, 3.0f, 4.0f}, {64, 4 * kCus, 1.5f, 3.0f}};
 
-TilePlan plan_tiles(int64_t rows, int64_t cols, int64_t red, int dt, bool checked)
+TilePlan plan_tiles(int64_t rows, int64_t cols, int64_t red, int dt, bool checked,
+                    float *estimate = nullptr)
 {
     const int64_t total = (red + 128 / elem_size(dt) - 1) / (128 / elem_size(dt));
     TilePlan best{64, 1, (int)(total > 0 ? total : 1), 0};
@@ -1192,7 +1207,20 @@ TilePlan plan_tiles(int64_t rows, int64_t cols, int64_t red, int dt, bool checke
     }
     if (best.split > 1)
         best.workspace = round_up((uint64_t)best.split * rows * round_up(cols, 8) * 4, 256);
+    if (estimate) *estimate = least;
     return best;
+}
+
+// linear_few's time (us): a workgroup's grows with its weights' row and with the rows of x,
+// and 256 workgroups (4096 channels) run at once.  Against tiles (M x K x N, the kernel's
+// and the tiles' measured us): bfloat16 1 x 4096 x 4096 8.5 and 11.3, 16 rows 10.7 and 12.2,
+// 32 rows 14.5 and 12.6, 16 x 4096 x 64 9.6 and 6.7, 32 x 1024 x 1024 5.5 and 7.2; float32
+// 1 x 4096 x 4096 16.6 and 25.4, 32 rows 26.3 and 26.8, 32 x 8192 x 64 44 and 10.5, 16 x 4096 x 1024
+// 17.6 and 13.9.  More than 32 rows would take two calls (33 x 4096 x 4096 21.4 and 12.6).
+float few_estimate(const flashblock_linear *p)
+{
+    const float bytes = (float)p->K * elem_size(p->dtype), rounds = (float)p->N / 4096.0f;
+    return 3.0f + bytes * (0.0005f + 0.000025f * (float)p->M) * (rounds > 1.0f ? rounds : 1.0f);
 }
 
 // What the sizes alone say about linear_stream's layout (linear_stream also needs
@@ -1217,9 +1245,11 @@ bool forms_d(const flashblock_linear *p)
 
 TilePlan plan_forward(const flashblock_linear *p)
 {
-    if (p->M <= kFewRows) return {0, 1, 0, 0};   // linear_few
-    return plan_tiles(p->M, p->N, p->K, p->dtype,
-                      !whole_granules(p->M, p->N, p->K, p->dtype, false, false, false));
+    float us;
+    const TilePlan t = plan_tiles(p->M, p->N, p->K, p->dtype,
+                                  !whole_granules(p->M, p->N, p->K, p->dtype, false, false, false), &us);
+    if (p->M <= kFewRows && few_estimate(p) <= us) return {0, 1, 0, 0};   // linear_few
+    return t;
 }
 
 TilePlan plan_grad_x(const flashblock_linear *p)
@@ -1443,7 +1473,7 @@ int flashblock_linear_forward(const flashblock_linear *p, const void *x, const v
     }
     Epilogue e{out, pre, bias, residual, p->ldo, p->ldp, p->ldr, p->scale, p->act,
                p->out_dtype == FLASHBEV_F32};
-    if (p->M <= kFewRows) {
+    if (plan.tile == 0) {
         Few f{static_cast<const char *>(x), static_cast<const char *>(weight), p->ldx * es,
               p->ldw * es, (int)p->M, p->N, p->K, e};
         const bool two = p->M > 16;

@@ -146,3 +146,22 @@ def test_input_gradients_past_32_bits(fb, device):
     got = fb.linear_backward(g, x, w, want=("x",))["x"]
     assert torch.equal(got[-5:], (g[-5:].double() @ w.double()).to(torch.bfloat16))
     assert (got[:-5] == 0).all()
+
+
+@pytest.mark.parametrize("types", TYPES, ids="-".join)
+@pytest.mark.parametrize("K,N", [(64, 64), (1032, 200), (4096, 64), (8192, 1000), (8200, 33), (4099, 70), (2048, 4099)])
+@pytest.mark.parametrize("M", [1, 2, 16, 17, 32, 33])
+def test_few_rows_exact(fb, device, M, K, N, types):
+    """On both sides of the rule that sends up to 32 rows to one pass over the weight or to
+    tiles; sums of at most 8200 products of at most 4 in magnitude."""
+    dt, odt = (ref.DTYPES[t] for t in types)
+    gen = torch.Generator(device=device).manual_seed(M + N)
+    x, w, b = (whole(gen, *s, dtype=dt) for s in ((M, K), (N, K), (N,)))
+    pre = x.double() @ w.double().t() + b.double()
+    r = whole(gen, M, N, dtype=odt, most=8)
+    big, into = inside(r, gen)
+    before = big.clone()
+    p = torch.empty(M, N, dtype=dt, device=device)
+    assert fb.linear_forward(x, w, b, "relu", into, 0.5, out=into, pre=p) is into
+    assert torch.equal(into, (r.double() + 0.5 * pre.clamp(min=0)).to(odt))
+    assert torch.equal(p, pre.to(dt)) and untouched(big, before, N)

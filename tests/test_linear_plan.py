@@ -30,3 +30,23 @@ def test_every_kernel_is_taken():
         assert {"s64", "s128", "s256", "e64", "e128", "e256", "c128"} <= tiles(f[i] for f in lp.FORWARD)
         assert {"s64", "s128", "s256", "c128"} <= tiles(f[i][0] for f in lp.BACKWARD)
         assert {"s64", "s128", "s256", "c64"} <= tiles(f[i][1] for f in lp.BACKWARD)
+
+
+@pytest.mark.parametrize("size,dtype,parts", [
+    ((1, 4096, 4096), 2, False), ((16, 4096, 4096), 2, False), ((32, 1024, 1024), 2, False),
+    ((32, 32, 32), 0, False), ((32, 256, 256), 0, False), ((1, 4096, 4096), 0, False), ((1, 8, 1 << 18), 2, False),
+    ((1, 8192, 64), 2, True), ((32, 4096, 4096), 2, True), ((16, 8192, 256), 0, True),
+    ((32, 8192, 64), 0, True), ((32, 8192, 8192), 0, True), ((17, 8192, 33), 0, True)])
+def test_few_rows(size, dtype, parts):
+    """Up to 32 rows take one pass over the weight (no workspace) where that is the faster
+    one, and tiles in parts where the reduction axis is long beside the rest."""
+    import ctypes
+
+    import paper_2607_10071_amd as fb
+    from paper_2607_10071_amd import block
+
+    M, K, N = size
+    n = ctypes.c_uint64()
+    args = block._PACK_LINEAR.pack(M, K, K, N, N, N, K, N, dtype, dtype, 0, 1.0)
+    assert fb._packed_call("flashblock_linear_workspace_size", "PP")(args, ctypes.byref(n)) == 0
+    assert (n.value > 0) == parts
