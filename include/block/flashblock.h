@@ -219,7 +219,8 @@ typedef struct {
  *   grad_residual [M, C] in stream_dtype at stride ldgr, or NULL.
  *   workspace     device, at least flashblock_norm_backward_workspace_size
  *                 bytes, 256-byte aligned (partial sums of the vectors'
- *                 gradients); NULL where that is 0.
+ *                 gradients: for each vector a float32 row for every range of
+ *                 rows, of which a sample has one or more); NULL where that is 0.
  *
  * At least one gradient must be asked for, and grad_y or grad_s given.
  */

@@ -522,7 +522,8 @@ def norm_backward(grad_y, grad_s, x, s, weight=None, gate=None, scale: float = 1
     x, s     the forward's input and its second result.
     want     which of "x", "residual", "gate", "weight", "bias", "post_weight" and
              "post_bias"; the vectors' gradients come in the vectors' dtype
-             (x's, where no vector is given).
+             (x's, where no vector is given).  Each vector asked for takes at least
+             one float32 row of workspace for every sample of a gate [G, C].
 
     Returns a dict of those gradients.  Asynchronous.
     """
@@ -680,6 +681,8 @@ def _autograd_functions():
     class _Linear(torch.autograd.Function):
         @staticmethod
         def forward(ctx, x, weight, bias, residual, activation, scale, out_dtype):
+            # in x's type: float32 would be twice the bytes to write and read again, for
+            # gradients 0.00235 off in place of 0.00241 (bfloat16, gelu)
             pre = None
             if _act_code(activation) and any(ctx.needs_input_grad[:3]):
                 pre = torch.empty((*x.shape[:-1], weight.shape[0]), dtype=x.dtype, device=x.device)
@@ -737,7 +740,7 @@ def norm_autograd(x, weight=None, bias=None, residual=None, gate=None, scale: fl
                   norm="layer", post_norm=None, post_weight=None, post_bias=None, eps: float = 1e-5):
     """``norm_forward`` as a differentiable function of x, residual, gate, weights
     and biases; the gradients are ``norm_backward``'s, computed only for the inputs
-    that need them."""
+    that need them.  (In a HIP graph as for ``linear_autograd``.)"""
     y, s = _autograd_functions()["norm"].apply(x, residual, gate, weight, bias, post_weight, post_bias,
                                                scale, norm, post_norm, eps)
     return y, x if s is None else s
