@@ -2,8 +2,9 @@
 encoder block for AMD MI355X.
 
 A thin Python binding over the C ABI of ``include/flashbev.h``,
-``include/flashsca.h`` and ``include/block/flashblock.h`` (``libflashbev.so``).  It only marshals arguments: every step of the
-operator runs in the library's HIP kernel.  PyTorch supplies device memory
+``include/flashsca.h``, ``include/block/flashblock.h`` and
+``include/block/flashlayer.h`` (``libflashbev.so``).  It only marshals arguments: every
+step of the operators runs in the library's HIP kernels.  PyTorch supplies device memory
 and the current stream.  If the built library is missing the calls raise;
 there is no fallback implementation.
 """
@@ -26,6 +27,9 @@ __all__ = [
     "linear_forward", "linear_backward", "linear_autograd",
     "norm_forward", "norm_backward", "norm_autograd",
     "prepare_linear_forward", "prepare_norm_forward",
+    "attention_forward", "attention_backward", "attention_autograd", "prepare_attention_forward",
+    "group_norm_forward", "group_norm_backward", "group_norm_autograd", "prepare_group_norm_forward",
+    "dropout_forward", "dropout_backward", "dropout_autograd", "prepare_dropout_forward",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -1182,3 +1186,11 @@ def sca_autograd(value, lidar2img, anchors, grid: BevGrid, img_hw: Tuple[int, in
 from .block import (linear_autograd, linear_backward, linear_forward,  # noqa: E402
                     norm_autograd, norm_backward, norm_forward, prepare_linear_forward,
                     prepare_norm_forward)
+
+# ---------------------------------------------------------------------------
+# the operators that complete a layer (include/block/flashlayer.h)
+# ---------------------------------------------------------------------------
+from .layer import (attention_autograd, attention_backward, attention_forward,  # noqa: E402
+                    dropout_autograd, dropout_backward, dropout_forward, group_norm_autograd,
+                    group_norm_backward, group_norm_forward, prepare_attention_forward,
+                    prepare_dropout_forward, prepare_group_norm_forward)

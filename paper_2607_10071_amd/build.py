@@ -4,8 +4,9 @@
 
 Produces ``paper_2607_10071_amd/libflashbev.so`` (the fused Sampling-VT
 forward and backward behind the C ABI of ``include/flashbev.h``, FlashSCA
-behind ``include/flashsca.h`` and the encoder block's product and norms behind
-``include/block/flashblock.h``) and
+behind ``include/flashsca.h``, the encoder block's product and norms behind
+``include/block/flashblock.h`` and the rest of a layer behind
+``include/block/flashlayer.h``) and
 ``libflashbev_membench.so`` (the memory-ceiling micro-benchmarks of
 ``include/flashbev_membench.h`` that bench.py uses) and
 ``libflashbev_phases.so`` (the same operator library with the forward's
@@ -27,7 +28,9 @@ INCLUDE = os.path.join(ROOT, "include")
 SRC = os.path.join(HERE, "csrc", "flashbev.hip")
 SCA_SRC = os.path.join(HERE, "csrc", "flashsca.hip")
 # the operators around FlashSCA in an encoder block
-BLOCK_SRCS = [os.path.join(HERE, "csrc", f) for f in ("flashlinear.hip", "flashnorm.hip")]
+BLOCK_SRCS = [os.path.join(HERE, "csrc", f) for f in (
+    "flashlinear.hip", "flashnorm.hip", "flashgroup.hip", "flashdrop.hip", "flashattend.hip",
+    "flashattend_grad.hip")]
 LIB = os.path.join(HERE, "libflashbev.so")
 # memory-ceiling micro-benchmarks used by bench.py (not part of the operator)
 MEMBENCH_SRC = os.path.join(HERE, "csrc", "membench.hip")

@@ -1,0 +1,487 @@
+// What the forward and the backward of attention share (flashattend.hip,
+// flashattend_grad.hip): a call's arguments in device form, panels of rows in LDS and the
+// fragments that the matrix units take from them, masks, and on the host the checks.
+//
+// Rows.  The query heads that share a head of the states are rows of one problem: for batch b
+// and head g of the states, row r is query r / share and query head g share + r % share.  Keys
+// and values are then read once for all of them, their gradients are sums over rows, and the
+// single new token of a serving step has `share` rows.
+//
+// Products.  A wavefront forms the scores of 32 keys and 32 rows with keys down and rows
+// across: a lane then holds 16 of its row's scores (row lane % 32, keys 8 k + 4 h + 0..3 for
+// k = 0..3 and its half h), a row's maximum and sum stay within a lane and its other half, and the
+// same registers, packed, are the operand of the product with v, whose reduction runs over
+// the keys in the order that the registers have.
+#pragma once
+
+#include <algorithm>
+
+#include "block/flashlayer.h"
+#include "block_mma.h"
+
+namespace {
+
+constexpr float kLog2 = 1.4426950408889634f;   // of e
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ __forceinline__ float log2_fast(float v) { return __builtin_amdgcn_logf(v); }
+
+struct Attend {
+    const char *q, *k, *v, *g;       // g: the output's gradient
+    char *o;
+    const char *mask;                // null: none
+    const int32_t *lengths;          // null: all Lk
+    int64_t qb, qr, qh, kb, kr, kh, vb, vr, vh, ob, orow, oh, mb, mh, mr;   // bytes
+    int B, Lq, Lk, H, Hk, D;
+    int share, rows;                 // rows = Lq share
+    uint32_t share_inv;              // ceil(2^32 / share), share > 1
+    int kind;                        // flashlayer_mask
+    int drops;                       // a boolean mask that is the same for all rows of a problem
+    float scale;
+    int tiles;                       // of rows (forward, grad_q) or of keys (grad_k, grad_v)
+    int splits;
+    uint32_t blocks, per_xcd;
+
+    __device__ __forceinline__ void row(int r, int &i, int &j) const   // query, head within the share
+    {
+        i = share > 1 ? (int)__umulhi((uint32_t)r, share_inv) : r;
+        j = r - i * share;
+    }
+
+    __device__ __forceinline__ int keys(int b) const
+    {
+        return lengths ? max(0, min(lengths[b], Lk)) : Lk;
+    }
+};
+
+// An XCD's workgroups (one in eight of the grid) take a contiguous share of the items: the
+// tiles that read the same keys meet in one L2.
+__device__ __forceinline__ uint32_t item_of(const Attend &p)
+{
+    return blockIdx.x / 8 < p.per_xcd ? blockIdx.x % 8 * p.per_xcd + blockIdx.x / 8 : p.blocks;
+}
+
+// R rows of up to DP elements in LDS, 16-byte granules.  Rows stand an odd multiple of 64 bytes
+// apart and granule g of row r at place g ^ (r / 4 & 3): 16 lanes that read one granule of 16
+// rows use all 64 banks, and so do half a wavefront's transposed reads of 4 rows x 64 bytes.
+template <int DT, int DP, int R>
+struct Panel {
+    static constexpr int ES = elem_size(DT), E = 16 / ES;
+    static constexpr int GR = DP * ES / 16;                    // granules of a row
+    static constexpr int STRIDE = DP * ES + (DP * ES / 64 % 2 ? 0 : 64);
+    static constexpr int BYTES = R * STRIDE;
+    static constexpr int RP = 256 / GR < R ? 256 / GR : R;     // rows that the workgroup takes at once
+    static constexpr int G = (R + RP - 1) / RP;                // granules of a thread
+    static constexpr int CHUNKS = GR / 2;                      // of an MFMA's reduction, in DP
+    static constexpr int STEPS = E == 8 ? 2 : 4;               // ..., in 32 rows
+
+    static __device__ __forceinline__ int place(int row, int g) { return row * STRIDE + ((g ^ (row >> 2 & 3)) << 4); }
+
+    // A row's granule, zeros past its D elements.
+    static __device__ __forceinline__ u32x4 granule(const char *row, int g, int D)
+    {
+        if ((g + 1) * E <= D) return load16(row + g * 16);
+        if (g * E < D) return load_granule_edge<DT>(row, g * E, D);
+        return u32x4{0, 0, 0, 0};
+    }
+
+    // Rows on their way from memory to LDS: thread tid takes granule tid % GR of rows
+    // tid / GR, + RP, ...  D a multiple of E: a tile's loads are under way while the last one
+    // is worked on.  Other widths are copied when it is their turn.
+    struct Mover {
+        int row, g;
+        uint32_t off;      // of the granule from the tile's first row
+        bool mine;
+
+        __device__ __forceinline__ void start(int tid, int D, int64_t stride)
+        {
+            row = tid / GR;
+            g = tid - row * GR;
+            off = (uint32_t)row * (uint32_t)stride + g * 16;
+            mine = row < RP && g * E < D;
+        }
+
+        // `base`: the tile's first row, of which `left` are there; there(i) says of row + i RP
+        // whether it is wanted
+        template <class There>
+        __device__ __forceinline__ void load(u32x4 (&v)[G], const char *base, int64_t stride, int left,
+                                             There there) const
+        {
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                v[i] = u32x4{0, 0, 0, 0};
+                if (mine && row + i * RP < left && there(row + i * RP)) v[i] = load16(base + i * RP * stride + off);
+            }
+        }
+
+        __device__ __forceinline__ void store(const u32x4 (&v)[G], char *lds) const
+        {
+            if (row >= RP) return;
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                if (R % RP == 0 || row + i * RP < R)
+                    *reinterpret_cast<u32x4 *>(lds + place(row + i * RP, g)) = v[i];
+        }
+
+        template <class There>
+        __device__ __forceinline__ void copy(char *lds, const char *base, int64_t stride, int left, int D,
+                                             There there) const
+        {
+            if (row >= RP) return;
+#pragma unroll 1
+            for (int i = row; i < R; i += RP) {
+                u32x4 v = {0, 0, 0, 0};
+                if (i < left && there(i)) v = granule(base + i * stride, g, D);
+                *reinterpret_cast<u32x4 *>(lds + place(i, g)) = v;
+            }
+        }
+    };
+
+    // A lane's places in a panel: all it reads is at these and distances that are known ahead.
+    struct Reader {
+        int along_[2], across_[2];
+
+        __device__ __forceinline__ void start(int lane)
+        {
+            const int i = lane & 31, h = lane >> 5;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) along_[e] = place(i, 2 * e + h);
+            if constexpr (ES == 2) {
+                const int j = lane & 15, a = lane >> 4 & 1, b = j >> 1 & 1;
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    across_[q] = (4 * h + (j >> 2)) * STRIDE + ((2 * (a ^ q) + (b ^ h)) << 4) + (j & 1) * 8;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    across_[e] = 4 * h * STRIDE + ((i >> 2 ^ (2 * e + h)) << 4) + (i & 3) * 4;
+            }
+        }
+
+        // Reduction along the rows' elements: the lane's granule of chunk c of row r0 + lane % 32.
+        __device__ __forceinline__ u32x4 along(const char *lds, int r0, int c) const
+        {
+            return *reinterpret_cast<const u32x4 *>(lds + along_[c & 1] + r0 * STRIDE + (c >> 1) * 64);
+        }
+
+        // Reduction over the rows, in the order of a block's registers (above): the lane's granule
+        // of step u of rows r0 .. r0 + 31 for element d0 + lane % 32.
+        __device__ __forceinline__ u32x4 across(const char *lds, int r0, int u, int d0) const
+        {
+            u32x4 v;
+            if constexpr (ES == 2) {
+                // ds_read_b64_tr_b16: 16 lanes take 4 rows x 16 elements, each ends with one
+                // element's 4 rows
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const s16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (__attribute__((address_space(3))) s16x4 *)(lds + across_[q] + (r0 + 16 * u + 8 * q) * STRIDE +
+                                                                    d0 * 2));
+                    const uint64_t w = __builtin_bit_cast(uint64_t, t);
+                    v[2 * q] = (uint32_t)w;
+                    v[2 * q + 1] = (uint32_t)(w >> 32);
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    v[q] = *reinterpret_cast<const uint32_t *>(lds + across_[u & 1] + (r0 + 8 * u + q) * STRIDE + d0 * 4);
+            }
+            return v;
+        }
+    };
+};
+
+// Step u's operand of a block's registers, rounded to the inputs' type.
+template <int DT>
+__device__ __forceinline__ u32x4 operand(const f32x16 &v, int u)
+{
+    if constexpr (DT == FLASHBEV_F32) {
+        return __builtin_bit_cast(u32x4, f32x4{v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]});
+    } else {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack2<DT>(v[8 * u + 2 * i], v[8 * u + 2 * i + 1]);
+        return w;
+    }
+}
+
+__device__ __forceinline__ f32x16 zeros16()
+{
+    f32x16 v;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+    return v;
+}
+
+// A lane's row of a block with the rows across: its fragments, straight from memory.
+template <int DT, int DP, int N>
+__device__ __forceinline__ void row_fragments(u32x4 (&f)[N], const char *row, bool there, int D, int lane)
+{
+    using P = Panel<DT, DP, 32>;
+    static_assert(N == P::CHUNKS, "a row's granules");
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        f[c] = u32x4{0, 0, 0, 0};
+        if (there) f[c] = P::granule(row, 2 * c + (lane >> 5), D);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// masks
+// ---------------------------------------------------------------------------
+typedef uint32_t u32_any __attribute__((aligned(1)));
+
+// Scores x of keys key0 + 8 k + 4 h + i of a lane's row, scaled and masked: x = scale x + mask.
+// `row` is the mask's row; Lk its length.
+__device__ __forceinline__ void mask_row(const Attend &p, f32x16 &x, const char *row, int key0, int h)
+{
+    const bool whole = key0 + 32 <= p.Lk;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int key = key0 + 8 * k + 4 * h;
+        if (p.kind == FLASHLAYER_MASK_BOOL) {
+            uint32_t w = 0;
+            if (whole) {
+                w = *reinterpret_cast<const u32_any *>(row + key);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (key + i < p.Lk) w |= (uint32_t)(uint8_t)row[key + i] << (8 * i);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                x[4 * k + i] = w >> (8 * i) & 0xff ? x[4 * k + i] * p.scale : -__builtin_inff();
+        } else {
+            float b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            const bool wide = p.kind == FLASHLAYER_MASK_ADD_F32;
+            if (wide) {
+                if (whole) {
+                    const f32x4 t = __builtin_bit_cast(f32x4, load16(row + (int64_t)key * 4));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) b[i] = t[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (key + i < p.Lk) b[i] = load_elem<FLASHBEV_F32>(row, key + i);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (key + i < p.Lk)
+                        b[i] = p.kind == FLASHLAYER_MASK_ADD + 16 ? load_elem<FLASHBEV_F16>(row, key + i)
+                                                                  : load_elem<FLASHBEV_BF16>(row, key + i);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * k + i] = __builtin_fmaf(x[4 * k + i], p.scale, b[i]);
+        }
+    }
+}
+
+// One place of a mask's row.
+__device__ __forceinline__ float mask_place(const Attend &p, float x, const char *row, int key)
+{
+    if (p.kind == FLASHLAYER_MASK_BOOL) return row[key] ? x * p.scale : -__builtin_inff();
+    const float b = p.kind == FLASHLAYER_MASK_ADD_F32  ? load_elem<FLASHBEV_F32>(row, key)
+                    : p.kind == FLASHLAYER_MASK_ADD + 16 ? load_elem<FLASHBEV_F16>(row, key)
+                                                         : load_elem<FLASHBEV_BF16>(row, key);
+    return __builtin_fmaf(x, p.scale, b);
+}
+
+// Scores of keys from `end` on leave a row.
+__device__ __forceinline__ void cut_keys(f32x16 &x, int key0, int h, int end)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (key0 + 8 * (i >> 2) + 4 * h + (i & 3) >= end) x[i] = -__builtin_inff();
+}
+
+// The other half's value of the lane's column joined with its own.
+__device__ __forceinline__ float both_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v),
+                                                    false, false);
+    const unsigned a = r[0], b = r[1];
+    return __builtin_fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
+__device__ __forceinline__ float both_sum(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v),
+                                                    false, false);
+    const unsigned a = r[0], b = r[1];
+    return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+}
+
+// ---------------------------------------------------------------------------
+// results: a block has row lane % 32 across and 32 channels down
+// ---------------------------------------------------------------------------
+// Channels d .. d + 7 of a row of D, and what their rounding took.
+template <int DT>
+__device__ __forceinline__ void put8(char *row, int d, int D, const float (&v)[8])
+{
+    if (d + 8 <= D) {
+        store_elems<DT>(row + d * elem_size(DT), v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (d + i < D) store_elem<DT>(row, d + i, v[i]);
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ float rounded(float v)
+{
+    if constexpr (DT == FLASHBEV_F16) {
+        return (float)(_Float16)v;
+    } else if constexpr (DT == FLASHBEV_BF16) {
+        return (float)(__bf16)v;
+    } else {
+        return v;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+constexpr int kCusOfCard = 256;
+
+inline int check_attention(const flashlayer_attention *a)
+{
+    if (!a) return FLASHBEV_ERR_NULLPTR;
+    if (a->B < 0 || a->Lq < 0 || a->Lk < 0 || a->H < 0 || a->Hk < 0 || a->D < 0) return FLASHBEV_ERR_SHAPE;
+    if (a->Hk ? a->H % a->Hk : a->H) return FLASHBEV_ERR_SHAPE;
+    for (const int64_t s : {a->q_batch, a->q_row, a->q_head, a->k_batch, a->k_row, a->k_head, a->v_batch, a->v_row,
+                            a->v_head, a->o_batch, a->o_row, a->o_head, a->mask_batch, a->mask_head, a->mask_row})
+        if (s < 0) return FLASHBEV_ERR_SHAPE;
+    if (!known_dtype(a->dtype)) return FLASHBEV_ERR_DTYPE;
+    if (a->mask < FLASHLAYER_MASK_NONE || a->mask > FLASHLAYER_MASK_ADD_F32) return FLASHBEV_ERR_VALUE;
+    if (!(a->scale > 0.0f) || !finite_value(a->scale)) return FLASHBEV_ERR_VALUE;
+    if (a->D > FLASHLAYER_HEAD_MAX) return FLASHBEV_ERR_UNSUPPORTED;
+    for (const int64_t s : {a->k_row, a->v_row})   // (a tile's rows lie within 32 bits)
+        if (s > FLASHBLOCK_LD_MAX) return FLASHBEV_ERR_UNSUPPORTED;
+    const uint64_t share = a->Hk ? a->H / a->Hk : 0;
+    // (rows by their share's reciprocal; places of the last tile within 31 bits)
+    if (size_prod({(uint64_t)a->Lq, share, share}) > 0xffffffffull ||
+        size_prod({(uint64_t)a->Lq, share}) > 0x7ffffe00ull || a->Lk > 0x7ffffe00)
+        return FLASHBEV_ERR_UNSUPPORTED;
+    return FLASHBEV_OK;
+}
+
+// Bytes from the first to the last element of a tensor [n0, n1, n2, D] by its strides;
+// kSizeOver past 2^62.
+inline uint64_t span4(int n0, int64_t s0, int n1, int64_t s1, int n2, int64_t s2, int D, int es)
+{
+    if (!n0 || !n1 || !n2 || !D) return 0;
+    uint64_t last = (uint64_t)D;
+    for (const auto &d : {std::pair<int, int64_t>{n0, s0}, {n1, s1}, {n2, s2}}) {
+        const uint64_t part = size_prod({(uint64_t)(d.first - 1), (uint64_t)d.second});
+        if (part > kSizeCap / 16) return kSizeOver;
+        last += part;
+    }
+    return last * es;
+}
+
+// Whether no two elements of such a tensor share a place (by each dimension clearing those of
+// smaller strides).
+inline bool apart(int n0, int64_t s0, int n1, int64_t s1, int n2, int64_t s2, int D)
+{
+    std::pair<int64_t, int> dims[3] = {{s0, n0}, {s1, n1}, {s2, n2}};
+    std::sort(dims, dims + 3);
+    uint64_t span = (uint64_t)D;
+    for (const auto &d : dims) {
+        if (d.second <= 1) continue;
+        if ((uint64_t)d.first < span) return false;
+        span += size_prod({(uint64_t)(d.second - 1), (uint64_t)d.first});
+    }
+    return true;
+}
+
+inline uint64_t align256(uint64_t v) { return (v + 255) & ~255ull; }
+
+inline int padded_head(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : 128; }
+
+inline Attend attend_of(const flashlayer_attention *a)
+{
+    Attend p{};
+    const int es = elem_size(a->dtype);
+    const int ms = a->mask == FLASHLAYER_MASK_BOOL ? 1 : a->mask == FLASHLAYER_MASK_ADD_F32 ? 4 : es;
+    p.qb = a->q_batch * es;
+    p.qr = a->q_row * es;
+    p.qh = a->q_head * es;
+    p.kb = a->k_batch * es;
+    p.kr = a->k_row * es;
+    p.kh = a->k_head * es;
+    p.vb = a->v_batch * es;
+    p.vr = a->v_row * es;
+    p.vh = a->v_head * es;
+    p.ob = a->o_batch * es;
+    p.orow = a->o_row * es;
+    p.oh = a->o_head * es;
+    p.mb = a->mask_batch * ms;
+    p.mh = a->mask_head * ms;
+    p.mr = a->mask_row * ms;
+    p.B = a->B;
+    p.Lq = a->Lq;
+    p.Lk = a->Lk;
+    p.H = a->H;
+    p.Hk = a->Hk;
+    p.D = a->D;
+    p.share = a->Hk ? a->H / a->Hk : 1;
+    p.rows = a->Lq * p.share;
+    p.share_inv = p.share > 1 ? (uint32_t)((0x100000000ull + p.share - 1) / p.share) : 0;
+    // additive masks of the inputs' type: float32 ones are one kind, float16 and bfloat16 two
+    p.kind = a->mask != FLASHLAYER_MASK_ADD      ? a->mask
+             : a->dtype == FLASHBEV_F32          ? FLASHLAYER_MASK_ADD_F32
+             : a->dtype == FLASHBEV_F16          ? FLASHLAYER_MASK_ADD + 16
+                                                 : FLASHLAYER_MASK_ADD + 32;
+    p.drops = a->mask == FLASHLAYER_MASK_BOOL && (a->mask_row == 0 || a->Lq == 1) && (a->mask_head == 0 || p.share == 1);
+    p.scale = a->scale;
+    return p;
+}
+
+// The grid's items, dealt to the XCDs.
+inline int deal(Attend &p, uint64_t items)
+{
+    if (items > 0x7fffffffull / 2) return FLASHBEV_ERR_UNSUPPORTED;
+    p.blocks = (uint32_t)items;
+    p.per_xcd = (uint32_t)((items + 7) / 8);
+    return FLASHBEV_OK;
+}
+
+template <class P>
+int launch_lds(const void *fn, uint64_t blocks, P &p, size_t lds, hipStream_t st)
+{
+    if (lds > 65536 && hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+        return FLASHBEV_ERR_HIP;
+    return launch_kernel(fn, blocks, 256, p, lds, st);
+}
+
+struct Bytes {
+    const void *p;
+    uint64_t n;
+};
+
+inline int check_overlaps(std::initializer_list<Bytes> outs, std::initializer_list<Bytes> ins)
+{
+    for (const Bytes *o = outs.begin(); o != outs.end(); ++o) {
+        if (o->n == kSizeOver) return FLASHBEV_ERR_UNSUPPORTED;
+        for (const Bytes &i : ins) {
+            if (i.n == kSizeOver) return FLASHBEV_ERR_UNSUPPORTED;
+            if (ranges_overlap(o->p, o->n, i.p, i.n)) return FLASHBEV_ERR_ALIAS;
+        }
+        for (const Bytes *q = outs.begin(); q != o; ++q)
+            if (ranges_overlap(o->p, o->n, q->p, q->n)) return FLASHBEV_ERR_ALIAS;
+    }
+    return FLASHBEV_OK;
+}
+
+inline int check_scratch(const void *ws, uint64_t bytes, uint64_t need)
+{
+    if (!need) return FLASHBEV_OK;
+    if (!ws) return FLASHBEV_ERR_NULLPTR;
+    if (misaligned(ws, 256)) return FLASHBEV_ERR_ALIGN;
+    return bytes < need ? FLASHBEV_ERR_SCRATCH : FLASHBEV_OK;
+}
+
+}  // namespace

@@ -1,0 +1,473 @@
+// Attention of queries to the states of an encoder of another length, for AMD MI355X (gfx950).
+// C ABI: include/block/flashlayer.h; what the backward shares: flashattend.h.
+//
+//   out = softmax(scale q k^T + mask) v
+//
+// One pass over the keys.  A row keeps a reference m of its scores, the sum l of exp(s - m) and
+// the sums of exp(s - m) v; when a score passes m by more than a few powers of two, all three
+// move to the new maximum.  Nothing of the scores is stored.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "flashattend.h"
+
+namespace {
+
+struct Forward : Attend {
+    char *rest;          // null: not wanted
+    float *stats;        // null: not wanted
+    float *part;         // splits > 1: [splits][B Hk rows][DP] sums, then [..][2] m and l
+    float *part_ml;
+};
+
+// How far a score may pass its row's reference before the reference moves, in powers of two:
+// exp(s - m) stays below 2^that, within float16's range with room for the backward's factors.
+template <int DT>
+constexpr float kSlack = DT == FLASHBEV_F16 ? 4.0f : 8.0f;
+
+// l and the weights' sums, of two packed weights: the sum takes them as the product with v does,
+// rounded, so that the result is a mean of v's rows with weights that add up to one.
+template <int DT>
+__device__ __forceinline__ float add_weights(float l, uint32_t two)
+{
+    if constexpr (DT == FLASHBEV_F16) {
+        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, two), h2{(_Float16)1.0f, (_Float16)1.0f}, l, false);
+    } else {
+        l += __builtin_bit_cast(float, two << 16);
+        return l + __builtin_bit_cast(float, two & 0xffff0000u);
+    }
+}
+
+// WQ = 4: a wavefront has 32 rows, the four of them share tiles of 64 keys.  WQ = 1: the
+// wavefronts share 32 rows and take 32 keys each of tiles of 128; their results are joined.
+template <int DT, int DP, int WQ>
+struct Shape {
+    static constexpr int BQ = 32 * WQ;
+    static constexpr int BK = WQ == 4 ? 64 : 128;
+    static constexpr int NB = WQ == 4 ? 2 : 1;         // blocks of 32 keys a wavefront has of a tile
+    static constexpr int STAGES = WQ == 4 ? 2 : 1;
+    using P = Panel<DT, DP, BK>;
+    static constexpr int STAGE = 2 * P::BYTES;
+    static constexpr int JOIN = WQ == 4 ? 0 : 2 * DP * 32 * 4 + 1024;
+    static constexpr int LDS = STAGES * STAGE > JOIN ? STAGES * STAGE : JOIN;
+};
+
+// MASK: with a mask (its code in kernels of its own: it takes registers).  Wide float32 heads
+// take one workgroup's registers of a CU.
+template <int DT, int DP, int WQ, bool MASK>
+__global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) attend(Forward p)
+{
+    using S = Shape<DT, DP, WQ>;
+    using P = typename S::P;
+    constexpr int ES = elem_size(DT), NB = S::NB, DB = DP / 32;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+
+    uint32_t id = item_of(p);
+    if (id >= p.blocks) return;
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int tile = 0, split, g, b;
+    if (p.tiles == 1) {   // heads next to each other, whose keys' rows share cache lines
+        g = id % p.Hk;
+        id /= p.Hk;
+        split = id % p.splits;
+        b = id / p.splits;
+    } else {
+        tile = id % p.tiles;
+        id /= p.tiles;
+        split = id % p.splits;
+        id /= p.splits;
+        g = id % p.Hk;
+        b = id / p.Hk;
+    }
+    const int len = p.keys(b);
+    const int all = (len + S::BK - 1) / S::BK, per = (all + p.splits - 1) / p.splits;
+    const int t0 = split * per, t1 = min(all, t0 + per);
+
+    const int r0 = tile * S::BQ + (WQ == 4 ? wave * 32 : 0), r = r0 + (lane & 31);
+    const bool row_there = r < p.rows;
+    int qi, qj;
+    p.row(min(r, p.rows - 1), qi, qj);
+    const int head = g * p.share + qj;
+    u32x4 qf[P::CHUNKS];
+    row_fragments<DT, DP>(qf, p.q + b * p.qb + qi * p.qr + head * p.qh, row_there, p.D, lane);
+    const char *mrow = p.mask + b * p.mb + head * p.mh + qi * p.mr;
+    const char *kbase = p.k + b * p.kb + g * p.kh, *vbase = p.v + b * p.vb + g * p.vh;
+    const bool odd = p.D % P::E != 0;
+    const float c = (MASK ? 1.0f : p.scale) * kLog2;   // of x, to powers of two
+
+    f32x16 o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = zeros16();
+    float m = -__builtin_inff(), l = 0.0f;
+
+    typename P::Reader read;
+    read.start(lane);
+    typename P::Mover km, vm;
+    km.start(tid, p.D, p.kr);
+    vm.start(tid, p.D, p.vr);
+    u32x4 kv[P::G], vv[P::G];
+    auto fetch = [&](int t) {
+        if (odd) return;
+        const int k0 = t * S::BK;
+        const char *kt = kbase + k0 * p.kr, *vt = vbase + k0 * p.vr;
+        if (MASK && p.drops) {   // (all rows' masks are the first one's)
+            const auto there = [&](int i) { return mrow[k0 + i] != 0; };
+            km.load(kv, kt, p.kr, len - k0, there);
+            vm.load(vv, vt, p.vr, len - k0, there);
+        } else {
+            const auto there = [](int) { return true; };
+            km.load(kv, kt, p.kr, len - k0, there);
+            vm.load(vv, vt, p.vr, len - k0, there);
+        }
+    };
+    auto put = [&](int t, char *lk, char *lv) {
+        if (!odd) {
+            km.store(kv, lk);
+            vm.store(vv, lv);
+            return;
+        }
+        const int k0 = t * S::BK;
+        const auto there = [&](int i) { return !MASK || !p.drops || mrow[k0 + i] != 0; };
+        km.copy(lk, kbase + k0 * p.kr, p.kr, len - k0, p.D, there);
+        vm.copy(lv, vbase + k0 * p.vr, p.vr, len - k0, p.D, there);
+    };
+    if (t0 < t1) fetch(t0);
+    for (int t = t0; t < t1; ++t) {
+        char *lk = lds + (S::STAGES > 1 ? (t - t0 & 1) * S::STAGE : 0), *lv = lk + P::BYTES;
+        if (S::STAGES == 1 && t > t0) __syncthreads();
+        put(t, lk, lv);
+        __syncthreads();
+        if (t + 1 < t1) fetch(t + 1);
+        if (WQ == 4 && r0 >= p.rows) continue;
+        const int b0 = WQ == 4 ? 0 : wave * 32;   // the wavefront's first key of the tile
+        const int k0 = t * S::BK + b0;
+        lk += b0 * P::STRIDE;
+        lv += b0 * P::STRIDE;
+        f32x16 x[NB];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            x[n] = zeros16();
+#pragma unroll
+            for (int e = 0; e < P::CHUNKS; ++e) mma<DT>(x[n], read.along(lk, n * 32, e), qf[e]);
+        }
+        if constexpr (MASK) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n) mask_row(p, x[n], mrow, k0 + n * 32, h);
+        }
+        if (k0 + NB * 32 > len) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n) cut_keys(x[n], k0 + n * 32, h, len);
+        }
+        float top = x[0][0];
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = __builtin_fmaxf(top, x[n][i]);
+        top = both_max(top);
+        if (__any((top - m) * c > kSlack<DT>)) {   // (-inf - -inf is no number, and not above)
+            const float to = __builtin_fmaxf(m, top);
+            const float f = to == -__builtin_inff() ? 1.0f : exp2_fast((m - to) * c);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        }
+        const float ref = m == -__builtin_inff() ? 0.0f : m;
+        if constexpr (MASK) {
+            // the difference first: x and m may be the type's lowest values, whose products
+            // with log2(e) are infinite
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[n][i] = exp2_fast((x[n][i] - ref) * c);
+        } else {
+            const float mc = ref * c;
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[n][i] = exp2_fast(__builtin_fmaf(x[n][i], c, -mc));
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int u = 0; u < P::STEPS; ++u) {
+                const u32x4 w = operand<DT>(x[n], u);
+                if constexpr (DT == FLASHBEV_F32) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) l += x[n][4 * u + i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) l = add_weights<DT>(l, w[i]);
+                }
+#pragma unroll
+                for (int d = 0; d < DB; ++d) mma<DT>(o[d], read.across(lv, n * 32, u, d * 32), w);
+            }
+    }
+    l = both_sum(l);
+
+    if constexpr (WQ == 1) {
+        // the wavefronts' results, at the largest of their references
+        float *ml = reinterpret_cast<float *>(lds), *area = ml + 256;
+        __syncthreads();
+        if (lane < 32) {
+            ml[wave * 32 + lane] = m;
+            ml[128 + wave * 32 + lane] = l;
+        }
+        __syncthreads();
+        float to = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) to = __builtin_fmaxf(to, ml[w * 32 + (lane & 31)]);
+        const auto factor = [&](float from) {
+            return from == -__builtin_inff() ? 0.0f : exp2_fast((from - to) * c);
+        };
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            sum += ml[128 + w * 32 + (lane & 31)] * factor(ml[w * 32 + (lane & 31)]);
+        const float f = factor(m);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        m = to;
+        l = sum;
+#pragma unroll
+        for (int half = 2; half > 0; half /= 2) {
+            if (wave >= half && wave < 2 * half) {
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        area[(((wave - half) * DB + d) * 16 + i) * 64 + lane] = o[d][i];
+            }
+            __syncthreads();
+            if (wave < half) {
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] += area[((wave * DB + d) * 16 + i) * 64 + lane];
+            }
+            __syncthreads();
+        }
+        if (wave) return;
+    }
+    if (!row_there) return;   // (both halves of a row)
+
+    if (p.splits > 1) {
+        const int64_t at = ((int64_t)split * p.B * p.Hk + (int64_t)b * p.Hk + g) * p.rows + r;
+        float *part = p.part + at * DP;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                float v[8];
+                columns_of(o[d], q, v);
+                store_elems<FLASHBEV_F32>(part + d * 32 + 16 * q + 8 * h, v);
+            }
+        if (!h) {
+            p.part_ml[2 * at] = m;
+            p.part_ml[2 * at + 1] = l;
+        }
+        return;
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // (a row that sees nothing)
+    char *out = p.o + b * p.ob + qi * p.orow + head * p.oh;
+    char *rest = p.rest ? p.rest + (((int64_t)b * p.Lq + qi) * p.H + head) * p.D * ES : nullptr;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            float v[8];
+            columns_of(o[d], q, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= inv;
+            put8<DT>(out, d * 32 + 16 * q + 8 * h, p.D, v);
+            if (rest) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] -= rounded<DT>(v[i]);
+                put8<DT>(rest, d * 32 + 16 * q + 8 * h, p.D, v);
+            }
+        }
+    if (p.stats && !h) {
+        float *st = p.stats + (((int64_t)b * p.H + head) * p.Lq + qi) * 2;
+        st[0] = MASK ? m : m * p.scale;
+        st[1] = l == 0.0f ? 0.0f : log2_fast(l) * kLn2;
+    }
+}
+
+// The splits' results: four channels of a row to a lane.
+template <int DT, int DP>
+__global__ void __launch_bounds__(256) attend_join(Forward p)
+{
+    constexpr int ES = elem_size(DT), LANES = DP / 4;
+    const int64_t n = (int64_t)p.B * p.Hk * p.rows;
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
+    const int d = (int)(((int64_t)blockIdx.x * 256 + threadIdx.x) % LANES) * 4;
+    if (at >= n) return;
+    const float c = (p.kind ? 1.0f : p.scale) * kLog2;
+    float m = -__builtin_inff(), l = 0.0f;
+    for (int s = 0; s < p.splits; ++s) m = __builtin_fmaxf(m, p.part_ml[2 * (s * n + at)]);
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < p.splits; ++s) {
+        const float from = p.part_ml[2 * (s * n + at)];
+        if (from == -__builtin_inff()) continue;
+        const float f = exp2_fast((from - m) * c);
+        l = __builtin_fmaf(p.part_ml[2 * (s * n + at) + 1], f, l);
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(p.part + (s * n + at) * DP + d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(v[i], f, sum[i]);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int64_t problem = at / p.rows;
+    const int b = problem / p.Hk, g = problem - (int64_t)b * p.Hk;
+    int qi, qj;
+    p.row((int)(at - problem * p.rows), qi, qj);
+    const int head = g * p.share + qj;
+    char *out = p.o + b * p.ob + qi * p.orow + head * p.oh;
+    char *rest = p.rest ? p.rest + (((int64_t)b * p.Lq + qi) * p.H + head) * p.D * ES : nullptr;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (d + i >= p.D) break;
+        const float v = sum[i] * inv;
+        store_elem<DT>(out, d + i, v);
+        if (rest) store_elem<DT>(rest, d + i, v - rounded<DT>(v));
+    }
+    if (p.stats && d == 0) {
+        float *st = p.stats + (((int64_t)b * p.H + head) * p.Lq + qi) * 2;
+        st[0] = p.kind ? m : m * p.scale;
+        st[1] = l == 0.0f ? 0.0f : log2_fast(l) * kLn2;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+struct Plan {
+    int wq, tiles, splits, dp;
+};
+
+// A call's shape.  Up to 32 rows: the wavefronts of a workgroup go over the keys in turn.  Where
+// that leaves fewer than two workgroups a CU the keys are split, for about three of them, at two tiles
+// each or more.
+Plan plan_of(const flashlayer_attention *a)
+{
+    Plan p{};
+    const int64_t rows = (int64_t)a->Lq * (a->Hk ? a->H / a->Hk : 1);
+    p.dp = padded_head(a->D);
+    p.wq = rows <= 32 ? 1 : 4;
+    const int bq = 32 * p.wq, bk = p.wq == 4 ? 64 : 128;
+    p.tiles = (int)((rows + bq - 1) / bq);
+    const int64_t base = (int64_t)a->B * a->Hk * p.tiles, keys = (a->Lk + bk - 1) / bk;
+    p.splits = 1;
+    if (base > 0 && base < 2 * kCusOfCard) {
+        const int64_t want = (3 * kCusOfCard + base - 1) / base;
+        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(want, keys / 2));
+    }
+    return p;
+}
+
+uint64_t part_bytes(const flashlayer_attention *a, const Plan &p)
+{
+    const uint64_t rows = (uint64_t)a->B * a->Lq * a->H;
+    return align256(size_prod({(uint64_t)p.splits, rows, (uint64_t)p.dp, 4}));
+}
+
+uint64_t forward_bytes(const flashlayer_attention *a)
+{
+    const Plan p = plan_of(a);
+    if (p.splits <= 1) return 0;
+    return part_bytes(a, p) + align256((uint64_t)p.splits * a->B * a->Lq * a->H * 8);
+}
+
+template <int DT, int DP>
+int run(Forward &p, const Plan &plan, hipStream_t st)
+{
+    const void *fn = plan.wq == 4 ? p.kind ? (const void *)attend<DT, DP, 4, true> : (const void *)attend<DT, DP, 4, false>
+                     : p.kind     ? (const void *)attend<DT, DP, 1, true>
+                                  : (const void *)attend<DT, DP, 1, false>;
+    const size_t lds = plan.wq == 4 ? Shape<DT, DP, 4>::LDS : Shape<DT, DP, 1>::LDS;
+    if (const int rc = launch_lds(fn, 8ull * p.per_xcd, p, lds, st)) return rc;
+    if (p.splits <= 1) return FLASHBEV_OK;
+    const uint64_t lanes = (uint64_t)p.B * p.Hk * p.rows * (DP / 4);
+    return launch_kernel((const void *)attend_join<DT, DP>, (lanes + 255) / 256, 256, p, 0, st);
+}
+
+template <int DT>
+int run_width(Forward &p, const Plan &plan, hipStream_t st)
+{
+    switch (plan.dp) {
+    case 32: return run<DT, 32>(p, plan, st);
+    case 64: return run<DT, 64>(p, plan, st);
+    case 96: return run<DT, 96>(p, plan, st);
+    default: return run<DT, 128>(p, plan, st);
+    }
+}
+
+}  // namespace
+
+extern "C" int flashlayer_attention_workspace_size(const flashlayer_attention *args, uint64_t *bytes)
+{
+    if (!bytes) return FLASHBEV_ERR_NULLPTR;
+    if (const int rc = check_attention(args)) return rc;
+    *bytes = forward_bytes(args);
+    return FLASHBEV_OK;
+}
+
+extern "C" int flashlayer_attention_forward(const flashlayer_attention *args, const void *q, const void *k,
+                                            const void *v, const void *mask, const int32_t *key_lengths,
+                                            void *out, void *rest, float *stats, void *workspace,
+                                            uint64_t workspace_bytes, void *stream)
+{
+    if (const int rc = check_attention(args)) return rc;
+    const flashlayer_attention &a = *args;
+    const int es = elem_size(a.dtype);
+    if (!a.B || !a.Lq || !a.H) return FLASHBEV_OK;
+    if (!a.D) return a.D || !stats ? FLASHBEV_OK : FLASHBEV_ERR_UNSUPPORTED;
+    if (!q || !out || (a.Lk && (!k || !v))) return FLASHBEV_ERR_NULLPTR;
+    if (a.mask && a.Lk && !mask) return FLASHBEV_ERR_NULLPTR;
+    if (!apart(a.B, a.o_batch, a.Lq, a.o_row, a.H, a.o_head, a.D)) return FLASHBEV_ERR_SHAPE;
+    const int ms = a.mask == FLASHLAYER_MASK_BOOL ? 1 : a.mask == FLASHLAYER_MASK_ADD_F32 ? 4 : es;
+    if (misaligned(q, es) || misaligned(k, es) || misaligned(v, es) || misaligned(out, es) || misaligned(rest, es) ||
+        misaligned(stats, 4) || misaligned(key_lengths, 4) || (a.mask && misaligned(mask, ms)))
+        return FLASHBEV_ERR_ALIGN;
+    const uint64_t need = forward_bytes(args);
+    if (const int rc = check_scratch(workspace, workspace_bytes, need)) return rc;
+    const uint64_t dense = (uint64_t)a.B * a.Lq * a.H * a.D * es;
+    if (const int rc = check_overlaps(
+            {{out, span4(a.B, a.o_batch, a.Lq, a.o_row, a.H, a.o_head, a.D, es)},
+             {rest, dense},
+             {stats, (uint64_t)a.B * a.H * a.Lq * 8},
+             {workspace, need}},
+            {{q, span4(a.B, a.q_batch, a.Lq, a.q_row, a.H, a.q_head, a.D, es)},
+             {k, span4(a.B, a.k_batch, a.Lk, a.k_row, a.Hk, a.k_head, a.D, es)},
+             {v, span4(a.B, a.v_batch, a.Lk, a.v_row, a.Hk, a.v_head, a.D, es)},
+             {a.mask ? mask : nullptr, span4(a.B, a.mask_batch, a.H, a.mask_head, a.Lq, a.mask_row, a.Lk, ms)},
+             {key_lengths, (uint64_t)a.B * 4}}))
+        return rc;
+    const Plan plan = plan_of(args);
+    Forward p{};
+    static_cast<Attend &>(p) = attend_of(args);
+    p.q = static_cast<const char *>(q);
+    p.k = static_cast<const char *>(k);
+    p.v = static_cast<const char *>(v);
+    p.mask = static_cast<const char *>(mask);
+    p.lengths = key_lengths;
+    p.o = static_cast<char *>(out);
+    p.rest = static_cast<char *>(rest);
+    p.stats = stats;
+    p.tiles = plan.tiles;
+    p.splits = plan.splits;
+    if (p.splits > 1) {
+        p.part = static_cast<float *>(workspace);
+        p.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + part_bytes(args, plan));
+    }
+    if (const int rc = deal(p, size_prod({(uint64_t)a.B, (uint64_t)a.Hk, (uint64_t)plan.tiles, (uint64_t)plan.splits})))
+        return rc;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (a.dtype == FLASHBEV_F32) return run_width<FLASHBEV_F32>(p, plan, st);
+    return a.dtype == FLASHBEV_F16 ? run_width<FLASHBEV_F16>(p, plan, st) : run_width<FLASHBEV_BF16>(p, plan, st);
+}

@@ -1,0 +1,668 @@
+// The gradients of attention, for AMD MI355X (gfx950).  C ABI: include/block/flashlayer.h; what
+// the forward shares: flashattend.h.
+//
+// With p = exp(s - m) / l of the stored row statistics and dS = p (g v^T - delta),
+// delta = g . out (g the output's gradient),
+//
+//   grad_q = scale dS k,   grad_k = scale dS^T q,   grad_v = p^T g
+//
+// Two kernels form the scores again, seven products in all: one with rows across sums grad_q
+// over the keys, one with keys across sums grad_k and grad_v over the rows.  Five products
+// in one kernel would leave grad_q to float atomics, whose order changes results.
+//
+// Digits.  p and dS are rounded to the inputs' type for their products.  bfloat16 has float32's
+// range; float16 loses digits below 6e-5, where weights of one in 40000 and scaled losses'
+// gradients lie, so its factors are kept near one: grad_q's kernel takes p l (at most 2^4) and
+// g / |g|, a row's factors coming back at the end; the other one takes p and dS times powers of
+// two that bring the largest 1 / l and |g| / l of its rows to about one.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "flashattend.h"
+
+namespace {
+
+// A row as the two kernels read it.
+struct RowData {
+    float m;       // its scores' reference; 0 for an empty row
+    float log2l;   // of the sum of exp(s - m); infinite for an empty row, whose weights are then 0
+    float delta;   // g . out
+    float norm;    // |g|
+};
+
+// an exponent whose power is a normal float32
+__device__ __forceinline__ float within_range(float e)
+{
+    return __builtin_fminf(__builtin_fmaxf(e, -100.0f), 100.0f);
+}
+
+struct Backward : Attend {
+    const char *out, *rest;   // [B, Lq, H, D]; rest null: none
+    const float *stats;
+    RowData *data;            // [B Hk][rows]
+    float *largest;           // [B Hk][ceil(rows / 64)][2]: the largest 1 / l and |g| / l of 64 rows
+    char *gq, *gk, *gv;       // contiguous; null: not wanted
+    float *part;              // splits > 1: grad_q's [splits][B Hk rows][DP] or
+                              // grad_k's and grad_v's [2][splits][B Hk Lk][DP]
+    int row_tiles;            // of 64
+};
+
+constexpr int kRowTile = 64;
+
+// delta and |g| of a tile of 64 rows, 16 lanes to a row.
+template <int DT>
+__global__ void __launch_bounds__(256) attend_rows(Backward p)
+{
+    constexpr int ES = elem_size(DT), E = 16 / ES;
+    __shared__ float lds[2][4];
+    const int tile = blockIdx.x % p.row_tiles, problem = blockIdx.x / p.row_tiles;
+    const int b = problem / p.Hk, g = problem - b * p.Hk;
+    const int part = threadIdx.x & 15;
+    float most_l = 0.0f, most_g = 0.0f;
+    for (int k = 0; k < 4; ++k) {
+        const int r = tile * kRowTile + k * 16 + (threadIdx.x >> 4);
+        if (r >= p.rows) break;   // (whole groups of 16 lanes)
+        int qi, qj;
+        p.row(r, qi, qj);
+        const int head = g * p.share + qj;
+        const char *gr = p.g + b * p.ob + qi * p.orow + head * p.oh;
+        const int64_t at = (((int64_t)b * p.Lq + qi) * p.H + head) * p.D;
+        float delta = 0.0f, sq = 0.0f;
+        for (int d = part * E; d < p.D; d += 16 * E) {
+            float vg[E], vo[E], vr[E];
+            u32x4 w[1] = {load_granule_edge<DT>(gr, d, p.D)};
+            elems_of<DT>(w, vg);
+            w[0] = load_granule_edge<DT>(p.out + at * ES, d, p.D);
+            elems_of<DT>(w, vo);
+            if (p.rest) {
+                w[0] = load_granule_edge<DT>(p.rest + at * ES, d, p.D);
+                elems_of<DT>(w, vr);
+            }
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                delta = __builtin_fmaf(vg[i], vo[i], delta);
+                if (p.rest) delta = __builtin_fmaf(vg[i], vr[i], delta);
+                sq = __builtin_fmaf(vg[i], vg[i], sq);
+            }
+        }
+#pragma unroll
+        for (int o = 1; o < 16; o *= 2) {
+            delta += __shfl_xor(delta, o);
+            sq += __shfl_xor(sq, o);
+        }
+        const float *st = p.stats + (((int64_t)b * p.H + head) * p.Lq + qi) * 2;
+        RowData row;
+        row.m = st[0];
+        row.log2l = st[1] * kLog2;
+        row.delta = delta;
+        row.norm = sqrtf(sq);
+        if (row.m == -__builtin_inff()) {
+            row.m = 0.0f;
+            row.log2l = __builtin_inff();
+            row.delta = 0.0f;
+        } else {
+            const float inv = exp2_fast(-row.log2l);
+            most_l = __builtin_fmaxf(most_l, inv);
+            most_g = __builtin_fmaxf(most_g, row.norm * inv);
+        }
+        if (part == 0) p.data[(int64_t)problem * p.rows + r] = row;
+    }
+#pragma unroll
+    for (int o = 16; o < 64; o *= 2) {
+        most_l = __builtin_fmaxf(most_l, __shfl_xor(most_l, o));
+        most_g = __builtin_fmaxf(most_g, __shfl_xor(most_g, o));
+    }
+    if ((threadIdx.x & 63) == 0) {
+        lds[0][threadIdx.x >> 6] = most_l;
+        lds[1][threadIdx.x >> 6] = most_g;
+    }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        float v = lds[threadIdx.x][0];
+        for (int w = 1; w < 4; ++w) v = __builtin_fmaxf(v, lds[threadIdx.x][w]);
+        p.largest[2 * (int64_t)blockIdx.x + threadIdx.x] = v;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// grad_q: 32 rows across to a wavefront, tiles of 64 keys
+// ---------------------------------------------------------------------------
+template <int DT, int DP>
+struct ShapeQ {
+    static constexpr int BQ = 128, BK = 64;
+    using P = Panel<DT, DP, BK>;
+    static constexpr int STAGE = 2 * P::BYTES, LDS = 2 * STAGE;
+};
+
+template <int DT, int DP, bool MASK>
+__global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_grad_q(Backward p)
+{
+    using S = ShapeQ<DT, DP>;
+    using P = typename S::P;
+    constexpr int ES = elem_size(DT), DB = DP / 32;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+
+    uint32_t id = item_of(p);
+    if (id >= p.blocks) return;
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tile = id % p.tiles;
+    id /= p.tiles;
+    const int split = id % p.splits;
+    id /= p.splits;
+    const int g = id % p.Hk, b = id / p.Hk;
+    const int len = p.keys(b);
+    const int all = (len + S::BK - 1) / S::BK, per = (all + p.splits - 1) / p.splits;
+    const int t0 = split * per, t1 = min(all, t0 + per);
+
+    const int r0 = tile * S::BQ + wave * 32, r = r0 + (lane & 31);
+    const bool row_there = r < p.rows;
+    int qi, qj;
+    p.row(min(r, p.rows - 1), qi, qj);
+    const int head = g * p.share + qj;
+    u32x4 qf[P::CHUNKS], gf[P::CHUNKS];
+    row_fragments<DT, DP>(qf, p.q + b * p.qb + qi * p.qr + head * p.qh, row_there, p.D, lane);
+    row_fragments<DT, DP>(gf, p.g + b * p.ob + qi * p.orow + head * p.oh, row_there, p.D, lane);
+    const char *mrow = p.mask + b * p.mb + head * p.mh + qi * p.mr;
+    const RowData row = p.data[((int64_t)b * p.Hk + g) * p.rows + min(r, p.rows - 1)];
+    const float c = (MASK ? 1.0f : p.scale) * kLog2;
+    // weights are p l; an empty row's are exp(-inf - 0) = 0
+    const float mc = row.m * kLog2;
+    const float inv = row.norm > 0.0f ? 1.0f / row.norm : 1.0f, off = -row.delta * inv;
+    const char *kbase = p.k + b * p.kb + g * p.kh, *vbase = p.v + b * p.vb + g * p.vh;
+    const bool odd = p.D % P::E != 0;
+
+    f32x16 o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = zeros16();
+
+    typename P::Reader read;
+    read.start(lane);
+    typename P::Mover km, vm;
+    km.start(tid, p.D, p.kr);
+    vm.start(tid, p.D, p.vr);
+    u32x4 kv[P::G], vv[P::G];
+    auto fetch = [&](int t) {
+        if (odd) return;
+        const int k0 = t * S::BK;
+        const char *kt = kbase + k0 * p.kr, *vt = vbase + k0 * p.vr;
+        if (MASK && p.drops) {
+            const auto there = [&](int i) { return mrow[k0 + i] != 0; };
+            km.load(kv, kt, p.kr, len - k0, there);
+            vm.load(vv, vt, p.vr, len - k0, there);
+        } else {
+            const auto there = [](int) { return true; };
+            km.load(kv, kt, p.kr, len - k0, there);
+            vm.load(vv, vt, p.vr, len - k0, there);
+        }
+    };
+    auto put = [&](int t, char *lk, char *lv) {
+        if (!odd) {
+            km.store(kv, lk);
+            vm.store(vv, lv);
+            return;
+        }
+        const int k0 = t * S::BK;
+        const auto there = [&](int i) { return !MASK || !p.drops || mrow[k0 + i] != 0; };
+        km.copy(lk, kbase + k0 * p.kr, p.kr, len - k0, p.D, there);
+        vm.copy(lv, vbase + k0 * p.vr, p.vr, len - k0, p.D, there);
+    };
+    if (t0 < t1) fetch(t0);
+    for (int t = t0; t < t1; ++t) {
+        char *lk = lds + (t - t0 & 1) * S::STAGE, *lv = lk + P::BYTES;
+        put(t, lk, lv);
+        __syncthreads();
+        if (t + 1 < t1) fetch(t + 1);
+        if (r0 >= p.rows) continue;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int k0 = t * S::BK + n * 32;
+            f32x16 x = zeros16(), y = zeros16();
+#pragma unroll
+            for (int e = 0; e < P::CHUNKS; ++e) {
+                mma<DT>(x, read.along(lk, n * 32, e), qf[e]);
+                mma<DT>(y, read.along(lv, n * 32, e), gf[e]);
+            }
+            if constexpr (MASK) mask_row(p, x, mrow, k0, h);
+            if (k0 + 32 > len) cut_keys(x, k0, h, len);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float w = MASK ? exp2_fast((x[i] - row.m) * c) : exp2_fast(__builtin_fmaf(x[i], c, -mc));
+                x[i] = w * __builtin_fmaf(y[i], inv, off);
+            }
+#pragma unroll
+            for (int u = 0; u < P::STEPS; ++u) {
+                const u32x4 w = operand<DT>(x, u);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) mma<DT>(o[d], read.across(lk, n * 32, u, d * 32), w);
+            }
+        }
+    }
+    if (!row_there) return;
+    const float back = p.scale * exp2_fast(-row.log2l) / inv;
+    const int64_t at = ((int64_t)b * p.Lq + qi) * p.H + head;
+    const int64_t slot = ((int64_t)split * p.B * p.Lq * p.H + at) * DP;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            float v[8];
+            columns_of(o[d], q, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= back;
+            if (p.splits > 1) {
+                store_elems<FLASHBEV_F32>(p.part + slot + d * 32 + 16 * q + 8 * h, v);
+            } else {
+                put8<DT>(p.gq + at * p.D * ES, d * 32 + 16 * q + 8 * h, p.D, v);
+            }
+        }
+}
+
+// ---------------------------------------------------------------------------
+// grad_k and grad_v: 32 keys across to a wavefront, tiles of rows
+// ---------------------------------------------------------------------------
+template <int DT, int DP>
+struct ShapeK {
+    static constexpr int BK = 128;
+    static constexpr int BR = DP * elem_size(DT) > 128 ? 32 : 64;
+    using P = Panel<DT, DP, BR>;
+    static constexpr int DATA = BR * 24;   // a row's mask (8 bytes), reference, exponent, delta
+    static constexpr int STAGE = 2 * P::BYTES + DATA, LDS = 2 * STAGE;
+};
+
+template <int DT, int DP, bool MASK>
+__global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_grad_kv(Backward p)
+{
+    using S = ShapeK<DT, DP>;
+    using P = typename S::P;
+    constexpr int ES = elem_size(DT), DB = DP / 32;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float shared[2][4];
+
+    uint32_t id = item_of(p);
+    if (id >= p.blocks) return;
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tile = id % p.tiles;
+    id /= p.tiles;
+    const int split = id % p.splits;
+    id /= p.splits;
+    const int g = id % p.Hk, b = id / p.Hk;
+    const int64_t problem = (int64_t)b * p.Hk + g;
+    const int len = p.keys(b);
+    const int k0 = tile * S::BK + wave * 32, key = k0 + (lane & 31);
+    const char *mbase = p.mask + b * p.mb + (int64_t)g * p.share * p.mh;
+    const bool key_there = key < len && !(MASK && p.drops && mbase[key] == 0);
+
+    const int all = tile * S::BK < len ? (p.rows + S::BR - 1) / S::BR : 0;
+    const int per = (all + p.splits - 1) / p.splits;
+    const int t0 = split * per, t1 = min(all, t0 + per);
+
+    // the factors of p and dS: 2^up and 2^up times `more`
+    float up = 0.0f, more = 1.0f;
+    if constexpr (DT == FLASHBEV_F16) {
+        float most_l = 0.0f, most_g = 0.0f;
+        const float *at = p.largest + problem * p.row_tiles * 2;
+        const int s0 = t0 * S::BR / kRowTile, s1 = min(p.row_tiles, (t1 * S::BR + kRowTile - 1) / kRowTile);
+        for (int s = s0 + tid; s < s1; s += 256) {
+            most_l = __builtin_fmaxf(most_l, at[2 * s]);
+            most_g = __builtin_fmaxf(most_g, at[2 * s + 1]);
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            most_l = __builtin_fmaxf(most_l, __shfl_xor(most_l, o));
+            most_g = __builtin_fmaxf(most_g, __shfl_xor(most_g, o));
+        }
+        if (lane == 0) {
+            shared[0][wave] = most_l;
+            shared[1][wave] = most_g;
+        }
+        __syncthreads();
+        most_l = __builtin_fmaxf(__builtin_fmaxf(shared[0][0], shared[0][1]), __builtin_fmaxf(shared[0][2], shared[0][3]));
+        most_g = __builtin_fmaxf(__builtin_fmaxf(shared[1][0], shared[1][1]), __builtin_fmaxf(shared[1][2], shared[1][3]));
+        // weights reach 2^4 times 1 / l and g v^T - delta 2 |g| |v|: an eighth of one leaves |v|
+        // up to 16000
+        up = most_l > 0.0f ? -__builtin_ceilf(log2_fast(most_l)) : 0.0f;
+        const float down = most_g > 0.0f && most_g < __builtin_inff() ? -__builtin_ceilf(log2_fast(most_g)) - 3.0f : 0.0f;
+        more = exp2_fast(within_range(down - up));
+    }
+
+    u32x4 kf[P::CHUNKS], vf[P::CHUNKS];
+    const int64_t key_at = min(key, p.Lk - 1);
+    row_fragments<DT, DP>(kf, p.k + b * p.kb + g * p.kh + key_at * p.kr, key_there, p.D, lane);
+    row_fragments<DT, DP>(vf, p.v + b * p.vb + g * p.vh + key_at * p.vr, key_there, p.D, lane);
+    const float c = (MASK ? 1.0f : p.scale) * kLog2;
+    const bool odd = p.D % P::E != 0;
+
+    f32x16 ok[DB], ov[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) ok[d] = ov[d] = zeros16();
+
+    typename P::Reader read;
+    read.start(lane);
+    // rows on their way: query r / share of head r % share, so each thread's rows one by one
+    const int my_row = tid / P::GR, my_g = tid - my_row * P::GR;
+    const char *qbase = p.q + b * p.qb + (int64_t)g * p.share * p.qh;
+    const char *gbase = p.g + b * p.ob + (int64_t)g * p.share * p.oh;
+    u32x4 qv[P::G], gv[P::G];
+    RowData rd{};
+    auto fetch = [&](int t) {
+        const int r0 = t * S::BR;
+        if (tid < S::BR && r0 + tid < p.rows) rd = p.data[problem * p.rows + r0 + tid];
+        if (odd) return;
+#pragma unroll
+        for (int i = 0; i < P::G; ++i) {
+            qv[i] = gv[i] = u32x4{0, 0, 0, 0};
+            const int r = r0 + my_row + i * P::RP;
+            if (my_row < P::RP && my_g * P::E < p.D && r < p.rows && my_row + i * P::RP < S::BR) {
+                int qi, qj;
+                p.row(r, qi, qj);
+                qv[i] = load16(qbase + qi * p.qr + qj * p.qh + my_g * 16);
+                gv[i] = load16(gbase + qi * p.orow + qj * p.oh + my_g * 16);
+            }
+        }
+    };
+    auto put = [&](int t, char *lq, char *lg, char *ld) {
+        const int r0 = t * S::BR;
+        if (tid < S::BR) {
+            const bool there = r0 + tid < p.rows;
+            int qi, qj;
+            p.row(there ? r0 + tid : 0, qi, qj);
+            reinterpret_cast<int64_t *>(ld)[tid] = qi * p.mr + qj * p.mh;
+            float *f = reinterpret_cast<float *>(ld + 8 * S::BR);
+            // rows past the last one weigh 2^-inf
+            const float e = there ? rd.log2l - up : __builtin_inff();
+            f[tid] = there ? rd.m : 0.0f;
+            f[S::BR + tid] = MASK || !there ? e : __builtin_fmaf(rd.m, kLog2, e);
+            f[2 * S::BR + tid] = there ? rd.delta * more : 0.0f;
+        }
+        if (my_row >= P::RP) return;
+        if (!odd) {
+#pragma unroll
+            for (int i = 0; i < P::G; ++i)
+                if (S::BR % P::RP == 0 || my_row + i * P::RP < S::BR) {
+                    *reinterpret_cast<u32x4 *>(lq + P::place(my_row + i * P::RP, my_g)) = qv[i];
+                    *reinterpret_cast<u32x4 *>(lg + P::place(my_row + i * P::RP, my_g)) = gv[i];
+                }
+            return;
+        }
+#pragma unroll 1
+        for (int i = my_row; i < S::BR; i += P::RP) {
+            u32x4 a = {0, 0, 0, 0}, w = {0, 0, 0, 0};
+            if (r0 + i < p.rows) {
+                int qi, qj;
+                p.row(r0 + i, qi, qj);
+                a = P::granule(qbase + qi * p.qr + qj * p.qh, my_g, p.D);
+                w = P::granule(gbase + qi * p.orow + qj * p.oh, my_g, p.D);
+            }
+            *reinterpret_cast<u32x4 *>(lq + P::place(i, my_g)) = a;
+            *reinterpret_cast<u32x4 *>(lg + P::place(i, my_g)) = w;
+        }
+    };
+    if (t0 < t1) fetch(t0);
+    for (int t = t0; t < t1; ++t) {
+        char *lq = lds + (t - t0 & 1) * S::STAGE, *lg = lq + P::BYTES, *ld = lg + P::BYTES;
+        put(t, lq, lg, ld);
+        __syncthreads();
+        if (t + 1 < t1) fetch(t + 1);
+        if (k0 >= len) continue;
+#pragma unroll
+        for (int n = 0; n < S::BR / 32; ++n) {
+            f32x16 x = zeros16(), y = zeros16();
+#pragma unroll
+            for (int e = 0; e < P::CHUNKS; ++e) {
+                mma<DT>(x, read.along(lq, n * 32, e), kf[e]);
+                mma<DT>(y, read.along(lg, n * 32, e), vf[e]);
+            }
+            const float *f = reinterpret_cast<const float *>(ld + 8 * S::BR) + n * 32 + 4 * h;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const f32x4 e4 = *reinterpret_cast<const f32x4 *>(f + S::BR + 8 * k);
+                const f32x4 d4 = *reinterpret_cast<const f32x4 *>(f + 2 * S::BR + 8 * k);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float s = x[4 * k + i];
+                    if constexpr (MASK) {
+                        const int64_t mo = reinterpret_cast<const int64_t *>(ld)[n * 32 + 8 * k + 4 * h + i];
+                        s = key_there ? mask_place(p, s, mbase + mo, key) : -__builtin_inff();
+                        s = exp2_fast(__builtin_fmaf(s - f[8 * k + i], c, -e4[i]));
+                    } else {
+                        s = exp2_fast(__builtin_fmaf(s, c, -e4[i]));
+                    }
+                    x[4 * k + i] = s;
+                    y[4 * k + i] = s * __builtin_fmaf(y[4 * k + i], more, -d4[i]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < P::STEPS; ++u) {
+                const u32x4 wp = operand<DT>(x, u), ws = operand<DT>(y, u);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    mma<DT>(ov[d], read.across(lg, n * 32, u, d * 32), wp);
+                    mma<DT>(ok[d], read.across(lq, n * 32, u, d * 32), ws);
+                }
+            }
+        }
+    }
+    if (key >= p.Lk) return;
+    const float back_v = exp2_fast(-up), back_k = back_v * p.scale / more;
+    const int64_t at = ((int64_t)b * p.Lk + key) * p.Hk + g, all_keys = (int64_t)p.B * p.Lk * p.Hk;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            float a[8], w[8];
+            columns_of(ok[d], q, a);
+            columns_of(ov[d], q, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {   // (a key that is left out has sums of no meaning)
+                a[i] = key_there ? a[i] * back_k : 0.0f;
+                w[i] = key_there ? w[i] * back_v : 0.0f;
+            }
+            const int ch = d * 32 + 16 * q + 8 * h;
+            if (p.splits > 1) {
+                store_elems<FLASHBEV_F32>(p.part + (split * all_keys + at) * DP + ch, a);
+                store_elems<FLASHBEV_F32>(p.part + ((p.splits + split) * all_keys + at) * DP + ch, w);
+            } else {
+                put8<DT>(p.gk + at * p.D * ES, ch, p.D, a);
+                put8<DT>(p.gv + at * p.D * ES, ch, p.D, w);
+            }
+        }
+}
+
+// The sums of the splits' rows [n][DP], four channels to a lane.
+struct Sum {
+    const float *part;
+    char *out;
+    int64_t n;
+    int splits, D;
+};
+
+template <int DT, int DP>
+__global__ void __launch_bounds__(256) attend_sum(Sum p)
+{
+    constexpr int LANES = DP / 4;
+    const int64_t t = (int64_t)block_index() * 256 + threadIdx.x, at = t / LANES;
+    const int d = (int)(t - at * LANES) * 4;
+    if (at >= p.n || d >= p.D) return;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int s = 0; s < p.splits; ++s) {
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(p.part + (s * p.n + at) * DP + d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += v[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (d + i < p.D) store_elem<DT>(p.out, at * p.D + d + i, sum[i]);
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+struct Plan {
+    int dp, row_tiles;
+    int q_tiles, q_splits;
+    int k_tiles, k_splits;
+};
+
+int splits_of(int64_t base, int64_t steps)
+{
+    if (base <= 0 || base >= 2 * kCusOfCard) return 1;
+    const int64_t want = (3 * kCusOfCard + base - 1) / base;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(want, steps / 2));
+}
+
+// Splits as the forward's: where there are fewer than two workgroups a CU, for about three.
+Plan plan_of(const flashlayer_attention *a)
+{
+    Plan p{};
+    const int64_t rows = (int64_t)a->Lq * (a->Hk ? a->H / a->Hk : 1), problems = (int64_t)a->B * a->Hk;
+    p.dp = padded_head(a->D);
+    p.row_tiles = (int)((rows + kRowTile - 1) / kRowTile);
+    p.q_tiles = (int)((rows + 127) / 128);
+    p.q_splits = splits_of(problems * p.q_tiles, (a->Lk + 63) / 64);
+    p.k_tiles = (a->Lk + 127) / 128;
+    p.k_splits = splits_of(problems * p.k_tiles, p.row_tiles);
+    return p;
+}
+
+uint64_t data_bytes(const flashlayer_attention *a)
+{
+    return align256((uint64_t)a->B * a->Lq * a->H * sizeof(RowData));
+}
+
+uint64_t largest_bytes(const flashlayer_attention *a, const Plan &p)
+{
+    return align256((uint64_t)a->B * a->Hk * p.row_tiles * 8);
+}
+
+uint64_t backward_bytes(const flashlayer_attention *a, bool want_q, bool want_kv)
+{
+    if (!a->B || !a->H || !a->D) return 0;
+    const Plan p = plan_of(a);
+    uint64_t q = 0, kv = 0;   // one after the other in one place
+    if (want_q && p.q_splits > 1)
+        q = size_prod({(uint64_t)p.q_splits, (uint64_t)a->B * a->Lq * a->H, (uint64_t)p.dp, 4});
+    if (want_kv && p.k_splits > 1)
+        kv = size_prod({2, (uint64_t)p.k_splits, (uint64_t)a->B * a->Lk * a->Hk, (uint64_t)p.dp, 4});
+    return data_bytes(a) + largest_bytes(a, p) + align256(std::max(q, kv));
+}
+
+template <int DT, int DP>
+int run(Backward &p, const Plan &plan, hipStream_t st)
+{
+    const uint64_t problems = (uint64_t)p.B * p.Hk;
+    if (p.gq && p.rows) {
+        p.tiles = plan.q_tiles;
+        p.splits = plan.q_splits;
+        if (const int rc = deal(p, size_prod({problems, (uint64_t)p.tiles, (uint64_t)p.splits}))) return rc;
+        const void *fn = p.kind ? (const void *)attend_grad_q<DT, DP, true> : (const void *)attend_grad_q<DT, DP, false>;
+        if (const int rc = launch_lds(fn, 8ull * p.per_xcd, p, ShapeQ<DT, DP>::LDS, st)) return rc;
+        if (p.splits > 1) {
+            Sum s{p.part, p.gq, (int64_t)problems * p.rows, p.splits, p.D};
+            const uint64_t lanes = (uint64_t)s.n * (DP / 4);
+            if (const int rc = launch_rows((const void *)attend_sum<DT, DP>, (lanes + 255) / 256, 256, s, st)) return rc;
+        }
+    }
+    if (!p.gk || !p.Lk) return FLASHBEV_OK;
+    p.tiles = plan.k_tiles;
+    p.splits = plan.k_splits;
+    if (const int rc = deal(p, size_prod({problems, (uint64_t)p.tiles, (uint64_t)p.splits}))) return rc;
+    const void *fn = p.kind ? (const void *)attend_grad_kv<DT, DP, true> : (const void *)attend_grad_kv<DT, DP, false>;
+    if (const int rc = launch_lds(fn, 8ull * p.per_xcd, p, ShapeK<DT, DP>::LDS, st)) return rc;
+    if (p.splits <= 1) return FLASHBEV_OK;
+    for (int half = 0; half < 2; ++half) {
+        Sum s{p.part, half ? p.gv : p.gk, (int64_t)problems * p.Lk, p.splits, p.D};
+        s.part += half * p.splits * s.n * DP;
+        const uint64_t lanes = (uint64_t)s.n * (DP / 4);
+        if (const int rc = launch_rows((const void *)attend_sum<DT, DP>, (lanes + 255) / 256, 256, s, st)) return rc;
+    }
+    return FLASHBEV_OK;
+}
+
+template <int DT>
+int run_width(Backward &p, const Plan &plan, hipStream_t st)
+{
+    const uint64_t tiles = size_prod({(uint64_t)p.B, (uint64_t)p.Hk, (uint64_t)plan.row_tiles});
+    if (const int rc = launch_kernel((const void *)attend_rows<DT>, tiles, 256, p, 0, st)) return rc;
+    switch (plan.dp) {
+    case 32: return run<DT, 32>(p, plan, st);
+    case 64: return run<DT, 64>(p, plan, st);
+    case 96: return run<DT, 96>(p, plan, st);
+    default: return run<DT, 128>(p, plan, st);
+    }
+}
+
+}  // namespace
+
+extern "C" int flashlayer_attention_backward_workspace_size(const flashlayer_attention *args, int32_t want_q,
+                                                            int32_t want_kv, uint64_t *bytes)
+{
+    if (!bytes) return FLASHBEV_ERR_NULLPTR;
+    if (const int rc = check_attention(args)) return rc;
+    *bytes = backward_bytes(args, want_q, want_kv);
+    return FLASHBEV_OK;
+}
+
+extern "C" int flashlayer_attention_backward(const flashlayer_attention *args, const void *grad_out, const void *q,
+                                             const void *k, const void *v, const void *mask,
+                                             const int32_t *key_lengths, const void *out, const void *rest,
+                                             const float *stats, void *grad_q, void *grad_k, void *grad_v,
+                                             void *workspace, uint64_t workspace_bytes, void *stream)
+{
+    if (const int rc = check_attention(args)) return rc;
+    const flashlayer_attention &a = *args;
+    const int es = elem_size(a.dtype);
+    const uint64_t rows = (uint64_t)a.B * a.Lq * a.H, keys = (uint64_t)a.B * a.Lk * a.Hk;
+    // (a gradient without elements may be null)
+    if (!a.B || !a.H || !a.D) return FLASHBEV_OK;
+    if (keys && (!grad_k) != (!grad_v)) return FLASHBEV_ERR_NULLPTR;
+    if (!(grad_q && rows) && !(grad_k && keys)) {
+        return (!rows && grad_q) || (!keys && grad_k) || !rows || !keys ? FLASHBEV_OK : FLASHBEV_ERR_NULLPTR;
+    }
+    if ((rows && (!grad_out || !q || !out || !stats)) || (keys && (!k || !v))) return FLASHBEV_ERR_NULLPTR;
+    if (a.mask && rows && keys && !mask) return FLASHBEV_ERR_NULLPTR;
+    const int ms = a.mask == FLASHLAYER_MASK_BOOL ? 1 : a.mask == FLASHLAYER_MASK_ADD_F32 ? 4 : es;
+    for (const void *t : {grad_out, q, k, v, out, rest, (const void *)grad_q, (const void *)grad_k, (const void *)grad_v})
+        if (misaligned(t, es)) return FLASHBEV_ERR_ALIGN;
+    if (misaligned(stats, 4) || misaligned(key_lengths, 4) || (a.mask && misaligned(mask, ms))) return FLASHBEV_ERR_ALIGN;
+    const uint64_t need = backward_bytes(args, grad_q, grad_k);
+    if (const int rc = check_scratch(workspace, workspace_bytes, need)) return rc;
+    if (const int rc = check_overlaps(
+            {{grad_q, rows * a.D * es}, {grad_k, keys * a.D * es}, {grad_v, keys * a.D * es}, {workspace, need}},
+            {{grad_out, span4(a.B, a.o_batch, a.Lq, a.o_row, a.H, a.o_head, a.D, es)},
+             {q, span4(a.B, a.q_batch, a.Lq, a.q_row, a.H, a.q_head, a.D, es)},
+             {k, span4(a.B, a.k_batch, a.Lk, a.k_row, a.Hk, a.k_head, a.D, es)},
+             {v, span4(a.B, a.v_batch, a.Lk, a.v_row, a.Hk, a.v_head, a.D, es)},
+             {a.mask ? mask : nullptr, span4(a.B, a.mask_batch, a.H, a.mask_head, a.Lq, a.mask_row, a.Lk, ms)},
+             {key_lengths, (uint64_t)a.B * 4},
+             {out, rows * a.D * es},
+             {rest, rows * a.D * es},
+             {stats, rows * 8}}))
+        return rc;
+    const Plan plan = plan_of(args);
+    Backward p{};
+    static_cast<Attend &>(p) = attend_of(args);
+    p.q = static_cast<const char *>(q);
+    p.k = static_cast<const char *>(k);
+    p.v = static_cast<const char *>(v);
+    p.g = static_cast<const char *>(grad_out);
+    p.mask = static_cast<const char *>(mask);
+    p.lengths = key_lengths;
+    p.out = static_cast<const char *>(out);
+    p.rest = static_cast<const char *>(rest);
+    p.stats = stats;
+    p.gq = static_cast<char *>(grad_q);
+    p.gk = static_cast<char *>(grad_k);
+    p.gv = static_cast<char *>(grad_v);
+    p.row_tiles = plan.row_tiles;
+    char *ws = static_cast<char *>(workspace);
+    p.data = reinterpret_cast<RowData *>(ws);
+    p.largest = reinterpret_cast<float *>(ws + data_bytes(args));
+    p.part = reinterpret_cast<float *>(ws + data_bytes(args) + largest_bytes(args, plan));
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (a.dtype == FLASHBEV_F32) return run_width<FLASHBEV_F32>(p, plan, st);
+    return a.dtype == FLASHBEV_F16 ? run_width<FLASHBEV_F16>(p, plan, st) : run_width<FLASHBEV_BF16>(p, plan, st);
+}

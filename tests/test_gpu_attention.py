@@ -1,0 +1,287 @@
+"""Attention on the GPU against float64, within bounds counted from its roundings."""
+import math
+
+import pytest
+import torch
+
+import layer_ref as ref
+import paper_2607_10071_amd as fb
+
+pytestmark = pytest.mark.gpu
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+LOWEST = torch.finfo(F32).min
+
+
+def make(B, Lq, Lk, H, Hk, D, dtype, seed=0, std=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed + 7 * Lq + 11 * Lk + D)
+    return [(torch.randn(s, generator=g, device="cuda") * std).to(dtype)
+            for s in ((B, Lq, H, D), (B, Lk, Hk, D), (B, Lk, Hk, D), (B, Lq, H, D))], g
+
+
+def run_forward(q, k, v, **kw):
+    stats = torch.full((q.shape[0], q.shape[2], q.shape[1], 2), 7.0, device="cuda")
+    rest = torch.empty_like(q, memory_format=torch.contiguous_format)
+    out = fb.attention_forward(q, k, v, stats=stats, rest=rest, **kw)
+    return out, rest, stats
+
+
+def check_all(q, k, v, g, scale=None, mask=None, key_lengths=None):
+    """The forward, its statistics, and all gradients."""
+    kw = dict(scale=scale, mask=mask, key_lengths=key_lengths)
+    want, tol = ref.attention(q, k, v, scale, mask, key_lengths, g)
+    out, rest, stats = run_forward(q, k, v, **kw)
+    ref.check(out, want["out"], tol["out"], "out")
+    # the statistics name the softmax's denominator
+    s, size, _ = ref.scores(q, k, q.shape[-1] ** -0.5 if scale is None else scale, mask, key_lengths)
+    if s.shape[-1]:
+        lse = torch.logsumexp(s, -1)
+        empty = lse == -math.inf
+        assert ((stats[..., 0] == -math.inf) == empty).all()
+        near = (stats.double().sum(-1) - lse).abs()[~empty]
+        lim = (size.amax(-1) * (q.shape[-1] + 8) * 2 * ref.U32 + lse.abs() * 2 ** -22 + ref.half(q.dtype) + 1e-5)[~empty]
+        assert (near <= lim).all(), (near - lim).max()
+    r = fb.attention_backward(g, q, k, v, out, stats, rest=rest if q.dtype != F32 else None, **kw)
+    for n in "qkv":
+        ref.check(r[n], want["grad_" + n], tol["grad_" + n], "grad_" + n)
+    return out, r
+
+
+SHAPES = [
+    # B, Lq, Lk, H, Hk, D
+    (1, 1, 1, 1, 1, 32), (2, 1, 129, 4, 4, 64), (2, 1, 1000, 8, 2, 128), (1, 5, 33, 3, 3, 1),
+    (1, 33, 64, 2, 2, 32), (2, 70, 65, 4, 2, 64), (1, 128, 128, 2, 1, 96), (1, 200, 300, 3, 3, 128),
+    (3, 77, 133, 6, 2, 72), (1, 129, 257, 2, 2, 33), (1, 31, 511, 5, 1, 17), (1, 300, 31, 2, 2, 8),
+    (1, 17, 2100, 2, 2, 40), (1, 2100, 40, 1, 1, 32), (2, 64, 640, 4, 4, 100), (1, 3, 700, 9, 3, 127),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_sizes(shape, dtype):
+    (q, k, v, g), _ = make(*shape, dtype)
+    check_all(q, k, v, g)
+
+
+def masks(kind, B, H, Lq, Lk, dtype, g):
+    """(mask, key lengths)"""
+    def rand(*s):
+        return torch.rand(s, generator=g, device="cuda")
+
+    if kind == "lengths":
+        lens = (rand(B) * (Lk + 1)).int()
+        lens[0] = 0
+        return None, lens
+    if kind == "keys":
+        return rand(B, 1, 1, Lk) < 0.6, None
+    if kind == "keys_of_heads":
+        return rand(1, H, 1, Lk) < 0.6, None
+    if kind == "pairs":
+        return (rand(B, 1, Lq, Lk) < 0.5) & (rand(B, 1, Lq, 1) < 0.8), None
+    if kind == "all":
+        return (rand(B, H, Lq, Lk) < 0.5) & (rand(B, H, Lq, 1) < 0.8), (rand(B) * (Lk + 1)).int()
+    if kind == "nothing":
+        return torch.zeros((1, 1, 1, Lk), dtype=torch.bool, device="cuda"), None
+    add = 2 * torch.randn((1, H, Lq, Lk), generator=g, device="cuda")
+    if kind == "inf":
+        add = add.masked_fill(rand(1, H, Lq, Lk) < 0.3, -math.inf).masked_fill(rand(1, 1, Lq, 1) < 0.2, -math.inf)
+    if kind == "lowest":
+        add = add.masked_fill(rand(1, H, Lq, Lk) < 0.3, LOWEST).masked_fill(rand(1, 1, Lq, 1) < 0.2, LOWEST)
+    if kind == "of_type":
+        low = torch.finfo(dtype).min
+        add = add.to(dtype).masked_fill(rand(1, H, Lq, Lk) < 0.3, low).masked_fill(rand(1, 1, Lq, 1) < 0.2, low)
+    return add, None
+
+
+@pytest.mark.parametrize("kind", ["lengths", "keys", "keys_of_heads", "pairs", "all", "nothing", "add", "inf", "lowest",
+                                  "of_type"])
+@pytest.mark.parametrize("shape", [(2, 40, 150, 4, 2, 32), (3, 1, 777, 6, 3, 72), (2, 131, 97, 2, 2, 128),
+                                   (1, 20, 1100, 2, 2, 37)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+def test_masks(shape, kind, dtype):
+    (q, k, v, g), gen = make(*shape, dtype, seed=3)
+    mask, lengths = masks(kind, shape[0], shape[3], shape[1], shape[2], dtype, gen)
+    check_all(q, k, v, g, mask=mask, key_lengths=lengths)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+def test_left_out_keys_may_hold_anything(dtype):
+    (q, k, v, g), gen = make(2, 37, 200, 4, 2, 48, dtype)
+    lengths = torch.tensor([130, 77], dtype=torch.int32, device="cuda")
+    mask = torch.rand((2, 1, 1, 200), generator=gen, device="cuda") < 0.7
+    clean = check_all(q, k, v, g, mask=mask, key_lengths=lengths)
+    gone = ~mask[:, 0, 0] | (torch.arange(200, device="cuda") >= lengths[:, None])
+    for bad in (math.nan, math.inf, -math.inf):
+        kb, vb = k.clone(), v.clone()
+        kb[gone], vb[gone] = bad, bad
+        out, rest, stats = run_forward(q, kb, vb, mask=mask, key_lengths=lengths)
+        assert torch.equal(out, clean[0])
+        r = fb.attention_backward(g, q, kb, vb, out, stats, mask, lengths, rest=rest if dtype != F32 else None)
+        for n in "qkv":
+            assert torch.equal(r[n], clean[1][n]), n
+        assert (r["k"][gone] == 0).all() and (r["v"][gone] == 0).all()
+
+
+def test_lengths_outside_the_keys_are_taken_as_within():
+    (q, k, v, g), _ = make(2, 9, 100, 2, 2, 32, BF16)
+    got = fb.attention_forward(q, k, v, key_lengths=torch.tensor([-5, 1 << 30], dtype=torch.int32, device="cuda"))
+    assert (got[0] == 0).all()
+    assert torch.equal(got[1], fb.attention_forward(q, k, v)[1])
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("std,scale", [(6.0, None), (1.0, 4.0), (1e-3, None), (1.0, 1e-20)])
+def test_large_and_small_scores(dtype, std, scale):
+    (q, k, v, g), _ = make(1, 70, 333, 2, 2, 64, dtype, std=std)
+    check_all(q, k, v, g, scale=scale)
+
+
+@pytest.mark.parametrize("lq", [20, 150])
+def test_growing_scores(lq):
+    """Every tile's scores pass those before it: the references move all the way."""
+    (q, k, v, g), _ = make(1, lq, 1500, 2, 2, 32, BF16)
+    q = q.abs()
+    k = (k.abs() * torch.linspace(0, 4, 1500, device="cuda")[None, :, None, None]).to(BF16)
+    check_all(q, k, v, g)
+    check_all(q, k.flip(1).contiguous(), v, g)
+
+
+def test_small_float16_gradients_keep_their_digits():
+    """Weights of one in 20000 and gradients of 1e-3: below float16's normal numbers unscaled."""
+    (q, k, v, g), _ = make(1, 64, 20000, 1, 1, 32, F16, std=0.1)
+    g = (g * 1e-2).to(F16)
+    out, rest, stats = run_forward(q, k, v)
+    r = fb.attention_backward(g, q, k, v, out, stats, rest=rest)
+    d = [t.double().squeeze(0).squeeze(1).requires_grad_() for t in (q, k, v)]
+    o = torch.softmax(d[0] @ d[1].t() * 32 ** -0.5, -1) @ d[2]
+    want = torch.autograd.grad(o, d, g.double().squeeze(0).squeeze(1))
+    for n, w in zip("qkv", want):
+        got = r[n].double().squeeze(0).squeeze(1)
+        # what float16 holds of the result itself: a step of 2^-24, and its relative half step;
+        # the sums' terms are rounded to relative 2^-11 (weights, dS), a root-mean-square sum of them
+        assert ((got - w).norm() <= 4 * 2 ** -11 * w.norm() + 2 ** -24 * w.numel() ** 0.5), n
+
+
+def test_strides():
+    """Heads of one projection, a cache longer than what is read, transposed heads, an expanded batch."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    qkv = torch.randn((2, 90, 3, 4, 32), generator=g, device="cuda").to(BF16)
+    q, k, v = qkv.unbind(2)
+    check_all(q, k, v, torch.randn(q.shape, generator=g, device="cuda").to(BF16))
+    cache = torch.randn((2, 4, 500, 64), generator=g, device="cuda").to(F16)   # heads before positions
+    k = cache.transpose(1, 2)[:, :333]
+    v = cache.flip(2).transpose(1, 2)[:, :333]
+    q = torch.randn((2, 4, 50, 64), generator=g, device="cuda").to(F16).transpose(1, 2)
+    go = torch.randn((2, 4, 50, 64), generator=g, device="cuda").to(F16).transpose(1, 2)
+    check_all(q, k, v, go)
+    k1 = torch.randn((1, 70, 2, 24), generator=g, device="cuda").expand(3, -1, -1, -1)
+    q3 = torch.randn((3, 40, 4, 24), generator=g, device="cuda")
+    check_all(q3, k1, k1.flip(1), torch.randn(q3.shape, generator=g, device="cuda"))
+    # odd addresses: 16-bit elements at any of them
+    flat = torch.randn(4 * 60 * 2 * 20 + 3, generator=g, device="cuda").to(BF16)
+    q, k, v, go = (flat[i:i + 60 * 2 * 20].view(1, 60, 2, 20) for i in (1, 2401, 3, 2402))
+    check_all(q, k, v, go)
+
+
+def test_out_in_place_of_a_larger_tensor():
+    (q, k, v, _), _ = make(2, 33, 70, 4, 2, 40, BF16)
+    big = torch.full((2, 33, 5, 4, 40), 3.0, dtype=BF16, device="cuda")
+    fb.attention_forward(q, k, v, out=big[:, :, 2])
+    assert torch.equal(big[:, :, 2], fb.attention_forward(q, k, v))
+    big[:, :, 2] = 3.0
+    assert (big == 3.0).all()
+
+
+def test_masks_by_stride():
+    (q, k, v, g), gen = make(2, 40, 130, 4, 2, 32, F32)
+    wide = torch.randn((2, 1, 64, 200), generator=gen, device="cuda")
+    view = wide[:, :, 3:43, 11:141]
+    a, b = fb.attention_forward(q, k, v, mask=view), fb.attention_forward(q, k, v, mask=view.contiguous())
+    assert torch.equal(a, b)
+    check_all(q, k, v, g, mask=view.expand(2, 4, 40, 130))
+    check_all(q, k, v, g, mask=(view > 0)[:1])
+
+
+def test_empty():
+    z = torch.zeros
+    q, k = z((2, 3, 4, 32), device="cuda", dtype=BF16), z((2, 0, 2, 32), device="cuda", dtype=BF16)
+    stats = z((2, 4, 3, 2), device="cuda")
+    out = fb.attention_forward(q + 1, k, k, stats=stats)
+    assert (out == 0).all() and (stats[..., 0] == -math.inf).all() and (stats[..., 1] == 0).all()
+    r = fb.attention_backward(q + 1, q + 1, k, k, out, stats)
+    assert (r["q"] == 0).all() and r["k"].shape == k.shape
+    q0 = q[:, :0]
+    k = z((2, 5, 2, 32), device="cuda", dtype=BF16) + 1
+    out = fb.attention_forward(q0, k, k)
+    r = fb.attention_backward(q0, q0, k, k, out.contiguous(), z((2, 4, 0, 2), device="cuda"))
+    assert out.shape == q0.shape and (r["k"] == 0).all() and (r["v"] == 0).all()
+    assert fb.attention_forward(q[:0], k[:0], k[:0]).shape == (0, 3, 4, 32)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+def test_autograd(dtype):
+    (q, k, v, g), gen = make(2, 60, 150, 4, 2, 40, dtype)
+    lengths = torch.tensor([150, 61], dtype=torch.int32, device="cuda")
+    mask = torch.randn((1, 4, 60, 150), generator=gen, device="cuda")
+    want, tol = ref.attention(q, k, v, None, mask, lengths, g)
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    out = fb.attention_autograd(*leaves, mask=mask, key_lengths=lengths)
+    got = torch.autograd.grad(out, leaves, g)
+    for n, t in zip("qkv", got):
+        ref.check(t, want["grad_" + n], tol["grad_" + n], n)
+    # some of them, with another gradient's strides
+    out = fb.attention_autograd(q, leaves[1], v, mask=mask, key_lengths=lengths)
+    (gk,) = torch.autograd.grad(out, [leaves[1]], g.transpose(1, 3).contiguous().transpose(1, 3))
+    assert torch.equal(gk, got[1])
+    with torch.no_grad():
+        assert torch.equal(fb.attention_autograd(*leaves, mask=mask, key_lengths=lengths), out.detach())
+
+
+def test_one_state_has_no_gradient_through_its_weight():
+    (q, k, v, g), _ = make(2, 40, 1, 2, 2, 32, BF16)
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    out = fb.attention_autograd(*leaves)
+    gq, gk, gv = torch.autograd.grad(out, leaves, g)
+    assert torch.equal(out, v.expand_as(q))
+    # dP and delta are the same sum in two orders: 32 products of float32
+    size = (g.double().abs() * v.double().abs()).sum(-1)
+    assert (gq.double().abs() <= 40 * ref.U32 * (size * 32 ** -0.5)[..., None] * k.double().abs() * 1.01 + 1e-30).all()
+
+
+def test_gradient_against_differences():
+    (q, k, v, g), _ = make(1, 7, 50, 2, 1, 16, F32)
+    leaves = [t.requires_grad_() for t in (q, k, v)]
+    grads = torch.autograd.grad(fb.attention_autograd(*leaves), leaves, g)
+    def loss(q, k, v):
+        k, v = (t.repeat_interleave(2, 2) for t in (k, v))
+        p = torch.softmax(torch.einsum("bihd,bjhd->bhij", q, k) * 16 ** -0.5, -1)
+        return (torch.einsum("bhij,bjhd->bihd", p, v) * g.double()).sum()
+
+    for i, gr in enumerate(grads):
+        step = torch.randn(gr.shape, device="cuda", dtype=torch.float64)
+        ends = []
+        for e in (1e-4, -1e-4):
+            moved = [x.detach().double() for x in leaves]
+            moved[i] = moved[i] + e * step
+            ends.append(loss(*moved))
+        slope = (ends[0] - ends[1]) / 2e-4
+        # differences are off by third derivatives times 1e-8, the gradient by float32's digits
+        assert abs(slope - (gr.double() * step).sum()) < 1e-5 * (1 + (gr.double() * step).abs().sum()), i
+
+
+def test_same_bits_again_and_on_another_stream():
+    (q, k, v, g), _ = make(2, 300, 900, 4, 2, 64, BF16)
+    first = [t.clone() for t in run_forward(q, k, v)]
+    grads = fb.attention_backward(g, q, k, v, first[0], first[2], rest=first[1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = run_forward(q, k, v)
+        more = fb.attention_backward(g, q, k, v, first[0], first[2], rest=first[1])
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    assert all(torch.equal(grads[n], more[n]) for n in "qkv")
+    out = torch.empty_like(q)
+    call = fb.prepare_attention_forward(q, k, v, out=out)
+    call()
+    call()
+    assert torch.equal(out, first[0])
