@@ -86,13 +86,12 @@ struct Panel {
         return u32x4{0, 0, 0, 0};
     }
 
-    // Rows on their way from memory to LDS: thread tid takes granule tid % GR of rows
-    // tid / GR, + RP, ...  D a multiple of E: a tile's loads are under way while the last one
-    // is worked on.  Other widths are copied when it is their turn.
+    // Rows on their way from memory to LDS: thread tid takes granule tid % GR of rows tid / GR, + RP,
+    // ..., and a tile's loads are under way while the last one is worked on.
     struct Mover {
         int row, g;
         uint32_t off;      // of the granule from the tile's first row
-        bool mine;
+        bool mine;         // D a multiple of E: the granule is there
 
         __device__ __forceinline__ void start(int tid, int D, int64_t stride)
         {
@@ -102,16 +101,29 @@ struct Panel {
             mine = row < RP && g * E < D;
         }
 
-        // `base`: the tile's first row, of which `left` are there; there(i) says of row + i RP
-        // whether it is wanted
-        template <class There>
-        __device__ __forceinline__ void load(u32x4 (&v)[G], const char *base, int64_t stride, int left,
-                                             There there) const
+        // whether the thread's i-th row lies within the tile
+        __device__ __forceinline__ bool inside(int i) const { return R % RP == 0 || i < G - 1 || row + i * RP < R; }
+
+        __device__ __forceinline__ void clear(u32x4 (&v)[G]) const
         {
 #pragma unroll
-            for (int i = 0; i < G; ++i) {
-                v[i] = u32x4{0, 0, 0, 0};
-                if (mine && row + i * RP < left && there(row + i * RP)) v[i] = load16(base + i * RP * stride + off);
+            for (int i = 0; i < G; ++i) v[i] = u32x4{0, 0, 0, 0};
+        }
+
+        // `base`: the tile's first row, of which `left` >= 1 are there; past them the last one
+        // again, whose scores the caller cuts
+        __device__ __forceinline__ void load(u32x4 (&v)[G], const char *base, int64_t stride, int left) const
+        {
+            if (!mine) return;
+            if (left >= R) {
+#pragma unroll
+                for (int i = 0; i < G; ++i)
+                    if (inside(i)) v[i] = load16(base + i * RP * stride + off);
+            } else {
+                asm volatile("");
+#pragma unroll
+                for (int i = 0; i < G; ++i)
+                    v[i] = load16(base + (uint32_t)min(row + i * RP, left - 1) * (uint32_t)stride + g * 16);
             }
         }
 
@@ -120,10 +132,11 @@ struct Panel {
             if (row >= RP) return;
 #pragma unroll
             for (int i = 0; i < G; ++i)
-                if (R % RP == 0 || row + i * RP < R)
-                    *reinterpret_cast<u32x4 *>(lds + place(row + i * RP, g)) = v[i];
+                if (inside(i)) *reinterpret_cast<u32x4 *>(lds + place(row + i * RP, g)) = v[i];
         }
 
+        // Any width, rows that there(i) says are wanted, zeros for the others: when it is their
+        // turn.
         template <class There>
         __device__ __forceinline__ void copy(char *lds, const char *base, int64_t stride, int left, int D,
                                              There there) const
@@ -232,7 +245,8 @@ __device__ __forceinline__ void row_fragments(u32x4 (&f)[N], const char *row, bo
 // ---------------------------------------------------------------------------
 typedef uint32_t u32_any __attribute__((aligned(1)));
 
-// Scores x of keys key0 + 8 k + 4 h + i of a lane's row, scaled and masked: x = scale x + mask.
+// Scores x of keys key0 + 8 k + 4 h + i of a lane's row, scaled and masked: x = scale x + mask
+// (without a mask too: the kernels with masks serve odd widths).
 // `row` is the mask's row; Lk its length.
 __device__ __forceinline__ void mask_row(const Attend &p, f32x16 &x, const char *row, int key0, int h)
 {
@@ -240,7 +254,10 @@ __device__ __forceinline__ void mask_row(const Attend &p, f32x16 &x, const char 
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const int key = key0 + 8 * k + 4 * h;
-        if (p.kind == FLASHLAYER_MASK_BOOL) {
+        if (p.kind == FLASHLAYER_MASK_NONE) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * k + i] *= p.scale;
+        } else if (p.kind == FLASHLAYER_MASK_BOOL) {
             uint32_t w = 0;
             if (whole) {
                 w = *reinterpret_cast<const u32_any *>(row + key);
@@ -281,6 +298,7 @@ __device__ __forceinline__ void mask_row(const Attend &p, f32x16 &x, const char 
 // One place of a mask's row.
 __device__ __forceinline__ float mask_place(const Attend &p, float x, const char *row, int key)
 {
+    if (p.kind == FLASHLAYER_MASK_NONE) return x * p.scale;
     if (p.kind == FLASHLAYER_MASK_BOOL) return row[key] ? x * p.scale : -__builtin_inff();
     const float b = p.kind == FLASHLAYER_MASK_ADD_F32  ? load_elem<FLASHBEV_F32>(row, key)
                     : p.kind == FLASHLAYER_MASK_ADD + 16 ? load_elem<FLASHBEV_F16>(row, key)
@@ -288,9 +306,11 @@ __device__ __forceinline__ float mask_place(const Attend &p, float x, const char
     return __builtin_fmaf(x, p.scale, b);
 }
 
-// Scores of keys from `end` on leave a row.
+// Scores of keys from `end` on leave a row.  (The empty statement keeps the last tile's branch a
+// branch: as selections every tile paid for it, 100 of 280 vector instructions.)
 __device__ __forceinline__ void cut_keys(f32x16 &x, int key0, int h, int end)
 {
+    asm volatile("");
 #pragma unroll
     for (int i = 0; i < 16; ++i)
         if (key0 + 8 * (i >> 2) + 4 * h + (i & 3) >= end) x[i] = -__builtin_inff();
@@ -358,9 +378,12 @@ inline int check_attention(const flashlayer_attention *a)
     if (a->mask < FLASHLAYER_MASK_NONE || a->mask > FLASHLAYER_MASK_ADD_F32) return FLASHBEV_ERR_VALUE;
     if (!(a->scale > 0.0f) || !finite_value(a->scale)) return FLASHBEV_ERR_VALUE;
     if (a->D > FLASHLAYER_HEAD_MAX) return FLASHBEV_ERR_UNSUPPORTED;
-    for (const int64_t s : {a->k_row, a->v_row})   // (a tile's rows lie within 32 bits)
+    // (a tile's rows lie within 32 bits)
+    for (const int64_t s : {a->q_row, a->q_head, a->k_row, a->v_row, a->o_row, a->o_head})
         if (s > FLASHBLOCK_LD_MAX) return FLASHBEV_ERR_UNSUPPORTED;
     const uint64_t share = a->Hk ? a->H / a->Hk : 0;
+    for (const int64_t s : {a->q_head, a->o_head})
+        if (size_prod({share, (uint64_t)s}) > 1ull << 28) return FLASHBEV_ERR_UNSUPPORTED;
     // (rows by their share's reciprocal; places of the last tile within 31 bits)
     if (size_prod({(uint64_t)a->Lq, share, share}) > 0xffffffffull ||
         size_prod({(uint64_t)a->Lq, share}) > 0x7ffffe00ull || a->Lk > 0x7ffffe00)
@@ -400,6 +423,12 @@ inline bool apart(int n0, int64_t s0, int n1, int64_t s1, int n2, int64_t s2, in
 inline uint64_t align256(uint64_t v) { return (v + 255) & ~255ull; }
 
 inline int padded_head(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : 128; }
+
+// Whether a call takes the kernels that do all: masks, and rows that end inside a granule.
+inline bool any_of(const flashlayer_attention *a)
+{
+    return a->mask != FLASHLAYER_MASK_NONE || a->D % (16 / elem_size(a->dtype)) != 0;
+}
 
 inline Attend attend_of(const flashlayer_attention *a)
 {

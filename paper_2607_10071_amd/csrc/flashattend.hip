@@ -19,6 +19,7 @@ struct Forward : Attend {
     float *stats;        // null: not wanted
     float *part;         // splits > 1: [splits][B Hk rows][DP] sums, then [..][2] m and l
     float *part_ml;
+    int any;             // the kernels with masks: scores are scaled, references are theirs
 };
 
 // How far a score may pass its row's reference before the reference moves, in powers of two:
@@ -35,8 +36,8 @@ __device__ __forceinline__ float add_weights(float l, uint32_t two)
         typedef _Float16 h2 __attribute__((ext_vector_type(2)));
         return __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, two), h2{(_Float16)1.0f, (_Float16)1.0f}, l, false);
     } else {
-        l += __builtin_bit_cast(float, two << 16);
-        return l + __builtin_bit_cast(float, two & 0xffff0000u);
+        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, two), b2{(__bf16)1.0f, (__bf16)1.0f}, l, false);
     }
 }
 
@@ -54,8 +55,8 @@ struct Shape {
     static constexpr int LDS = STAGES * STAGE > JOIN ? STAGES * STAGE : JOIN;
 };
 
-// MASK: with a mask (its code in kernels of its own: it takes registers).  Wide float32 heads
-// take one workgroup's registers of a CU.
+// MASK: with a mask or rows that end inside a granule (that code in kernels of its own: it takes
+// registers).  Wide float32 heads take one workgroup's registers of a CU.
 template <int DT, int DP, int WQ, bool MASK>
 __global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) attend(Forward p)
 {
@@ -95,7 +96,6 @@ __global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) at
     row_fragments<DT, DP>(qf, p.q + b * p.qb + qi * p.qr + head * p.qh, row_there, p.D, lane);
     const char *mrow = p.mask + b * p.mb + head * p.mh + qi * p.mr;
     const char *kbase = p.k + b * p.kb + g * p.kh, *vbase = p.v + b * p.vb + g * p.vh;
-    const bool odd = p.D % P::E != 0;
     const float c = (MASK ? 1.0f : p.scale) * kLog2;   // of x, to powers of two
 
     f32x16 o[DB];
@@ -109,28 +109,24 @@ __global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) at
     km.start(tid, p.D, p.kr);
     vm.start(tid, p.D, p.vr);
     u32x4 kv[P::G], vv[P::G];
+    km.clear(kv);
+    vm.clear(vv);
+    const bool copies = MASK && (p.drops || p.D % P::E != 0);
     auto fetch = [&](int t) {
-        if (odd) return;
+        if (copies) return;
         const int k0 = t * S::BK;
-        const char *kt = kbase + k0 * p.kr, *vt = vbase + k0 * p.vr;
-        if (MASK && p.drops) {   // (all rows' masks are the first one's)
-            const auto there = [&](int i) { return mrow[k0 + i] != 0; };
-            km.load(kv, kt, p.kr, len - k0, there);
-            vm.load(vv, vt, p.vr, len - k0, there);
-        } else {
-            const auto there = [](int) { return true; };
-            km.load(kv, kt, p.kr, len - k0, there);
-            vm.load(vv, vt, p.vr, len - k0, there);
-        }
+        km.load(kv, kbase + k0 * p.kr, p.kr, len - k0);
+        vm.load(vv, vbase + k0 * p.vr, p.vr, len - k0);
     };
     auto put = [&](int t, char *lk, char *lv) {
-        if (!odd) {
+        if (!copies) {
             km.store(kv, lk);
             vm.store(vv, lv);
             return;
         }
         const int k0 = t * S::BK;
-        const auto there = [&](int i) { return !MASK || !p.drops || mrow[k0 + i] != 0; };
+        // (all rows' masks are the first one's where keys drop out)
+        const auto there = [&](int i) { return !p.drops || mrow[k0 + i] != 0; };
         km.copy(lk, kbase + k0 * p.kr, p.kr, len - k0, p.D, there);
         vm.copy(lv, vbase + k0 * p.vr, p.vr, len - k0, p.D, there);
     };
@@ -308,14 +304,15 @@ __global__ void __launch_bounds__(256) attend_join(Forward p)
     const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
     const int d = (int)(((int64_t)blockIdx.x * 256 + threadIdx.x) % LANES) * 4;
     if (at >= n) return;
-    const float c = (p.kind ? 1.0f : p.scale) * kLog2;
+    const float c = (p.any ? 1.0f : p.scale) * kLog2;
     float m = -__builtin_inff(), l = 0.0f;
+#pragma unroll 8
     for (int s = 0; s < p.splits; ++s) m = __builtin_fmaxf(m, p.part_ml[2 * (s * n + at)]);
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
     for (int s = 0; s < p.splits; ++s) {
         const float from = p.part_ml[2 * (s * n + at)];
-        if (from == -__builtin_inff()) continue;
-        const float f = exp2_fast((from - m) * c);
+        const float f = from == -__builtin_inff() ? 0.0f : exp2_fast((from - m) * c);
         l = __builtin_fmaf(p.part_ml[2 * (s * n + at) + 1], f, l);
         const f32x4 v = *reinterpret_cast<const f32x4 *>(p.part + (s * n + at) * DP + d);
 #pragma unroll
@@ -338,7 +335,7 @@ __global__ void __launch_bounds__(256) attend_join(Forward p)
     }
     if (p.stats && d == 0) {
         float *st = p.stats + (((int64_t)b * p.H + head) * p.Lq + qi) * 2;
-        st[0] = p.kind ? m : m * p.scale;
+        st[0] = p.any ? m : m * p.scale;
         st[1] = l == 0.0f ? 0.0f : log2_fast(l) * kLn2;
     }
 }
@@ -348,6 +345,7 @@ __global__ void __launch_bounds__(256) attend_join(Forward p)
 // ---------------------------------------------------------------------------
 struct Plan {
     int wq, tiles, splits, dp;
+    bool any;
 };
 
 // A call's shape.  Up to 32 rows: the wavefronts of a workgroup go over the keys in turn.  Where
@@ -358,6 +356,7 @@ Plan plan_of(const flashlayer_attention *a)
     Plan p{};
     const int64_t rows = (int64_t)a->Lq * (a->Hk ? a->H / a->Hk : 1);
     p.dp = padded_head(a->D);
+    p.any = any_of(a);
     p.wq = rows <= 32 ? 1 : 4;
     const int bq = 32 * p.wq, bk = p.wq == 4 ? 64 : 128;
     p.tiles = (int)((rows + bq - 1) / bq);
@@ -386,8 +385,8 @@ uint64_t forward_bytes(const flashlayer_attention *a)
 template <int DT, int DP>
 int run(Forward &p, const Plan &plan, hipStream_t st)
 {
-    const void *fn = plan.wq == 4 ? p.kind ? (const void *)attend<DT, DP, 4, true> : (const void *)attend<DT, DP, 4, false>
-                     : p.kind     ? (const void *)attend<DT, DP, 1, true>
+    const void *fn = plan.wq == 4 ? plan.any ? (const void *)attend<DT, DP, 4, true> : (const void *)attend<DT, DP, 4, false>
+                     : plan.any   ? (const void *)attend<DT, DP, 1, true>
                                   : (const void *)attend<DT, DP, 1, false>;
     const size_t lds = plan.wq == 4 ? Shape<DT, DP, 4>::LDS : Shape<DT, DP, 1>::LDS;
     if (const int rc = launch_lds(fn, 8ull * p.per_xcd, p, lds, st)) return rc;
@@ -461,6 +460,7 @@ extern "C" int flashlayer_attention_forward(const flashlayer_attention *args, co
     p.stats = stats;
     p.tiles = plan.tiles;
     p.splits = plan.splits;
+    p.any = plan.any;
     if (p.splits > 1) {
         p.part = static_cast<float *>(workspace);
         p.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + part_bytes(args, plan));

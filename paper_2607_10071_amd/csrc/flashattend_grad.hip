@@ -41,16 +41,16 @@ struct Backward : Attend {
     const char *out, *rest;   // [B, Lq, H, D]; rest null: none
     const float *stats;
     RowData *data;            // [B Hk][rows]
-    float *largest;           // [B Hk][ceil(rows / 64)][2]: the largest 1 / l and |g| / l of 64 rows
+    float *largest;           // [B Hk][ceil(rows / 16)][2]: the largest 1 / l and |g| / l of 16 rows
     char *gq, *gk, *gv;       // contiguous; null: not wanted
     float *part;              // splits > 1: grad_q's [splits][B Hk rows][DP] or
                               // grad_k's and grad_v's [2][splits][B Hk Lk][DP]
-    int row_tiles;            // of 64
+    int row_tiles;            // of 16
 };
 
-constexpr int kRowTile = 64;
+constexpr int kRowTile = 16;
 
-// delta and |g| of a tile of 64 rows, 16 lanes to a row.
+// delta and |g| of a tile of 16 rows, 16 lanes to a row.
 template <int DT>
 __global__ void __launch_bounds__(256) attend_rows(Backward p)
 {
@@ -60,9 +60,8 @@ __global__ void __launch_bounds__(256) attend_rows(Backward p)
     const int b = problem / p.Hk, g = problem - b * p.Hk;
     const int part = threadIdx.x & 15;
     float most_l = 0.0f, most_g = 0.0f;
-    for (int k = 0; k < 4; ++k) {
-        const int r = tile * kRowTile + k * 16 + (threadIdx.x >> 4);
-        if (r >= p.rows) break;   // (whole groups of 16 lanes)
+    const int r = tile * kRowTile + (threadIdx.x >> 4);
+    if (r < p.rows) {   // (whole groups of 16 lanes)
         int qi, qj;
         p.row(r, qi, qj);
         const int head = g * p.share + qj;
@@ -171,8 +170,6 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
     const float mc = row.m * kLog2;
     const float inv = row.norm > 0.0f ? 1.0f / row.norm : 1.0f, off = -row.delta * inv;
     const char *kbase = p.k + b * p.kb + g * p.kh, *vbase = p.v + b * p.vb + g * p.vh;
-    const bool odd = p.D % P::E != 0;
-
     f32x16 o[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = zeros16();
@@ -183,28 +180,24 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
     km.start(tid, p.D, p.kr);
     vm.start(tid, p.D, p.vr);
     u32x4 kv[P::G], vv[P::G];
+    km.clear(kv);
+    vm.clear(vv);
+    const bool copies = MASK && (p.drops || p.D % P::E != 0);
     auto fetch = [&](int t) {
-        if (odd) return;
+        if (copies) return;
         const int k0 = t * S::BK;
-        const char *kt = kbase + k0 * p.kr, *vt = vbase + k0 * p.vr;
-        if (MASK && p.drops) {
-            const auto there = [&](int i) { return mrow[k0 + i] != 0; };
-            km.load(kv, kt, p.kr, len - k0, there);
-            vm.load(vv, vt, p.vr, len - k0, there);
-        } else {
-            const auto there = [](int) { return true; };
-            km.load(kv, kt, p.kr, len - k0, there);
-            vm.load(vv, vt, p.vr, len - k0, there);
-        }
+        km.load(kv, kbase + k0 * p.kr, p.kr, len - k0);
+        vm.load(vv, vbase + k0 * p.vr, p.vr, len - k0);
     };
     auto put = [&](int t, char *lk, char *lv) {
-        if (!odd) {
+        if (!copies) {
             km.store(kv, lk);
             vm.store(vv, lv);
             return;
         }
         const int k0 = t * S::BK;
-        const auto there = [&](int i) { return !MASK || !p.drops || mrow[k0 + i] != 0; };
+        // (all rows' masks are the first one's where keys drop out)
+        const auto there = [&](int i) { return !p.drops || mrow[k0 + i] != 0; };
         km.copy(lk, kbase + k0 * p.kr, p.kr, len - k0, p.D, there);
         vm.copy(lv, vbase + k0 * p.vr, p.vr, len - k0, p.D, there);
     };
@@ -333,7 +326,6 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
     row_fragments<DT, DP>(kf, p.k + b * p.kb + g * p.kh + key_at * p.kr, key_there, p.D, lane);
     row_fragments<DT, DP>(vf, p.v + b * p.vb + g * p.vh + key_at * p.vr, key_there, p.D, lane);
     const float c = (MASK ? 1.0f : p.scale) * kLog2;
-    const bool odd = p.D % P::E != 0;
 
     f32x16 ok[DB], ov[DB];
 #pragma unroll
@@ -341,35 +333,51 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
 
     typename P::Reader read;
     read.start(lane);
-    // rows on their way: query r / share of head r % share, so each thread's rows one by one
-    const int my_row = tid / P::GR, my_g = tid - my_row * P::GR;
+    // Rows on their way: row r is query r / share, head r % share.  A thread's places in a tile are
+    // the same in every tile where tiles are whole queries.
+    typename P::Mover mover;
+    mover.start(tid, p.D, 0);
     const char *qbase = p.q + b * p.qb + (int64_t)g * p.share * p.qh;
     const char *gbase = p.g + b * p.ob + (int64_t)g * p.share * p.oh;
+    const bool even = S::BR % p.share == 0, copies = MASK && p.D % P::E != 0;
     u32x4 qv[P::G], gv[P::G];
+    mover.clear(qv);
+    mover.clear(gv);
+    uint32_t qoff[P::G], goff[P::G];
     RowData rd{};
+    auto places = [&](int r0, int i0) {
+#pragma unroll
+        for (int i = 0; i < P::G; ++i) {
+            int qi, qj;   // past the last row the last one again, whose weights are zeros
+            p.row(min(r0 + mover.row + i * P::RP, p.rows - 1), qi, qj);
+            qoff[i] = (uint32_t)(qi - i0) * (uint32_t)p.qr + (uint32_t)qj * (uint32_t)p.qh + mover.g * 16;
+            goff[i] = (uint32_t)(qi - i0) * (uint32_t)p.orow + (uint32_t)qj * (uint32_t)p.oh + mover.g * 16;
+        }
+    };
     auto fetch = [&](int t) {
         const int r0 = t * S::BR;
         if (tid < S::BR && r0 + tid < p.rows) rd = p.data[problem * p.rows + r0 + tid];
-        if (odd) return;
+        if (copies) return;
+        const int i0 = r0 / p.share;
+        if (t == t0 || !even || r0 + S::BR > p.rows) places(r0, i0);
+        if (!mover.mine) return;
+        const char *qt = qbase + i0 * p.qr, *gt = gbase + i0 * p.orow;
 #pragma unroll
-        for (int i = 0; i < P::G; ++i) {
-            qv[i] = gv[i] = u32x4{0, 0, 0, 0};
-            const int r = r0 + my_row + i * P::RP;
-            if (my_row < P::RP && my_g * P::E < p.D && r < p.rows && my_row + i * P::RP < S::BR) {
-                int qi, qj;
-                p.row(r, qi, qj);
-                qv[i] = load16(qbase + qi * p.qr + qj * p.qh + my_g * 16);
-                gv[i] = load16(gbase + qi * p.orow + qj * p.oh + my_g * 16);
+        for (int i = 0; i < P::G; ++i)
+            if (mover.inside(i)) {
+                qv[i] = load16(qt + qoff[i]);
+                gv[i] = load16(gt + goff[i]);
             }
-        }
     };
     auto put = [&](int t, char *lq, char *lg, char *ld) {
         const int r0 = t * S::BR;
         if (tid < S::BR) {
             const bool there = r0 + tid < p.rows;
-            int qi, qj;
-            p.row(there ? r0 + tid : 0, qi, qj);
-            reinterpret_cast<int64_t *>(ld)[tid] = qi * p.mr + qj * p.mh;
+            if constexpr (MASK) {
+                int qi, qj;
+                p.row(there ? r0 + tid : 0, qi, qj);
+                reinterpret_cast<int64_t *>(ld)[tid] = qi * p.mr + qj * p.mh;
+            }
             float *f = reinterpret_cast<float *>(ld + 8 * S::BR);
             // rows past the last one weigh 2^-inf
             const float e = there ? rd.log2l - up : __builtin_inff();
@@ -377,27 +385,23 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
             f[S::BR + tid] = MASK || !there ? e : __builtin_fmaf(rd.m, kLog2, e);
             f[2 * S::BR + tid] = there ? rd.delta * more : 0.0f;
         }
-        if (my_row >= P::RP) return;
-        if (!odd) {
-#pragma unroll
-            for (int i = 0; i < P::G; ++i)
-                if (S::BR % P::RP == 0 || my_row + i * P::RP < S::BR) {
-                    *reinterpret_cast<u32x4 *>(lq + P::place(my_row + i * P::RP, my_g)) = qv[i];
-                    *reinterpret_cast<u32x4 *>(lg + P::place(my_row + i * P::RP, my_g)) = gv[i];
-                }
+        if (!copies) {
+            mover.store(qv, lq);
+            mover.store(gv, lg);
             return;
         }
+        if (mover.row >= P::RP) return;
 #pragma unroll 1
-        for (int i = my_row; i < S::BR; i += P::RP) {
+        for (int i = mover.row; i < S::BR; i += P::RP) {
             u32x4 a = {0, 0, 0, 0}, w = {0, 0, 0, 0};
             if (r0 + i < p.rows) {
                 int qi, qj;
                 p.row(r0 + i, qi, qj);
-                a = P::granule(qbase + qi * p.qr + qj * p.qh, my_g, p.D);
-                w = P::granule(gbase + qi * p.orow + qj * p.oh, my_g, p.D);
+                a = P::granule(qbase + qi * p.qr + qj * p.qh, mover.g, p.D);
+                w = P::granule(gbase + qi * p.orow + qj * p.oh, mover.g, p.D);
             }
-            *reinterpret_cast<u32x4 *>(lq + P::place(i, my_g)) = a;
-            *reinterpret_cast<u32x4 *>(lg + P::place(i, my_g)) = w;
+            *reinterpret_cast<u32x4 *>(lq + P::place(i, mover.g)) = a;
+            *reinterpret_cast<u32x4 *>(lg + P::place(i, mover.g)) = w;
         }
     };
     if (t0 < t1) fetch(t0);
@@ -503,6 +507,7 @@ __global__ void __launch_bounds__(256) attend_sum(Sum p)
 // ---------------------------------------------------------------------------
 struct Plan {
     int dp, row_tiles;
+    bool any;
     int q_tiles, q_splits;
     int k_tiles, k_splits;
 };
@@ -520,11 +525,12 @@ Plan plan_of(const flashlayer_attention *a)
     Plan p{};
     const int64_t rows = (int64_t)a->Lq * (a->Hk ? a->H / a->Hk : 1), problems = (int64_t)a->B * a->Hk;
     p.dp = padded_head(a->D);
+    p.any = any_of(a);
     p.row_tiles = (int)((rows + kRowTile - 1) / kRowTile);
     p.q_tiles = (int)((rows + 127) / 128);
     p.q_splits = splits_of(problems * p.q_tiles, (a->Lk + 63) / 64);
     p.k_tiles = (a->Lk + 127) / 128;
-    p.k_splits = splits_of(problems * p.k_tiles, p.row_tiles);
+    p.k_splits = splits_of(problems * p.k_tiles, (rows + 63) / 64);
     return p;
 }
 
@@ -558,7 +564,7 @@ int run(Backward &p, const Plan &plan, hipStream_t st)
         p.tiles = plan.q_tiles;
         p.splits = plan.q_splits;
         if (const int rc = deal(p, size_prod({problems, (uint64_t)p.tiles, (uint64_t)p.splits}))) return rc;
-        const void *fn = p.kind ? (const void *)attend_grad_q<DT, DP, true> : (const void *)attend_grad_q<DT, DP, false>;
+        const void *fn = plan.any ? (const void *)attend_grad_q<DT, DP, true> : (const void *)attend_grad_q<DT, DP, false>;
         if (const int rc = launch_lds(fn, 8ull * p.per_xcd, p, ShapeQ<DT, DP>::LDS, st)) return rc;
         if (p.splits > 1) {
             Sum s{p.part, p.gq, (int64_t)problems * p.rows, p.splits, p.D};
@@ -570,7 +576,7 @@ int run(Backward &p, const Plan &plan, hipStream_t st)
     p.tiles = plan.k_tiles;
     p.splits = plan.k_splits;
     if (const int rc = deal(p, size_prod({problems, (uint64_t)p.tiles, (uint64_t)p.splits}))) return rc;
-    const void *fn = p.kind ? (const void *)attend_grad_kv<DT, DP, true> : (const void *)attend_grad_kv<DT, DP, false>;
+    const void *fn = plan.any ? (const void *)attend_grad_kv<DT, DP, true> : (const void *)attend_grad_kv<DT, DP, false>;
     if (const int rc = launch_lds(fn, 8ull * p.per_xcd, p, ShapeK<DT, DP>::LDS, st)) return rc;
     if (p.splits <= 1) return FLASHBEV_OK;
     for (int half = 0; half < 2; ++half) {
