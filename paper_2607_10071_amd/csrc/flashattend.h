@@ -18,6 +18,7 @@
 
 #include "block/flashlayer.h"
 #include "block_mma.h"
+#include "block_stream.h"
 
 namespace {
 
@@ -204,6 +205,157 @@ struct Panel {
         }
     };
 };
+
+// Rows of DP elements in LDS as global_load_lds leaves them, four wavefronts loading: 64 granules to
+// a wavefront's instruction, one after the other, so the rows are not padded.  Granule g of row r
+// stands at place g ^ turn(r) of its row: lanes that read one granule of 16 rows, and half a
+// wavefront that reads 4 rows x 64 bytes transposed, use all 64 banks.
+template <int DT, int DP, int R>
+struct Strip {
+    static constexpr int W = 4;
+    static constexpr int ES = elem_size(DT), E = 16 / ES;
+    static constexpr int ROW = DP * ES, GR = ROW / 16, BYTES = R * ROW;
+    static constexpr int PIECES = BYTES / 1024;                // instructions
+    static constexpr int LOADS = (PIECES + W - 1) / W;         // of a wavefront
+    static constexpr int CHUNKS = GR / 2, STEPS = E == 8 ? 2 : 4;
+    static_assert(BYTES % 1024 == 0, "whole instructions");
+
+    static __device__ __forceinline__ int turn(int r)
+    {
+        if constexpr (GR % 16 == 0) return (r & 3) << 2 | (r >> 2 & 3);
+        if constexpr (GR % 16 == 8) return (r >> 1 & 1) << 2 | (r >> 2 & 3);
+        return r >> 2 & 3;
+    }
+
+    // A lane's granules of a strip: its rows and their offsets from the strip's first one.
+    struct Loader {
+        int row[LOADS];
+        uint32_t off[LOADS];
+        bool mine[LOADS];
+        uint32_t place;    // the wavefront's first instruction's, within the strip
+
+        __device__ __forceinline__ void start(int wave, int lane, int D, int64_t stride)
+        {
+            place = wave * 1024;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int n = (wave + i * W) * 64 + lane;
+                row[i] = n / GR;
+                const int g = (n - row[i] * GR) ^ turn(row[i]);
+                off[i] = (uint32_t)row[i] * (uint32_t)stride + g * 16;
+                mine[i] = g * E < D;
+            }
+        }
+
+        // `left` of the strip's rows are there; zeros for the others and past D
+        __device__ __forceinline__ void load(const char *base, int left, uint32_t lds, int wave) const
+        {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                if (PIECES % W != 0 && wave + i * W >= PIECES) break;
+                const char *p = base + off[i];
+                to_lds(mine[i] && row[i] < left ? p : reinterpret_cast<const char *>(kZeros), lds + place + i * W * 1024);
+            }
+        }
+    };
+
+    // The same of a problem's rows: row r is query r / share, head r % share, at `base` + its offset
+    // from the tile's first query.  Past the last one it comes again.
+    struct RowLoader {
+        int row[LOADS], g[LOADS];
+        uint32_t off[LOADS];
+
+        __device__ __forceinline__ void start(int wave, int lane)
+        {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int n = (wave + i * W) * 64 + lane;
+                row[i] = n / GR;
+                g[i] = (n - row[i] * GR) ^ turn(row[i]);
+            }
+        }
+
+        __device__ __forceinline__ void places(const Attend &p, int r0, int i0, int64_t stride, int64_t head)
+        {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                int qi, qj;
+                p.row(min(r0 + row[i], p.rows - 1), qi, qj);
+                off[i] = (uint32_t)(qi - i0) * (uint32_t)stride + (uint32_t)qj * (uint32_t)head + g[i] * 16;
+            }
+        }
+
+        __device__ __forceinline__ void load(const char *base, int D, uint32_t lds, int wave) const
+        {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                if (PIECES % W != 0 && wave + i * W >= PIECES) break;
+                const char *p = base + off[i];
+                to_lds(g[i] * E < D ? p : reinterpret_cast<const char *>(kZeros), lds + (wave + i * W) * 1024);
+            }
+        }
+    };
+
+    // A lane's places: sums of a part of its own, an exclusive or with what is known ahead, and
+    // distances that are known ahead.
+    struct Reader {
+        int along_row, along_turn, across_row, across_turn;
+
+        __device__ __forceinline__ void start(int lane)
+        {
+            const int i = lane & 31, h = lane >> 5;
+            along_row = i * ROW;
+            along_turn = (h ^ turn(i)) << 4;
+            if constexpr (ES == 2) {
+                const int j = lane & 15, a = lane >> 4 & 1, b = j >> 1 & 1;
+                across_row = (4 * h + (j >> 2)) * ROW + (j & 1) * 8;
+                across_turn = ((2 * a + b) ^ turn(4 * h + (j >> 2))) << 4;
+            } else {
+                across_row = 4 * h * ROW + (i & 3) * 4;
+                across_turn = ((i >> 2) ^ h) << 4;
+            }
+        }
+
+        // As Panel's.
+        __device__ __forceinline__ u32x4 along(const char *lds, int r0, int c) const
+        {
+            return *reinterpret_cast<const u32x4 *>(lds + along_row + (along_turn ^ (c << 5)) + r0 * ROW);
+        }
+
+        __device__ __forceinline__ u32x4 across(const char *lds, int r0, int u, int d0) const
+        {
+            u32x4 v;
+            if constexpr (ES == 2) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {   // (rows 8 q further on turn by 2 q more)
+                    const s16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (__attribute__((address_space(3))) s16x4 *)(lds + across_row +
+                                                                    (across_turn ^ (d0 * 2 ^ q << 5)) +
+                                                                    (r0 + 16 * u + 8 * q) * ROW));
+                    const uint64_t w = __builtin_bit_cast(uint64_t, t);
+                    v[2 * q] = (uint32_t)w;
+                    v[2 * q + 1] = (uint32_t)(w >> 32);
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    v[q] = *reinterpret_cast<const uint32_t *>(
+                        lds + across_row + (across_turn ^ (d0 * 4 ^ (turn(8 * u + q) << 4))) + (r0 + 8 * u + q) * ROW);
+            }
+            return v;
+        }
+    };
+};
+
+// Until this wavefront's loads to LDS are done, and then all wavefronts'.
+__device__ __forceinline__ void meet()
+{
+    wait_loads<0>();
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // its reads of LDS too: lgkmcnt 0
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 // Step u's operand of a block's registers, rounded to the inputs' type.
 template <int DT>

@@ -10,6 +10,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "flashattend.h"
 
 namespace {
@@ -22,10 +24,11 @@ struct Forward : Attend {
     int any;             // the kernels with masks: scores are scaled, references are theirs
 };
 
-// How far a score may pass its row's reference before the reference moves, in powers of two:
-// exp(s - m) stays below 2^that, within float16's range with room for the backward's factors.
+// How large weights exp(s - m) may become before the reference m moves: within float16's range
+// with room for the backward's factors, and above the 16 that a lane's share of 32 equal scores
+// adds up to, where sums are looked at.
 template <int DT>
-constexpr float kSlack = DT == FLASHBEV_F16 ? 4.0f : 8.0f;
+constexpr float kLargest = DT == FLASHBEV_F16 ? 64.0f : 256.0f;
 
 // l and the weights' sums, of two packed weights: the sum takes them as the product with v does,
 // rounded, so that the result is a mean of v's rows with weights that add up to one.
@@ -38,6 +41,56 @@ __device__ __forceinline__ float add_weights(float l, uint32_t two)
     } else {
         typedef __bf16 b2 __attribute__((ext_vector_type(2)));
         return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, two), b2{(__bf16)1.0f, (__bf16)1.0f}, l, false);
+    }
+}
+
+// A row's result of a wavefront (both halves' channels), or its part of one.
+template <int DT, int DP, bool MASK>
+__device__ __forceinline__ void put_row(const Forward &p, int b, int g, int split, int r, int qi, int head, float m,
+                                        float l, const f32x16 (&o)[DP / 32], int h)
+{
+    constexpr int ES = elem_size(DT), DB = DP / 32;
+    if (r >= p.rows) return;
+
+    if (p.splits > 1) {
+        const int64_t at = ((int64_t)split * p.B * p.Hk + (int64_t)b * p.Hk + g) * p.rows + r;
+        float *part = p.part + at * DP;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                float v[8];
+                columns_of(o[d], q, v);
+                store_elems<FLASHBEV_F32>(part + d * 32 + 16 * q + 8 * h, v);
+            }
+        if (!h) {
+            p.part_ml[2 * at] = m;
+            p.part_ml[2 * at + 1] = l;
+        }
+        return;
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // (a row that sees nothing)
+    char *out = p.o + b * p.ob + qi * p.orow + head * p.oh;
+    char *rest = p.rest ? p.rest + (((int64_t)b * p.Lq + qi) * p.H + head) * p.D * ES : nullptr;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            float v[8];
+            columns_of(o[d], q, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= inv;
+            put8<DT>(out, d * 32 + 16 * q + 8 * h, p.D, v);
+            if (rest) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] -= rounded<DT>(v[i]);
+                put8<DT>(rest, d * 32 + 16 * q + 8 * h, p.D, v);
+            }
+        }
+    if (p.stats && !h) {
+        float *st = p.stats + (((int64_t)b * p.H + head) * p.Lq + qi) * 2;
+        st[0] = MASK ? m : m * p.scale;
+        st[1] = l == 0.0f ? 0.0f : log2_fast(l) * kLn2;
     }
 }
 
@@ -62,7 +115,7 @@ __global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) at
 {
     using S = Shape<DT, DP, WQ>;
     using P = typename S::P;
-    constexpr int ES = elem_size(DT), NB = S::NB, DB = DP / 32;
+    constexpr int NB = S::NB, DB = DP / 32;
     extern __shared__ __attribute__((aligned(16))) char lds[];
 
     uint32_t id = item_of(p);
@@ -163,7 +216,7 @@ __global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) at
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = __builtin_fmaxf(top, x[n][i]);
         top = both_max(top);
-        if (__any((top - m) * c > kSlack<DT>)) {   // (-inf - -inf is no number, and not above)
+        if (__any(exp2_fast((top - m) * c) > kLargest<DT>)) {   // (-inf - -inf is no number, and not above)
             const float to = __builtin_fmaxf(m, top);
             const float f = to == -__builtin_inff() ? 1.0f : exp2_fast((m - to) * c);
             m = to;
@@ -251,48 +304,208 @@ __global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) at
         }
         if (wave) return;
     }
-    if (!row_there) return;   // (both halves of a row)
+    put_row<DT, DP, MASK>(p, b, g, split, r, qi, head, m, l, o, h);
+}
 
-    if (p.splits > 1) {
-        const int64_t at = ((int64_t)split * p.B * p.Hk + (int64_t)b * p.Hk + g) * p.rows + r;
-        float *part = p.part + at * DP;
+// Without masks: four wavefronts of 32 rows each share tiles of TK keys, which go from memory to LDS
+// without passing registers, and take them 32 keys at a time.  In one step a wavefront forms the
+// next 32 keys' scores, this 32's weights and the product of the last 32's with v: matrix
+// and vector instructions that do not wait for each other, in turn.  (Scores, then weights, then
+// the product: 2048 queries of 32 heads x 4096 keys x 128 bf16 165 us.)
+template <int DT, int DP>
+struct Flow {
+    static constexpr int TK = DP * elem_size(DT) <= 64 ? 128 : 64;
+    static constexpr int SUBS = TK / 32;
+    using T = Strip<DT, DP, TK>;
+    // K of two tiles and V of three: a tile's last product is taken with the next one's first step
+    static constexpr int LDS = 5 * T::BYTES;
+    // (the place in LDS that a load is told has 17 bits: what went past 128 KiB arrived at its
+    // start.  float32 heads of 128 channels take attend.)
+    static_assert(DP * elem_size(DT) >= 512 || LDS <= 131072, "within a load's reach");
+};
+
+// Wavefronts a SIMD that the registers are to leave room for.
+constexpr int flow_waves(int dt, int dp)
+{
+    return dp * elem_size(dt) <= 64 ? 4 : 2;
+}
+
+template <int DT, int DP>
+__global__ void __launch_bounds__(256, flow_waves(DT, DP)) attend_flow(Forward p)
+{
+    using F = Flow<DT, DP>;
+    using T = typename F::T;
+    constexpr int DB = DP / 32, PAIRS = 8, E = T::E;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+
+    uint32_t id = item_of(p);
+    if (id >= p.blocks) return;
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tile = id % p.tiles;
+    id /= p.tiles;
+    const int split = id % p.splits;
+    id /= p.splits;
+    const int g = id % p.Hk, b = id / p.Hk;
+    const int len = p.keys(b);
+    const int all = (len + F::TK - 1) / F::TK, per = (all + p.splits - 1) / p.splits;
+    const int t0 = split * per, t1 = min(all, t0 + per), end = min(len, t1 * F::TK);
+
+    const int r = tile * 128 + wave * 32 + (lane & 31);
+    int qi, qj;
+    p.row(min(r, p.rows - 1), qi, qj);
+    const int head = g * p.share + qj;
+    u32x4 qf[T::CHUNKS];
+    row_fragments<DT, DP>(qf, p.q + b * p.qb + qi * p.qr + head * p.qh, r < p.rows, p.D, lane);
+    const float c = p.scale * kLog2;   // of scores, to powers of two
+
+    f32x16 o[DB];
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DB; ++d) o[d] = zeros16();
+    float m = -__builtin_inff(), l = 0.0f;
+
+    typename T::Reader read;
+    read.start(lane);
+    typename T::Loader kl, vl;
+    kl.start(wave, lane, p.D, p.kr);
+    vl.start(wave, lane, p.D, p.vr);
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds);
+    const char *kbase = p.k + b * p.kb + g * p.kh, *vbase = p.v + b * p.vb + g * p.vh;
+    // K of tile t lies at k_at(t); V's places turn by one a tile
+    const auto k_at = [&](int t) { return (t & 1) * T::BYTES; };
+    const auto load = [&](int t, int v_at) {
+        kl.load(kbase + t * F::TK * p.kr, len - t * F::TK, lds0 + k_at(t), wave);
+        vl.load(vbase + t * F::TK * p.vr, len - t * F::TK, lds0 + v_at, wave);
+    };
+
+    // Weights 2 j and 2 j + 1 of a step: their exponents, their powers, and the packed word, which
+    // the lane's sum takes as it is.
+    const auto exponents = [&](const f32x16 &x, float(&v)[16], int j, float mc) {
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                float v[8];
-                columns_of(o[d], q, v);
-                store_elems<FLASHBEV_F32>(part + d * 32 + 16 * q + 8 * h, v);
-            }
-        if (!h) {
-            p.part_ml[2 * at] = m;
-            p.part_ml[2 * at + 1] = l;
+        for (int i = 2 * j; i < 2 * j + 2; ++i) v[i] = __builtin_fmaf(x[i], c, -mc);
+    };
+    const auto powers = [&](float(&v)[16], int j) {
+#pragma unroll
+        for (int i = 2 * j; i < 2 * j + 2; ++i) v[i] = exp2_fast(v[i]);
+    };
+    const auto packed = [&](const float(&v)[16], u32x4(&w)[T::STEPS], float &sum, int j) {
+        const int u = 2 * j / E, i = 2 * j % E;
+        if constexpr (DT == FLASHBEV_F32) {
+            w[u][i] = __builtin_bit_cast(uint32_t, v[2 * j]);
+            w[u][i + 1] = __builtin_bit_cast(uint32_t, v[2 * j + 1]);
+            sum += v[2 * j];
+            sum += v[2 * j + 1];
+        } else {
+            w[u][i / 2] = pack2<DT>(v[2 * j], v[2 * j + 1]);
+            sum = add_weights<DT>(sum, w[u][i / 2]);
         }
-        return;
-    }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // (a row that sees nothing)
-    char *out = p.o + b * p.ob + qi * p.orow + head * p.oh;
-    char *rest = p.rest ? p.rest + (((int64_t)b * p.Lq + qi) * p.H + head) * p.D * ES : nullptr;
+    };
+
+    // One step on scores x and their weights w: `next` scores of the 32 keys at lk, and the
+    // product of the last step's weights with the 32 rows of v at lv (FIRST: there are none).
+    const auto step = [&](auto first, f32x16 &x, f32x16 &next, u32x4(&w)[T::STEPS], const u32x4(&last)[T::STEPS],
+                          const char *lk, const char *lv, int key0) {
+        constexpr bool FIRST = decltype(first)::value;
+        // products: scores' at even places, v's at odd ones
+        constexpr int NS = T::CHUNKS, NP = FIRST ? 0 : T::STEPS * DB, N = 2 * (NS > NP ? NS : NP);
+        constexpr int AHEAD = 4, Q = (PAIRS * 2 + N - 1) / N;   // pairs of weights to two products
+        const auto is = [](int i) { return i % 2 == 0 ? i / 2 < NS : i / 2 < NP; };
+        const auto fragment = [&](int i) {
+            return i % 2 == 0 ? read.along(lk, 0, i / 2) : read.across(lv, 0, i / 2 / DB, i / 2 % DB * 32);
+        };
+        if (key0 + 32 > end) cut_keys(x, key0, h, end);
+        const float mc = m * c;
+        float v[16], sum = 0.0f;
+        u32x4 f[AHEAD];
+        next = zeros16();
+        // (places are formed again for every step: kept over the loop they spilled)
+        asm volatile("" : "+v"(read.along_turn), "+v"(read.across_turn));
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+        for (int i = 0; i < AHEAD; ++i)
+            if (is(i)) f[i] = fragment(i);
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            float v[8];
-            columns_of(o[d], q, v);
+        for (int i = 0; i < N + 4; ++i) {
+            if (i < N && is(i)) {
+                if (i % 2 == 0) {
+                    mma<DT>(next, f[i % AHEAD], qf[i / 2 % NS]);
+                } else if constexpr (!FIRST) {
+                    mma<DT>(o[i / 2 % DB], f[i % AHEAD], last[i / 2 / DB % T::STEPS]);
+                }
+            }
+            if (i + AHEAD < N && is(i + AHEAD)) f[i % AHEAD] = fragment(i + AHEAD);
+            if (i % 2 == 0) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= inv;
-            put8<DT>(out, d * 32 + 16 * q + 8 * h, p.D, v);
-            if (rest) {
+                for (int n = 0; n < Q; ++n) {
+                    if (const int j = (i / 2 - 2) * Q + n; j >= 0 && j < PAIRS) packed(v, w, sum, j);
+                    if (const int j = (i / 2 - 1) * Q + n; j >= 0 && j < PAIRS) powers(v, j);
+                    if (const int j = i / 2 * Q + n; j < PAIRS) exponents(x, v, j, mc);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // A reference that is too low shows in the sum of its weights; so does one that is not set
+        // yet, -inf, in weights that are infinite or no numbers.  (No maximum is taken of the
+        // other steps' scores.)
+        if (__any(!(sum <= kLargest<DT>))) {
+            asm volatile("");
+            float top = x[0];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] -= rounded<DT>(v[i]);
-                put8<DT>(rest, d * 32 + 16 * q + 8 * h, p.D, v);
+            for (int i = 0; i < 16; ++i) top = __builtin_fmaxf(top, x[i]);
+            const float to = __builtin_fmaxf(m, both_max(top));
+            const float by = m == -__builtin_inff() ? 0.0f : exp2_fast((m - to) * c);
+            // (scores that are all -inf leave the reference unset, and weights of 0)
+            const float at = (to == -__builtin_inff() ? 0.0f : to) * c;
+            m = to;
+            l *= by;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= by;
+            sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < PAIRS; ++j) {
+                exponents(x, v, j, at);
+                powers(v, j);
+                packed(v, w, sum, j);
             }
         }
-    if (p.stats && !h) {
-        float *st = p.stats + (((int64_t)b * p.H + head) * p.Lq + qi) * 2;
-        st[0] = MASK ? m : m * p.scale;
-        st[1] = l == 0.0f ? 0.0f : log2_fast(l) * kLn2;
+        l += sum;
+    };
+
+    if (t0 < t1) {
+        int v_now = 2 * T::BYTES, v_next = 3 * T::BYTES, v_free = 4 * T::BYTES;   // V of tiles t, t + 1, t + 2
+        load(t0, v_now);
+        if (t0 + 1 < t1) load(t0 + 1, v_next);
+        meet();
+        f32x16 x[2];
+        u32x4 w[2][T::STEPS];
+        x[0] = zeros16();
+#pragma unroll
+        for (int e = 0; e < T::CHUNKS; ++e) mma<DT>(x[0], read.along(lds + k_at(t0), 0, e), qf[e]);
+        step(std::true_type{}, x[0], x[1], w[0], w[1], lds + k_at(t0) + 32 * T::ROW, lds, t0 * F::TK);
+        for (int t = t0; t < t1; ++t) {
+            // Steps 1, 2, .. of the tile and step 0 of the next one (past the last tile it only takes
+            // the last step's product: its scores, of whatever lies there, are all cut).
+            const char *lk = lds + k_at(t), *lk2 = lds + k_at(t + 1), *lv = lds + v_now;
+#pragma unroll
+            for (int s = 1; s <= F::SUBS; ++s) {
+                if (s == F::SUBS - 1) {
+                    // the next tile is there; K's place of this one is free, and a third one of V's
+                    meet();
+                    if (t + 2 < t1) load(t + 2, v_free);
+                }
+                const char *k_next = s + 1 < F::SUBS ? lk + (s + 1) * 32 * T::ROW : lk2 + (s + 1 - F::SUBS) * 32 * T::ROW;
+                step(std::false_type{}, x[s & 1], x[s + 1 & 1], w[s & 1], w[s + 1 & 1], k_next,
+                     lv + (s - 1) * 32 * T::ROW, t * F::TK + s * 32);
+            }
+            const int turn = v_now;
+            v_now = v_next;
+            v_next = v_free;
+            v_free = turn;
+        }
     }
+    l = both_sum(l);
+    put_row<DT, DP, false>(p, b, g, split, r, qi, head, m, l, o, h);
 }
 
 // The splits' results: four channels of a row to a lane.
@@ -344,7 +557,7 @@ __global__ void __launch_bounds__(256) attend_join(Forward p)
 // host
 // ---------------------------------------------------------------------------
 struct Plan {
-    int wq, tiles, splits, dp;
+    int wq, tiles, splits, dp;   // wq 4: attend_flow; 5: attend with four wavefronts' rows; 1: with one's
     bool any;
 };
 
@@ -357,8 +570,9 @@ Plan plan_of(const flashlayer_attention *a)
     const int64_t rows = (int64_t)a->Lq * (a->Hk ? a->H / a->Hk : 1);
     p.dp = padded_head(a->D);
     p.any = any_of(a);
-    p.wq = rows <= 32 ? 1 : 4;
-    const int bq = 32 * p.wq, bk = p.wq == 4 ? 64 : 128;
+    const bool flows = !p.any && p.dp * elem_size(a->dtype) < 512;
+    p.wq = rows <= 32 ? 1 : flows ? 4 : 5;
+    const int bq = p.wq == 1 ? 32 : 128, bk = p.wq == 1 ? 128 : 64;
     p.tiles = (int)((rows + bq - 1) / bq);
     const int64_t base = (int64_t)a->B * a->Hk * p.tiles, keys = (a->Lk + bk - 1) / bk;
     p.splits = 1;
@@ -385,10 +599,21 @@ uint64_t forward_bytes(const flashlayer_attention *a)
 template <int DT, int DP>
 int run(Forward &p, const Plan &plan, hipStream_t st)
 {
-    const void *fn = plan.wq == 4 ? plan.any ? (const void *)attend<DT, DP, 4, true> : (const void *)attend<DT, DP, 4, false>
-                     : plan.any   ? (const void *)attend<DT, DP, 1, true>
-                                  : (const void *)attend<DT, DP, 1, false>;
-    const size_t lds = plan.wq == 4 ? Shape<DT, DP, 4>::LDS : Shape<DT, DP, 1>::LDS;
+    const void *fn = nullptr;
+    size_t lds = 0;
+    if constexpr (DP * elem_size(DT) < 512) {
+        if (plan.wq == 4) {
+            fn = (const void *)attend_flow<DT, DP>;
+            lds = Flow<DT, DP>::LDS;
+        }
+    }
+    if (plan.wq == 5) {
+        fn = (const void *)attend<DT, DP, 4, true>;
+        lds = Shape<DT, DP, 4>::LDS;
+    } else if (plan.wq == 1) {
+        fn = plan.any ? (const void *)attend<DT, DP, 1, true> : (const void *)attend<DT, DP, 1, false>;
+        lds = Shape<DT, DP, 1>::LDS;
+    }
     if (const int rc = launch_lds(fn, 8ull * p.per_xcd, p, lds, st)) return rc;
     if (p.splits <= 1) return FLASHBEV_OK;
     const uint64_t lanes = (uint64_t)p.B * p.Hk * p.rows * (DP / 4);
@@ -460,7 +685,7 @@ extern "C" int flashlayer_attention_forward(const flashlayer_attention *args, co
     p.stats = stats;
     p.tiles = plan.tiles;
     p.splits = plan.splits;
-    p.any = plan.any;
+    p.any = plan.any || plan.wq == 5;
     if (p.splits > 1) {
         p.part = static_cast<float *>(workspace);
         p.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + part_bytes(args, plan));

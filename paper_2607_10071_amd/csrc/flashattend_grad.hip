@@ -12,12 +12,14 @@
 //
 // Digits.  p and dS are rounded to the inputs' type for their products.  bfloat16 has float32's
 // range; float16 loses digits below 6e-5, where weights of one in 40000 and scaled losses'
-// gradients lie, so its factors are kept near one: grad_q's kernel takes p l (at most 2^4) and
-// g / |g|, a row's factors coming back at the end; the other one takes p and dS times powers of
+// gradients lie, so its factors are kept near one: grad_q's kernel takes p l (at most 2^6) and
+// g / (8 |g|), a row's factors coming back at the end; the other one takes p and dS times powers of
 // two that bring the largest 1 / l and |g| / l of its rows to about one.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "flashattend.h"
 
@@ -41,7 +43,11 @@ struct Backward : Attend {
     const char *out, *rest;   // [B, Lq, H, D]; rest null: none
     const float *stats;
     RowData *data;            // [B Hk][rows]
-    float *largest;           // [B Hk][ceil(rows / 16)][2]: the largest 1 / l and |g| / l of 16 rows
+    float *largest;           // [B Hk][padded / 16][2]: the largest 1 / l and |g| / l of 16 rows
+    // [B Hk][padded rows] each, for grad_k's and grad_v's kernel without masks: the exponent that a
+    // row's weights lose, m log2(e) + log2(l), infinite past the last row; and delta
+    float *lose, *delta;
+    int padded;               // rows of a problem there: a multiple of 128
     char *gq, *gk, *gv;       // contiguous; null: not wanted
     float *part;              // splits > 1: grad_q's [splits][B Hk rows][DP] or
                               // grad_k's and grad_v's [2][splits][B Hk Lk][DP]
@@ -105,7 +111,14 @@ __global__ void __launch_bounds__(256) attend_rows(Backward p)
             most_l = __builtin_fmaxf(most_l, inv);
             most_g = __builtin_fmaxf(most_g, row.norm * inv);
         }
-        if (part == 0) p.data[(int64_t)problem * p.rows + r] = row;
+        if (part == 0) {
+            p.data[(int64_t)problem * p.rows + r] = row;
+            p.lose[(int64_t)problem * p.padded + r] = __builtin_fmaf(row.m, kLog2, row.log2l);
+            p.delta[(int64_t)problem * p.padded + r] = row.delta;
+        }
+    } else if (part == 0 && r < p.padded) {
+        p.lose[(int64_t)problem * p.padded + r] = __builtin_inff();
+        p.delta[(int64_t)problem * p.padded + r] = 0.0f;
     }
 #pragma unroll
     for (int o = 16; o < 64; o *= 2) {
@@ -168,7 +181,7 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
     const float c = (MASK ? 1.0f : p.scale) * kLog2;
     // weights are p l; an empty row's are exp(-inf - 0) = 0
     const float mc = row.m * kLog2;
-    const float inv = row.norm > 0.0f ? 1.0f / row.norm : 1.0f, off = -row.delta * inv;
+    const float inv = row.norm > 0.0f ? 0.125f / row.norm : 1.0f, off = -row.delta * inv;
     const char *kbase = p.k + b * p.kb + g * p.kh, *vbase = p.v + b * p.vb + g * p.vh;
     f32x16 o[DB];
 #pragma unroll
@@ -255,6 +268,69 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
 // ---------------------------------------------------------------------------
 // grad_k and grad_v: 32 keys across to a wavefront, tiles of rows
 // ---------------------------------------------------------------------------
+// float16's factors (above) for rows r0 .. r1 - 1 of a problem: 2^up and 2^up times `more`.
+__device__ __forceinline__ void factors(const Backward &p, int64_t problem, int r0, int r1, float (&shared)[2][4],
+                                        float &up, float &more)
+{
+    const int tid = threadIdx.x, wave = tid >> 6;
+    float most_l = 0.0f, most_g = 0.0f;
+    const float *at = p.largest + problem * p.row_tiles * 2;
+    const int s1 = min(p.row_tiles, (r1 + kRowTile - 1) / kRowTile);
+    for (int s = r0 / kRowTile + tid; s < s1; s += 256) {
+        most_l = __builtin_fmaxf(most_l, at[2 * s]);
+        most_g = __builtin_fmaxf(most_g, at[2 * s + 1]);
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        most_l = __builtin_fmaxf(most_l, __shfl_xor(most_l, o));
+        most_g = __builtin_fmaxf(most_g, __shfl_xor(most_g, o));
+    }
+    if ((tid & 63) == 0) {
+        shared[0][wave] = most_l;
+        shared[1][wave] = most_g;
+    }
+    __syncthreads();
+    most_l = __builtin_fmaxf(__builtin_fmaxf(shared[0][0], shared[0][1]), __builtin_fmaxf(shared[0][2], shared[0][3]));
+    most_g = __builtin_fmaxf(__builtin_fmaxf(shared[1][0], shared[1][1]), __builtin_fmaxf(shared[1][2], shared[1][3]));
+    // weights reach 2^6 times 1 / l and g v^T - delta 2 |g| |v|: an eighth of one leaves |v|
+    // up to 4000 (as in grad_q's kernel)
+    up = most_l > 0.0f ? -__builtin_ceilf(log2_fast(most_l)) : 0.0f;
+    const float down = most_g > 0.0f && most_g < __builtin_inff() ? -__builtin_ceilf(log2_fast(most_g)) - 3.0f : 0.0f;
+    more = exp2_fast(within_range(down - up));
+}
+
+// A key's gradients of a wavefront (both halves' channels), or its part of them.
+template <int DT, int DP>
+__device__ __forceinline__ void put_key(const Backward &p, int b, int g, int split, int key, bool key_there, float up,
+                                        float more, const f32x16 (&ok)[DP / 32], const f32x16 (&ov)[DP / 32], int h)
+{
+    constexpr int ES = elem_size(DT), DB = DP / 32;
+    if (key >= p.Lk) return;
+    const float back_v = exp2_fast(-up), back_k = back_v * p.scale / more;
+    const int64_t at = ((int64_t)b * p.Lk + key) * p.Hk + g, all_keys = (int64_t)p.B * p.Lk * p.Hk;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            float a[8], w[8];
+            columns_of(ok[d], q, a);
+            columns_of(ov[d], q, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {   // (a key that is left out has sums of no meaning)
+                a[i] = key_there ? a[i] * back_k : 0.0f;
+                w[i] = key_there ? w[i] * back_v : 0.0f;
+            }
+            const int ch = d * 32 + 16 * q + 8 * h;
+            if (p.splits > 1) {
+                store_elems<FLASHBEV_F32>(p.part + (split * all_keys + at) * DP + ch, a);
+                store_elems<FLASHBEV_F32>(p.part + ((p.splits + split) * all_keys + at) * DP + ch, w);
+            } else {
+                put8<DT>(p.gk + at * p.D * ES, ch, p.D, a);
+                put8<DT>(p.gv + at * p.D * ES, ch, p.D, w);
+            }
+        }
+}
+
 template <int DT, int DP>
 struct ShapeK {
     static constexpr int BK = 128;
@@ -269,7 +345,7 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
 {
     using S = ShapeK<DT, DP>;
     using P = typename S::P;
-    constexpr int ES = elem_size(DT), DB = DP / 32;
+    constexpr int DB = DP / 32;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ float shared[2][4];
 
@@ -294,32 +370,7 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
 
     // the factors of p and dS: 2^up and 2^up times `more`
     float up = 0.0f, more = 1.0f;
-    if constexpr (DT == FLASHBEV_F16) {
-        float most_l = 0.0f, most_g = 0.0f;
-        const float *at = p.largest + problem * p.row_tiles * 2;
-        const int s0 = t0 * S::BR / kRowTile, s1 = min(p.row_tiles, (t1 * S::BR + kRowTile - 1) / kRowTile);
-        for (int s = s0 + tid; s < s1; s += 256) {
-            most_l = __builtin_fmaxf(most_l, at[2 * s]);
-            most_g = __builtin_fmaxf(most_g, at[2 * s + 1]);
-        }
-#pragma unroll
-        for (int o = 1; o < 64; o *= 2) {
-            most_l = __builtin_fmaxf(most_l, __shfl_xor(most_l, o));
-            most_g = __builtin_fmaxf(most_g, __shfl_xor(most_g, o));
-        }
-        if (lane == 0) {
-            shared[0][wave] = most_l;
-            shared[1][wave] = most_g;
-        }
-        __syncthreads();
-        most_l = __builtin_fmaxf(__builtin_fmaxf(shared[0][0], shared[0][1]), __builtin_fmaxf(shared[0][2], shared[0][3]));
-        most_g = __builtin_fmaxf(__builtin_fmaxf(shared[1][0], shared[1][1]), __builtin_fmaxf(shared[1][2], shared[1][3]));
-        // weights reach 2^4 times 1 / l and g v^T - delta 2 |g| |v|: an eighth of one leaves |v|
-        // up to 16000
-        up = most_l > 0.0f ? -__builtin_ceilf(log2_fast(most_l)) : 0.0f;
-        const float down = most_g > 0.0f && most_g < __builtin_inff() ? -__builtin_ceilf(log2_fast(most_g)) - 3.0f : 0.0f;
-        more = exp2_fast(within_range(down - up));
-    }
+    if constexpr (DT == FLASHBEV_F16) factors(p, problem, t0 * S::BR, t1 * S::BR, shared, up, more);
 
     u32x4 kf[P::CHUNKS], vf[P::CHUNKS];
     const int64_t key_at = min(key, p.Lk - 1);
@@ -449,30 +500,411 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
             }
         }
     }
-    if (key >= p.Lk) return;
-    const float back_v = exp2_fast(-up), back_k = back_v * p.scale / more;
-    const int64_t at = ((int64_t)b * p.Lk + key) * p.Hk + g, all_keys = (int64_t)p.B * p.Lk * p.Hk;
+    put_key<DT, DP>(p, b, g, split, key, key_there, up, more, ok, ov, h);
+}
+
+// ---------------------------------------------------------------------------
+// without masks: loads that pass no registers, and one step's vector instructions among the
+// products of the next and the last one, as the forward's attend_flow
+// ---------------------------------------------------------------------------
+template <int DT, int DP>
+struct FlowQ {
+    static constexpr int TK = DP * elem_size(DT) <= 64 ? 128 : 64;
+    static constexpr int SUBS = TK / 32;
+    using T = Strip<DT, DP, TK>;
+    static constexpr int LDS = 5 * T::BYTES;   // V of two tiles and K of three
+    static constexpr bool FITS = LDS <= 131072;   // a load's reach
+};
+
+constexpr int grad_q_waves(int dt, int dp)
+{
+    return dp * elem_size(dt) <= 64 ? 3 : dp * elem_size(dt) <= 256 ? 2 : 1;
+}
+
+template <int DT, int DP>
+__global__ void __launch_bounds__(256, grad_q_waves(DT, DP)) attend_grad_q_flow(Backward p)
+{
+    using F = FlowQ<DT, DP>;
+    using T = typename F::T;
+    constexpr int ES = elem_size(DT), DB = DP / 32, PAIRS = 8, E = T::E;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+
+    uint32_t id = item_of(p);
+    if (id >= p.blocks) return;
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tile = id % p.tiles;
+    id /= p.tiles;
+    const int split = id % p.splits;
+    id /= p.splits;
+    const int g = id % p.Hk, b = id / p.Hk;
+    const int len = p.keys(b);
+    const int all = (len + F::TK - 1) / F::TK, per = (all + p.splits - 1) / p.splits;
+    const int t0 = split * per, t1 = min(all, t0 + per), end = min(len, t1 * F::TK);
+
+    const int r = tile * 128 + wave * 32 + (lane & 31);
+    const bool row_there = r < p.rows;
+    int qi, qj;
+    p.row(min(r, p.rows - 1), qi, qj);
+    const int head = g * p.share + qj;
+    u32x4 qf[T::CHUNKS], gf[T::CHUNKS];
+    row_fragments<DT, DP>(qf, p.q + b * p.qb + qi * p.qr + head * p.qh, row_there, p.D, lane);
+    row_fragments<DT, DP>(gf, p.g + b * p.ob + qi * p.orow + head * p.oh, row_there, p.D, lane);
+    const RowData row = p.data[((int64_t)b * p.Hk + g) * p.rows + min(r, p.rows - 1)];
+    const float c = p.scale * kLog2, mc = row.m * kLog2;   // weights are p l
+    const float inv = row.norm > 0.0f ? 0.125f / row.norm : 1.0f, off = -row.delta * inv;
+
+    f32x16 o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = zeros16();
+
+    typename T::Reader read;
+    read.start(lane);
+    typename T::Loader kl, vl;
+    kl.start(wave, lane, p.D, p.kr);
+    vl.start(wave, lane, p.D, p.vr);
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds);
+    const char *kbase = p.k + b * p.kb + g * p.kh, *vbase = p.v + b * p.vb + g * p.vh;
+    const auto v_at = [&](int t) { return (t & 1) * T::BYTES; };
+    const auto load = [&](int t, int k_at) {
+        kl.load(kbase + t * F::TK * p.kr, len - t * F::TK, lds0 + k_at, wave);
+        vl.load(vbase + t * F::TK * p.vr, len - t * F::TK, lds0 + v_at(t), wave);
+    };
+
+    // One step on scores x and products y of g with v: w, the packed dS; next_x and next_y of the 32
+    // keys at lk and lv; and the product of the last step's dS with the 32 rows of k at lk0.
+    const auto step = [&](auto first, f32x16 &x, f32x16 &y, f32x16 &next_x, f32x16 &next_y, u32x4(&w)[T::STEPS],
+                          const u32x4(&last)[T::STEPS], const char *lk, const char *lv, const char *lk0, int key0) {
+        constexpr bool FIRST = decltype(first)::value;
+        constexpr int NS = T::CHUNKS, NP = T::STEPS * DB, N = 3 * NS, AHEAD = NS < 8 ? 3 : 2, Q = (PAIRS + NS - 1) / NS;
+        static_assert(NS == NP, "as many products of each kind");
+        const auto fragment = [&](int i) {
+            return i % 3 == 0   ? read.along(lk, 0, i / 3)
+                   : i % 3 == 1 ? read.along(lv, 0, i / 3)
+                                : read.across(lk0, 0, i / 3 / DB, i / 3 % DB * 32);
+        };
+        if (key0 + 32 > end) cut_keys(x, key0, h, end);
+        float v[16];
+        u32x4 f[AHEAD];
+        next_x = zeros16();
+        next_y = zeros16();
+        asm volatile("" : "+v"(read.along_turn), "+v"(read.across_turn));
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (!FIRST || i % 3 != 2) f[i] = fragment(i);
+#pragma unroll
+        for (int i = 0; i < N + 6; ++i) {
+            if (i < N) {
+                if (i % 3 == 0) {
+                    mma<DT>(next_x, f[i % AHEAD], qf[i / 3 % NS]);
+                } else if (i % 3 == 1) {
+                    mma<DT>(next_y, f[i % AHEAD], gf[i / 3 % NS]);
+                } else if constexpr (!FIRST) {
+                    mma<DT>(o[i / 3 % DB], f[i % AHEAD], last[i / 3 / DB % T::STEPS]);
+                }
+            }
+            if (i + AHEAD < N && (!FIRST || (i + AHEAD) % 3 != 2)) f[i % AHEAD] = fragment(i + AHEAD);
+            if (i % 3 == 0) {   // (few iterations: the compiler unrolls so much and no more)
+#pragma unroll
+                for (int n = 0; n < Q; ++n) {
+                    if (const int j = (i / 3 - 2) * Q + n; j >= 0 && j < PAIRS) {
+                        const int u = 2 * j / E, k = 2 * j % E;
+                        v[2 * j] *= __builtin_fmaf(y[2 * j], inv, off);
+                        v[2 * j + 1] *= __builtin_fmaf(y[2 * j + 1], inv, off);
+                        if constexpr (DT == FLASHBEV_F32) {
+                            w[u][k] = __builtin_bit_cast(uint32_t, v[2 * j]);
+                            w[u][k + 1] = __builtin_bit_cast(uint32_t, v[2 * j + 1]);
+                        } else {
+                            w[u][k / 2] = pack2<DT>(v[2 * j], v[2 * j + 1]);
+                        }
+                    }
+                    if (const int j = (i / 3 - 1) * Q + n; j >= 0 && j < PAIRS) {
+                        v[2 * j] = exp2_fast(v[2 * j]);
+                        v[2 * j + 1] = exp2_fast(v[2 * j + 1]);
+                    }
+                    if (const int j = i / 3 * Q + n; j < PAIRS) {
+                        v[2 * j] = __builtin_fmaf(x[2 * j], c, -mc);
+                        v[2 * j + 1] = __builtin_fmaf(x[2 * j + 1], c, -mc);
+                    }
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    if (t0 < t1) {
+        int k_now = 2 * T::BYTES, k_next = 3 * T::BYTES, k_free = 4 * T::BYTES;   // K of tiles t, t + 1, t + 2
+        load(t0, k_now);
+        if (t0 + 1 < t1) load(t0 + 1, k_next);
+        meet();
+        f32x16 x[2], y[2];
+        u32x4 w[2][T::STEPS];
+        x[0] = zeros16();
+        y[0] = zeros16();
+#pragma unroll
+        for (int e = 0; e < T::CHUNKS; ++e) {
+            mma<DT>(x[0], read.along(lds + k_now, 0, e), qf[e]);
+            mma<DT>(y[0], read.along(lds + v_at(t0), 0, e), gf[e]);
+        }
+        step(std::true_type{}, x[0], y[0], x[1], y[1], w[0], w[1], lds + k_now + 32 * T::ROW,
+             lds + v_at(t0) + 32 * T::ROW, lds, t0 * F::TK);
+        for (int t = t0; t < t1; ++t) {
+            // steps 1, 2, .. of the tile and step 0 of the next one, as the forward's
+            const char *lk = lds + k_now, *lk2 = lds + k_next, *lv = lds + v_at(t), *lv2 = lds + v_at(t + 1);
+#pragma unroll
+            for (int s = 1; s <= F::SUBS; ++s) {
+                if (s == F::SUBS - 1) {
+                    meet();
+                    if (t + 2 < t1) load(t + 2, k_free);
+                }
+                const int n = (s + 1) % F::SUBS * 32 * T::ROW;
+                step(std::false_type{}, x[s & 1], y[s & 1], x[s + 1 & 1], y[s + 1 & 1], w[s & 1], w[s + 1 & 1],
+                     (s + 1 < F::SUBS ? lk : lk2) + n, (s + 1 < F::SUBS ? lv : lv2) + n, lk + (s - 1) * 32 * T::ROW,
+                     t * F::TK + s * 32);
+            }
+            const int turn = k_now;
+            k_now = k_next;
+            k_next = k_free;
+            k_free = turn;
+        }
+    }
+    if (!row_there) return;
+    const float back = p.scale * exp2_fast(-row.log2l) / inv;
+    const int64_t at = ((int64_t)b * p.Lq + qi) * p.H + head;
+    const int64_t slot = ((int64_t)split * p.B * p.Lq * p.H + at) * DP;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            float a[8], w[8];
-            columns_of(ok[d], q, a);
-            columns_of(ov[d], q, w);
+            float v[8];
+            columns_of(o[d], q, v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {   // (a key that is left out has sums of no meaning)
-                a[i] = key_there ? a[i] * back_k : 0.0f;
-                w[i] = key_there ? w[i] * back_v : 0.0f;
-            }
-            const int ch = d * 32 + 16 * q + 8 * h;
+            for (int i = 0; i < 8; ++i) v[i] *= back;
             if (p.splits > 1) {
-                store_elems<FLASHBEV_F32>(p.part + (split * all_keys + at) * DP + ch, a);
-                store_elems<FLASHBEV_F32>(p.part + ((p.splits + split) * all_keys + at) * DP + ch, w);
+                store_elems<FLASHBEV_F32>(p.part + slot + d * 32 + 16 * q + 8 * h, v);
             } else {
-                put8<DT>(p.gk + at * p.D * ES, ch, p.D, a);
-                put8<DT>(p.gv + at * p.D * ES, ch, p.D, w);
+                put8<DT>(p.gq + at * p.D * ES, d * 32 + 16 * q + 8 * h, p.D, v);
             }
         }
+}
+
+template <int DT, int DP>
+struct FlowK {
+    static constexpr int TR = DP * elem_size(DT) <= 64 ? 128 : 64;
+    static constexpr int SUBS = TR / 32;
+    using T = Strip<DT, DP, TR>;
+    static constexpr int DATA = TR * 8;          // the rows' exponents and deltas
+    static constexpr int STAGE = 2 * T::BYTES + DATA, LDS = 3 * STAGE;
+    // Heads of up to 32 16-bit channels have vector instructions for twice the products' time, and
+    // four wavefronts a SIMD of attend_grad_kv do them faster than two of this kernel: 900
+    // queries x 40000 states 115 us and 131.
+    static constexpr bool FITS = LDS <= 131072 && DP * elem_size(DT) > 64;
+};
+
+constexpr int grad_kv_waves(int dt, int dp)
+{
+    return dp * elem_size(dt) <= 128 ? 2 : 1;
+}
+
+template <int DT, int DP>
+__global__ void __launch_bounds__(256, grad_kv_waves(DT, DP)) attend_grad_kv_flow(Backward p)
+{
+    using F = FlowK<DT, DP>;
+    using T = typename F::T;
+    constexpr int DB = DP / 32, PAIRS = 8, E = T::E;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float shared[2][4];
+
+    uint32_t id = item_of(p);
+    if (id >= p.blocks) return;
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tile = id % p.tiles;
+    id /= p.tiles;
+    const int split = id % p.splits;
+    id /= p.splits;
+    const int g = id % p.Hk, b = id / p.Hk;
+    const int64_t problem = (int64_t)b * p.Hk + g;
+    const int len = p.keys(b);
+    const int key = tile * 128 + wave * 32 + (lane & 31);
+    const bool key_there = key < len;
+
+    const int all = tile * 128 < len ? (p.rows + F::TR - 1) / F::TR : 0;
+    const int per = (all + p.splits - 1) / p.splits;
+    const int t0 = split * per, t1 = min(all, t0 + per);
+    float up = 0.0f, more = 1.0f;
+    if constexpr (DT == FLASHBEV_F16) {
+        factors(p, problem, t0 * F::TR, t1 * F::TR, shared, up, more);
+    }
+
+    u32x4 kf[T::CHUNKS], vf[T::CHUNKS];
+    const int64_t key_at = min(key, p.Lk - 1);
+    row_fragments<DT, DP>(kf, p.k + b * p.kb + g * p.kh + key_at * p.kr, key_there, p.D, lane);
+    row_fragments<DT, DP>(vf, p.v + b * p.vb + g * p.vh + key_at * p.vr, key_there, p.D, lane);
+    const float c = p.scale * kLog2;
+
+    f32x16 ok[DB], ov[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) ok[d] = ov[d] = zeros16();
+
+    typename T::Reader read;
+    read.start(lane);
+    typename T::RowLoader ql, gl;
+    ql.start(wave, lane);
+    gl.start(wave, lane);
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds);
+    const char *qbase = p.q + b * p.qb + (int64_t)g * p.share * p.qh;
+    const char *gbase = p.g + b * p.ob + (int64_t)g * p.share * p.oh;
+    const float *lose = p.lose + problem * p.padded, *delta = p.delta + problem * p.padded;
+    const bool even = F::TR % p.share == 0;   // a thread's places are the same in every tile
+    const auto load = [&](int t, int stage) {
+        const int r0 = t * F::TR, i0 = r0 / p.share;
+        if (t == t0 || !even || r0 + F::TR > p.rows) {
+            ql.places(p, r0, i0, p.qr, p.qh);
+            gl.places(p, r0, i0, p.orow, p.oh);
+        }
+        ql.load(qbase + i0 * p.qr, p.D, lds0 + stage, wave);
+        gl.load(gbase + i0 * p.orow, p.D, lds0 + stage + T::BYTES, wave);
+        if (wave < 2 * F::TR / 64) {   // exponents, then deltas, 64 rows to an instruction
+            const int part = wave * 64 % F::TR;
+            word_to_lds((wave * 64 < F::TR ? lose : delta) + r0 + part + lane, lds0 + stage + 2 * T::BYTES + wave * 256);
+        }
+    };
+
+    // One step on scores x and products y of the rows' g with v: wp and ws, the packed p and dS;
+    // next_x and next_y of the 32 rows at lq and lg; and the products of the last step's p and dS
+    // with the 32 rows at lq0 and lg0.
+    const auto step = [&](auto first, f32x16 &x, f32x16 &y, f32x16 &next_x, f32x16 &next_y, u32x4(&wp)[T::STEPS],
+                          u32x4(&ws)[T::STEPS], const u32x4(&last_p)[T::STEPS], const u32x4(&last_s)[T::STEPS],
+                          const char *lq, const char *lg, const char *lq0, const char *lg0, const float *data) {
+        constexpr bool FIRST = decltype(first)::value;
+        constexpr int NS = T::CHUNKS, NP = T::STEPS * DB, N = 4 * NS, AHEAD = 4, Q = (PAIRS + NS - 1) / NS;
+        static_assert(NS == NP, "as many products of each kind");
+        const auto fragment = [&](int i) {
+            return i % 4 == 0   ? read.along(lq, 0, i / 4)
+                   : i % 4 == 1 ? read.along(lg, 0, i / 4)
+                   : i % 4 == 2 ? read.across(lg0, 0, i / 4 / DB, i / 4 % DB * 32)
+                                : read.across(lq0, 0, i / 4 / DB, i / 4 % DB * 32);
+        };
+        float v[16];
+        u32x4 f[AHEAD];
+        f32x4 e4[4], d4[4];
+        next_x = zeros16();
+        next_y = zeros16();
+        asm volatile("" : "+v"(read.along_turn), "+v"(read.across_turn));
+        const float *rows = data + 4 * h;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (!FIRST || i % 4 < 2) f[i] = fragment(i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (2 * k / Q == 0) {
+                e4[k] = *reinterpret_cast<const f32x4 *>(rows + 8 * k);
+                d4[k] = *reinterpret_cast<const f32x4 *>(rows + F::TR + 8 * k);
+            }
+#pragma unroll
+        for (int i = 0; i < N + 8; ++i) {
+            if (i < N) {
+                if (i % 4 == 0) {
+                    mma<DT>(next_x, f[i % AHEAD], kf[i / 4 % NS]);
+                } else if (i % 4 == 1) {
+                    mma<DT>(next_y, f[i % AHEAD], vf[i / 4 % NS]);
+                } else if constexpr (!FIRST) {
+                    if (i % 4 == 2) {
+                        mma<DT>(ov[i / 4 % DB], f[i % AHEAD], last_p[i / 4 / DB % T::STEPS]);
+                    } else {
+                        mma<DT>(ok[i / 4 % DB], f[i % AHEAD], last_s[i / 4 / DB % T::STEPS]);
+                    }
+                }
+            }
+            if (i + AHEAD < N && (!FIRST || (i + AHEAD) % 4 < 2)) f[i % AHEAD] = fragment(i + AHEAD);
+            if (i % 4 == 0) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)   // the next pairs' rows
+                    if (2 * k / Q > 0 && 2 * k / Q == i / 4 + 1) {
+                        e4[k] = *reinterpret_cast<const f32x4 *>(rows + 8 * k);
+                        d4[k] = *reinterpret_cast<const f32x4 *>(rows + F::TR + 8 * k);
+                    }
+            }
+            if (i % 2 == 0) {
+#pragma unroll
+                for (int n = 0; n < Q; ++n) {
+                    if (const int j = (i / 4 - 2) * Q + n; i % 4 == 0 && j >= 0 && j < PAIRS) {
+                        const int u = 2 * j / E, at = 2 * j % E;
+                        float s[2];
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            s[q] = v[2 * j + q] * (y[2 * j + q] - d4[j / 2][2 * j % 4 + q]);
+                            if (DT == FLASHBEV_F16) s[q] *= more;
+                        }
+                        if constexpr (DT == FLASHBEV_F32) {
+#pragma unroll
+                            for (int q = 0; q < 2; ++q) {
+                                wp[u][at + q] = __builtin_bit_cast(uint32_t, v[2 * j + q]);
+                                ws[u][at + q] = __builtin_bit_cast(uint32_t, s[q]);
+                            }
+                        } else {
+                            wp[u][at / 2] = pack2<DT>(v[2 * j], v[2 * j + 1]);
+                            ws[u][at / 2] = pack2<DT>(s[0], s[1]);
+                        }
+                    }
+                    if (const int j = (i / 4 - 1) * Q + n; i % 4 == 2 && j >= 0 && j < PAIRS) {
+                        v[2 * j] = exp2_fast(v[2 * j]);
+                        v[2 * j + 1] = exp2_fast(v[2 * j + 1]);
+                    }
+                    if (const int j = i / 4 * Q + n; i % 4 == 0 && j < PAIRS) {
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const float e = e4[j / 2][2 * j % 4 + q];   // (a pair's rows in their four)
+                            v[2 * j + q] = __builtin_fmaf(x[2 * j + q], c, DT == FLASHBEV_F16 ? up - e : -e);
+                        }
+                    }
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    if (t0 < t1) {
+        int now = 0, next = F::STAGE, free = 2 * F::STAGE;   // of tiles t, t + 1, t + 2
+        load(t0, now);
+        if (t0 + 1 < t1) load(t0 + 1, next);
+        meet();
+        f32x16 x[2], y[2];
+        u32x4 wp[2][T::STEPS], ws[2][T::STEPS];
+        x[0] = zeros16();
+        y[0] = zeros16();
+#pragma unroll
+        for (int e = 0; e < T::CHUNKS; ++e) {
+            mma<DT>(x[0], read.along(lds + now, 0, e), kf[e]);
+            mma<DT>(y[0], read.along(lds + now + T::BYTES, 0, e), vf[e]);
+        }
+        constexpr int D0 = 2 * T::BYTES;
+        step(std::true_type{}, x[0], y[0], x[1], y[1], wp[0], ws[0], wp[1], ws[1], lds + now + 32 * T::ROW,
+             lds + now + T::BYTES + 32 * T::ROW, lds, lds, reinterpret_cast<const float *>(lds + now + D0));
+        for (int t = t0; t < t1; ++t) {
+            // Steps 1, 2, .. of the tile and step 0 of the next one (past the last tile for the last
+            // step's products alone: its weights, of whatever lies there, are not used).
+            const char *l0 = lds + now, *l1 = lds + next;
+#pragma unroll
+            for (int s = 1; s <= F::SUBS; ++s) {
+                if (s == F::SUBS - 1) {
+                    meet();
+                    if (t + 2 < t1) load(t + 2, free);
+                }
+                const char *ln = (s + 1 < F::SUBS ? l0 : l1) + (s + 1) % F::SUBS * 32 * T::ROW;
+                const char *lp = l0 + (s - 1) * 32 * T::ROW;
+                const float *data = reinterpret_cast<const float *>((s < F::SUBS ? l0 : l1) + D0) + s % F::SUBS * 32;
+                step(std::false_type{}, x[s & 1], y[s & 1], x[s + 1 & 1], y[s + 1 & 1], wp[s & 1], ws[s & 1],
+                     wp[s + 1 & 1], ws[s + 1 & 1], ln, ln + T::BYTES, lp, lp + T::BYTES, data);
+            }
+            const int turn = now;
+            now = next;
+            next = free;
+            free = turn;
+        }
+    }
+    put_key<DT, DP>(p, b, g, split, key, key_there, up, more, ok, ov, h);
 }
 
 // The sums of the splits' rows [n][DP], four channels to a lane.
@@ -506,7 +938,7 @@ __global__ void __launch_bounds__(256) attend_sum(Sum p)
 // host
 // ---------------------------------------------------------------------------
 struct Plan {
-    int dp, row_tiles;
+    int dp, row_tiles, padded;
     bool any;
     int q_tiles, q_splits;
     int k_tiles, k_splits;
@@ -526,7 +958,8 @@ Plan plan_of(const flashlayer_attention *a)
     const int64_t rows = (int64_t)a->Lq * (a->Hk ? a->H / a->Hk : 1), problems = (int64_t)a->B * a->Hk;
     p.dp = padded_head(a->D);
     p.any = any_of(a);
-    p.row_tiles = (int)((rows + kRowTile - 1) / kRowTile);
+    p.padded = (int)((rows + 127) / 128 * 128);
+    p.row_tiles = p.padded / kRowTile;
     p.q_tiles = (int)((rows + 127) / 128);
     p.q_splits = splits_of(problems * p.q_tiles, (a->Lk + 63) / 64);
     p.k_tiles = (a->Lk + 127) / 128;
@@ -537,6 +970,12 @@ Plan plan_of(const flashlayer_attention *a)
 uint64_t data_bytes(const flashlayer_attention *a)
 {
     return align256((uint64_t)a->B * a->Lq * a->H * sizeof(RowData));
+}
+
+// the exponents and deltas for the kernel without masks
+uint64_t rows_bytes(const flashlayer_attention *a, const Plan &p)
+{
+    return align256((uint64_t)a->B * a->Hk * p.padded * 4);
 }
 
 uint64_t largest_bytes(const flashlayer_attention *a, const Plan &p)
@@ -553,7 +992,7 @@ uint64_t backward_bytes(const flashlayer_attention *a, bool want_q, bool want_kv
         q = size_prod({(uint64_t)p.q_splits, (uint64_t)a->B * a->Lq * a->H, (uint64_t)p.dp, 4});
     if (want_kv && p.k_splits > 1)
         kv = size_prod({2, (uint64_t)p.k_splits, (uint64_t)a->B * a->Lk * a->Hk, (uint64_t)p.dp, 4});
-    return data_bytes(a) + largest_bytes(a, p) + align256(std::max(q, kv));
+    return data_bytes(a) + 2 * rows_bytes(a, p) + largest_bytes(a, p) + align256(std::max(q, kv));
 }
 
 template <int DT, int DP>
@@ -564,8 +1003,15 @@ int run(Backward &p, const Plan &plan, hipStream_t st)
         p.tiles = plan.q_tiles;
         p.splits = plan.q_splits;
         if (const int rc = deal(p, size_prod({problems, (uint64_t)p.tiles, (uint64_t)p.splits}))) return rc;
-        const void *fn = plan.any ? (const void *)attend_grad_q<DT, DP, true> : (const void *)attend_grad_q<DT, DP, false>;
-        if (const int rc = launch_lds(fn, 8ull * p.per_xcd, p, ShapeQ<DT, DP>::LDS, st)) return rc;
+        const void *fn = (const void *)attend_grad_q<DT, DP, true>;
+        size_t lds = ShapeQ<DT, DP>::LDS;
+        if constexpr (FlowQ<DT, DP>::FITS) {
+            if (!plan.any) {
+                fn = (const void *)attend_grad_q_flow<DT, DP>;
+                lds = FlowQ<DT, DP>::LDS;
+            }
+        }
+        if (const int rc = launch_lds(fn, 8ull * p.per_xcd, p, lds, st)) return rc;
         if (p.splits > 1) {
             Sum s{p.part, p.gq, (int64_t)problems * p.rows, p.splits, p.D};
             const uint64_t lanes = (uint64_t)s.n * (DP / 4);
@@ -576,8 +1022,18 @@ int run(Backward &p, const Plan &plan, hipStream_t st)
     p.tiles = plan.k_tiles;
     p.splits = plan.k_splits;
     if (const int rc = deal(p, size_prod({problems, (uint64_t)p.tiles, (uint64_t)p.splits}))) return rc;
-    const void *fn = plan.any ? (const void *)attend_grad_kv<DT, DP, true> : (const void *)attend_grad_kv<DT, DP, false>;
-    if (const int rc = launch_lds(fn, 8ull * p.per_xcd, p, ShapeK<DT, DP>::LDS, st)) return rc;
+    const void *fn = (const void *)attend_grad_kv<DT, DP, true>;
+    size_t lds = ShapeK<DT, DP>::LDS;
+    if constexpr (DP * elem_size(DT) <= 64) {
+        if (!plan.any) fn = (const void *)attend_grad_kv<DT, DP, false>;
+    }
+    if constexpr (FlowK<DT, DP>::FITS) {
+        if (!plan.any) {
+            fn = (const void *)attend_grad_kv_flow<DT, DP>;
+            lds = FlowK<DT, DP>::LDS;
+        }
+    }
+    if (const int rc = launch_lds(fn, 8ull * p.per_xcd, p, lds, st)) return rc;
     if (p.splits <= 1) return FLASHBEV_OK;
     for (int half = 0; half < 2; ++half) {
         Sum s{p.part, half ? p.gv : p.gk, (int64_t)problems * p.Lk, p.splits, p.D};
@@ -664,10 +1120,16 @@ extern "C" int flashlayer_attention_backward(const flashlayer_attention *args, c
     p.gk = static_cast<char *>(grad_k);
     p.gv = static_cast<char *>(grad_v);
     p.row_tiles = plan.row_tiles;
+    p.padded = plan.padded;
     char *ws = static_cast<char *>(workspace);
     p.data = reinterpret_cast<RowData *>(ws);
-    p.largest = reinterpret_cast<float *>(ws + data_bytes(args));
-    p.part = reinterpret_cast<float *>(ws + data_bytes(args) + largest_bytes(args, plan));
+    ws += data_bytes(args);
+    p.lose = reinterpret_cast<float *>(ws);
+    ws += rows_bytes(args, plan);
+    p.delta = reinterpret_cast<float *>(ws);
+    ws += rows_bytes(args, plan);
+    p.largest = reinterpret_cast<float *>(ws);
+    p.part = reinterpret_cast<float *>(ws + largest_bytes(args, plan));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (a.dtype == FLASHBEV_F32) return run_width<FLASHBEV_F32>(p, plan, st);
     return a.dtype == FLASHBEV_F16 ? run_width<FLASHBEV_F16>(p, plan, st) : run_width<FLASHBEV_BF16>(p, plan, st);

@@ -63,8 +63,8 @@ def attention(q, k, v, scale=None, mask=None, key_lengths=None, grad_out=None):
     # much in the sum that it is divided by.
     ds = torch.where(p > 0, size, 0.0).amax(-1, keepdim=True) * (D + 4) * U32 * 2 if n else 0.0
     rel = 2 * (ds + 8 * U32) + (2 * h if q.dtype != torch.float32 else 0.0) + 2 * n * U32
-    # float16 below its normal numbers: half a step is 2^-25, of weights whose largest is one
-    # or (where a reference lags) up to 2^4
+    # float16 below its normal numbers: half a step is 2^-25, of weights whose largest is at
+    # least one; of dS of a row over 8 |g|; of p and dS of all rows brought to at least 1 / 2 and 1 / 16
     tiny = 2.0 ** -25 if q.dtype == torch.float16 else 0.0
     size_o = torch.matmul(p, v64.abs())
     err_o = size_o * rel + n * tiny * peak * v64.abs().amax(-2, keepdim=True) if n and v64.shape[-2] else size_o * 0
@@ -91,7 +91,7 @@ def attention(q, k, v, scale=None, mask=None, key_lengths=None, grad_out=None):
     q64 = q.detach().double().transpose(1, 2)
     res["grad_q"] = scale * torch.matmul(d, kt)
     tol["grad_q"] = scale * (torch.matmul(err_d + n * U32 * d.abs(), kt.abs())
-                             + n * tiny * 2 * peak * norm * kt.abs().amax(-2, keepdim=True))
+                             + n * tiny * 8 * peak * norm * kt.abs().amax(-2, keepdim=True))
     res["grad_k"] = scale * torch.matmul(d.transpose(2, 3).contiguous(), q64)
     tol["grad_k"] = scale * torch.matmul((err_d + rows * U32 * d.abs()).transpose(2, 3).contiguous(), q64.abs())
     res["grad_v"] = torch.matmul(p.transpose(2, 3).contiguous(), gt)
