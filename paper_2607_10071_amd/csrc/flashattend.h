@@ -396,67 +396,127 @@ __device__ __forceinline__ void row_fragments(u32x4 (&f)[N], const char *row, bo
 // masks
 // ---------------------------------------------------------------------------
 typedef uint32_t u32_any __attribute__((aligned(1)));
+typedef u32x4 u32x4_f __attribute__((aligned(4)));
 
-// Scores x of keys key0 + 8 k + 4 h + i of a lane's row, scaled and masked: x = scale x + mask
-// (without a mask too: the kernels with masks serve odd widths).
-// `row` is the mask's row; Lk its length.
-__device__ __forceinline__ void mask_row(const Attend &p, f32x16 &x, const char *row, int key0, int h)
-{
-    const bool whole = key0 + 32 <= p.Lk;
+constexpr int kAddF16 = 16 + FLASHLAYER_MASK_ADD, kAddBf16 = 32 + FLASHLAYER_MASK_ADD;   // kinds
+
+// A block's mask as it is stored.  Its loads are issued before the block's products and used
+// behind them.
+struct MaskBlock {
+    u32x4 w[4];
+
+    // Keys key0 + 8 k + 4 h + 0 .. 3 for k = 0 .. 3 of a lane's row; Lk keys to a row.
+    __device__ __forceinline__ void load_row(const Attend &p, const char *row, int key0, int h)
+    {
+        if (p.kind == FLASHLAYER_MASK_NONE) return;
+        const bool whole = key0 + 32 <= p.Lk;
+        const int size = p.kind == FLASHLAYER_MASK_BOOL ? 1 : p.kind == FLASHLAYER_MASK_ADD_F32 ? 4 : 2;
+        const char *at = row + (int64_t)(key0 + 4 * h) * size;
+        if (!whole) {
+            asm volatile("");
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int key = key0 + 8 * k + 4 * h;
-        if (p.kind == FLASHLAYER_MASK_NONE) {
+            for (int k = 0; k < 4; ++k) {
+                u32x4 v = {0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[4 * k + i] *= p.scale;
-        } else if (p.kind == FLASHLAYER_MASK_BOOL) {
-            uint32_t w = 0;
-            if (whole) {
-                w = *reinterpret_cast<const u32_any *>(row + key);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (key + i < p.Lk) w |= (uint32_t)(uint8_t)row[key + i] << (8 * i);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                x[4 * k + i] = w >> (8 * i) & 0xff ? x[4 * k + i] * p.scale : -__builtin_inff();
-        } else {
-            float b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            const bool wide = p.kind == FLASHLAYER_MASK_ADD_F32;
-            if (wide) {
-                if (whole) {
-                    const f32x4 t = __builtin_bit_cast(f32x4, load16(row + (int64_t)key * 4));
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) b[i] = t[i];
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (key + i < p.Lk) b[i] = load_elem<FLASHBEV_F32>(row, key + i);
+                for (int i = 0; i < 4; ++i) {
+                    if (key0 + 8 * k + 4 * h + i >= p.Lk) continue;
+                    const char *e = at + (8 * k + i) * size;
+                    if (size == 1) {
+                        v[0] |= (uint32_t)(uint8_t)*e << (8 * i);
+                    } else if (size == 2) {
+                        v[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t *>(e) << (16 * (i & 1));
+                    } else {
+                        v[i] = *reinterpret_cast<const uint32_t *>(e);
+                    }
                 }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (key + i < p.Lk)
-                        b[i] = p.kind == FLASHLAYER_MASK_ADD + 16 ? load_elem<FLASHBEV_F16>(row, key + i)
-                                                                  : load_elem<FLASHBEV_BF16>(row, key + i);
+                w[k] = v;
             }
+        } else if (size == 1) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[4 * k + i] = __builtin_fmaf(x[4 * k + i], p.scale, b[i]);
+            for (int k = 0; k < 4; ++k) w[k][0] = *reinterpret_cast<const u32_any *>(at + 8 * k);
+        } else if (size == 2) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const u32x2 v = load8(at + 16 * k);
+                w[k][0] = v[0];
+                w[k][1] = v[1];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const u32x4_f *>(at + 32 * k);
         }
     }
-}
 
-// One place of a mask's row.
-__device__ __forceinline__ float mask_place(const Attend &p, float x, const char *row, int key)
-{
-    if (p.kind == FLASHLAYER_MASK_NONE) return x * p.scale;
-    if (p.kind == FLASHLAYER_MASK_BOOL) return row[key] ? x * p.scale : -__builtin_inff();
-    const float b = p.kind == FLASHLAYER_MASK_ADD_F32  ? load_elem<FLASHBEV_F32>(row, key)
-                    : p.kind == FLASHLAYER_MASK_ADD + 16 ? load_elem<FLASHBEV_F16>(row, key)
-                                                         : load_elem<FLASHBEV_BF16>(row, key);
-    return __builtin_fmaf(x, p.scale, b);
-}
+    // x = scale x + mask.  (Without a mask too: these kernels serve odd widths.)
+    __device__ __forceinline__ void apply_row(const Attend &p, f32x16 &x) const
+    {
+        if (p.kind == FLASHLAYER_MASK_NONE) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] *= p.scale;
+        } else if (p.kind == FLASHLAYER_MASK_BOOL) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                x[i] = w[i / 4][0] >> (8 * (i & 3)) & 0xff ? x[i] * p.scale : -__builtin_inff();
+        } else if (p.kind == FLASHLAYER_MASK_ADD_F32) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t v = w[i / 4][i & 3];
+                x[i] = __builtin_fmaf(x[i], p.scale, __builtin_bit_cast(float, v));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = __builtin_fmaf(x[i], p.scale, half_at(p, w[i / 4][i / 2 & 1] >> (16 * (i & 1))));
+        }
+    }
+
+    // One key of a lane, rows at `offsets` (in bytes, from `base`).
+    __device__ __forceinline__ void load_key(const Attend &p, const char *base, const int64_t *offsets, int key)
+    {
+        if (p.kind == FLASHLAYER_MASK_NONE) return;
+        if (p.kind == FLASHLAYER_MASK_BOOL) {
+            base += key;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                w[i / 4][i & 3] = *reinterpret_cast<const uint8_t *>(base + offsets[8 * (i >> 2) + (i & 3)]);
+        } else if (p.kind == FLASHLAYER_MASK_ADD_F32) {
+            base += (int64_t)key * 4;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                w[i / 4][i & 3] = *reinterpret_cast<const uint32_t *>(base + offsets[8 * (i >> 2) + (i & 3)]);
+        } else {
+            base += (int64_t)key * 2;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                w[i / 4][i & 3] = *reinterpret_cast<const uint16_t *>(base + offsets[8 * (i >> 2) + (i & 3)]);
+        }
+    }
+
+    __device__ __forceinline__ void apply_key(const Attend &p, f32x16 &x) const
+    {
+        if (p.kind == FLASHLAYER_MASK_NONE) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] *= p.scale;
+        } else if (p.kind == FLASHLAYER_MASK_BOOL) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = w[i / 4][i & 3] ? x[i] * p.scale : -__builtin_inff();
+        } else if (p.kind == FLASHLAYER_MASK_ADD_F32) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t v = w[i / 4][i & 3];
+                x[i] = __builtin_fmaf(x[i], p.scale, __builtin_bit_cast(float, v));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = __builtin_fmaf(x[i], p.scale, half_at(p, w[i / 4][i & 3]));
+        }
+    }
+
+    static __device__ __forceinline__ float half_at(const Attend &p, uint32_t w)
+    {
+        const uint16_t v = (uint16_t)w;
+        return p.kind == kAddF16 ? (float)__builtin_bit_cast(_Float16, v) : __builtin_bit_cast(float, w << 16);
+    }
+};
 
 // Scores of keys from `end` on leave a row.  (The empty statement keeps the last tile's branch a
 // branch: as selections every tile paid for it, 100 of 280 vector instructions.)
@@ -614,8 +674,8 @@ inline Attend attend_of(const flashlayer_attention *a)
     // additive masks of the inputs' type: float32 ones are one kind, float16 and bfloat16 two
     p.kind = a->mask != FLASHLAYER_MASK_ADD      ? a->mask
              : a->dtype == FLASHBEV_F32          ? FLASHLAYER_MASK_ADD_F32
-             : a->dtype == FLASHBEV_F16          ? FLASHLAYER_MASK_ADD + 16
-                                                 : FLASHLAYER_MASK_ADD + 32;
+             : a->dtype == FLASHBEV_F16          ? kAddF16
+                                                 : kAddBf16;
     p.drops = a->mask == FLASHLAYER_MASK_BOOL && (a->mask_row == 0 || a->Lq == 1) && (a->mask_head == 0 || p.share == 1);
     p.scale = a->scale;
     return p;

@@ -196,6 +196,11 @@ __global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) at
         lk += b0 * P::STRIDE;
         lv += b0 * P::STRIDE;
         f32x16 x[NB];
+        [[maybe_unused]] MaskBlock mask[NB];
+        if constexpr (MASK) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n) mask[n].load_row(p, mrow, k0 + n * 32, h);
+        }
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             x[n] = zeros16();
@@ -204,7 +209,7 @@ __global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) at
         }
         if constexpr (MASK) {
 #pragma unroll
-            for (int n = 0; n < NB; ++n) mask_row(p, x[n], mrow, k0 + n * 32, h);
+            for (int n = 0; n < NB; ++n) mask[n].apply_row(p, x[n]);
         }
         if (k0 + NB * 32 > len) {
 #pragma unroll
@@ -518,18 +523,35 @@ __global__ void __launch_bounds__(256) attend_join(Forward p)
     const int d = (int)(((int64_t)blockIdx.x * 256 + threadIdx.x) % LANES) * 4;
     if (at >= n) return;
     const float c = (p.any ? 1.0f : p.scale) * kLog2;
+    // eight splits' parts are loaded together
+    constexpr int U = 8;
     float m = -__builtin_inff(), l = 0.0f;
-#pragma unroll 8
-    for (int s = 0; s < p.splits; ++s) m = __builtin_fmaxf(m, p.part_ml[2 * (s * n + at)]);
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 8
-    for (int s = 0; s < p.splits; ++s) {
-        const float from = p.part_ml[2 * (s * n + at)];
-        const float f = from == -__builtin_inff() ? 0.0f : exp2_fast((from - m) * c);
-        l = __builtin_fmaf(p.part_ml[2 * (s * n + at) + 1], f, l);
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(p.part + (s * n + at) * DP + d);
+    for (int s0 = 0; s0 < p.splits; s0 += U) {
+        float from[U], part_l[U];
+        f32x4 v[U];
+        float to = m;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(v[i], f, sum[i]);
+        for (int u = 0; u < U; ++u) {
+            const int64_t i = min(s0 + u, p.splits - 1) * n + at;
+            from[u] = p.part_ml[2 * i];
+            part_l[u] = p.part_ml[2 * i + 1];
+            v[u] = *reinterpret_cast<const f32x4 *>(p.part + i * DP + d);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) to = __builtin_fmaxf(to, from[u]);
+        const float by = m == -__builtin_inff() ? 0.0f : exp2_fast((m - to) * c);
+        l *= by;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] *= by;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float f = s0 + u >= p.splits || from[u] == -__builtin_inff() ? 0.0f : exp2_fast((from[u] - to) * c);
+            l = __builtin_fmaf(part_l[u], f, l);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(v[u][i], f, sum[i]);
+        }
+        m = to;
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const int64_t problem = at / p.rows;
@@ -563,7 +585,7 @@ struct Plan {
 
 // A call's shape.  Up to 32 rows: the wavefronts of a workgroup go over the keys in turn.  Where
 // that leaves fewer than two workgroups a CU the keys are split, for about three of them, at two tiles
-// each or more.
+// each or more (at one where all tiles together are not more than two a CU).
 Plan plan_of(const flashlayer_attention *a)
 {
     Plan p{};
@@ -571,14 +593,15 @@ Plan plan_of(const flashlayer_attention *a)
     p.dp = padded_head(a->D);
     p.any = any_of(a);
     const bool flows = !p.any && p.dp * elem_size(a->dtype) < 512;
+    const int64_t problems = (int64_t)a->B * a->Hk;
     p.wq = rows <= 32 ? 1 : flows ? 4 : 5;
     const int bq = p.wq == 1 ? 32 : 128, bk = p.wq == 1 ? 128 : 64;
     p.tiles = (int)((rows + bq - 1) / bq);
-    const int64_t base = (int64_t)a->B * a->Hk * p.tiles, keys = (a->Lk + bk - 1) / bk;
+    const int64_t base = problems * p.tiles, keys = (a->Lk + bk - 1) / bk;
     p.splits = 1;
     if (base > 0 && base < 2 * kCusOfCard) {
         const int64_t want = (3 * kCusOfCard + base - 1) / base;
-        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(want, keys / 2));
+        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(want, base * keys <= 2 * kCusOfCard ? keys : keys / 2));
     }
     return p;
 }

@@ -225,12 +225,14 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
         for (int n = 0; n < 2; ++n) {
             const int k0 = t * S::BK + n * 32;
             f32x16 x = zeros16(), y = zeros16();
+            [[maybe_unused]] MaskBlock mask;
+            if constexpr (MASK) mask.load_row(p, mrow, k0, h);
 #pragma unroll
             for (int e = 0; e < P::CHUNKS; ++e) {
                 mma<DT>(x, read.along(lk, n * 32, e), qf[e]);
                 mma<DT>(y, read.along(lv, n * 32, e), gf[e]);
             }
-            if constexpr (MASK) mask_row(p, x, mrow, k0, h);
+            if constexpr (MASK) mask.apply_row(p, x);
             if (k0 + 32 > len) cut_keys(x, k0, h, len);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -465,11 +467,16 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
 #pragma unroll
         for (int n = 0; n < S::BR / 32; ++n) {
             f32x16 x = zeros16(), y = zeros16();
+            [[maybe_unused]] MaskBlock mask;
+            // (keys that are not there: the last one's, for sums of no meaning)
+            if constexpr (MASK)
+                mask.load_key(p, mbase, reinterpret_cast<const int64_t *>(ld) + n * 32 + 4 * h, min(key, p.Lk - 1));
 #pragma unroll
             for (int e = 0; e < P::CHUNKS; ++e) {
                 mma<DT>(x, read.along(lq, n * 32, e), kf[e]);
                 mma<DT>(y, read.along(lg, n * 32, e), vf[e]);
             }
+            if constexpr (MASK) mask.apply_key(p, x);
             const float *f = reinterpret_cast<const float *>(ld + 8 * S::BR) + n * 32 + 4 * h;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -479,8 +486,6 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
                 for (int i = 0; i < 4; ++i) {
                     float s = x[4 * k + i];
                     if constexpr (MASK) {
-                        const int64_t mo = reinterpret_cast<const int64_t *>(ld)[n * 32 + 8 * k + 4 * h + i];
-                        s = key_there ? mask_place(p, s, mbase + mo, key) : -__builtin_inff();
                         s = exp2_fast(__builtin_fmaf(s - f[8 * k + i], c, -e4[i]));
                     } else {
                         s = exp2_fast(__builtin_fmaf(s, c, -e4[i]));

@@ -12,6 +12,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "block/flashlayer.h"
 #include "block_act.h"
@@ -122,11 +123,13 @@ __device__ __forceinline__ float lane_stats(const Group &p, int64_t n_, int c, i
         mean[i] = sq[i] = 0.0f;
         from[i] = pivot<DT>(p, n_, min(c + i, C - 1) / p.per);
     }
-    int64_t r = r0;
-    for (; r + (kBatch - 1) * step < r1; r += kBatch * step) {
+    const auto batch = [&](int64_t r, int rows, auto whole) {
         u32x4 raw[kBatch];
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) raw[b] = L::load(x + (r + b * step) * ld * L::ES, c, C);
+        for (int b = 0; b < kBatch; ++b) {
+            raw[b] = u32x4{0, 0, 0, 0};
+            if (whole.value || b < rows) raw[b] = L::load(x + (r + b * step) * ld * L::ES, c, C);
+        }
         float s[L::V], q[L::V], v[L::V];
 #pragma unroll
         for (int i = 0; i < L::V; ++i) s[i] = q[i] = 0.0f;
@@ -134,30 +137,27 @@ __device__ __forceinline__ float lane_stats(const Group &p, int64_t n_, int c, i
         for (int b = 0; b < kBatch; ++b) {
             L::floats(raw[b], v);
 #pragma unroll
-            for (int i = 0; i < L::V; ++i) s[i] += v[i] - from[i];
+            for (int i = 0; i < L::V; ++i) s[i] += whole.value || b < rows ? v[i] - from[i] : 0.0f;
         }
+        const float share = whole.value ? 1.0f / kBatch : 1.0f / (float)rows;
 #pragma unroll
-        for (int i = 0; i < L::V; ++i) s[i] *= 1.0f / kBatch;
+        for (int i = 0; i < L::V; ++i) s[i] *= share;
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             L::floats(raw[b], v);
 #pragma unroll
             for (int i = 0; i < L::V; ++i) {
-                const float d = v[i] - from[i] - s[i];
+                const float d = whole.value || b < rows ? v[i] - from[i] - s[i] : 0.0f;
                 q[i] = __builtin_fmaf(d, d, q[i]);
             }
         }
 #pragma unroll
-        for (int i = 0; i < L::V; ++i) join(mean[i], sq[i], n, s[i], q[i], (float)kBatch);
-        n += kBatch;
-    }
-    for (; r < r1; r += step) {
-        float v[L::V];
-        L::floats(L::load(x + r * ld * L::ES, c, C), v);
-#pragma unroll
-        for (int i = 0; i < L::V; ++i) join(mean[i], sq[i], n, v[i] - from[i], 0.0f, 1.0f);
-        n += 1.0f;
-    }
+        for (int i = 0; i < L::V; ++i) join(mean[i], sq[i], n, s[i], q[i], (float)rows);
+        n += (float)rows;
+    };
+    int64_t r = r0;
+    for (; r + (kBatch - 1) * step < r1; r += kBatch * step) batch(r, kBatch, std::true_type{});
+    if (r < r1) batch(r, (int)((r1 - r + step - 1) / step), std::false_type{});
     return n;
 }
 
@@ -190,12 +190,11 @@ __device__ __forceinline__ void column_stats(float *lds, int rr, int rows, int c
     }
 }
 
-// The wavefront's 64 (mean, squares, count); all lanes end with the whole.  Both sides of a
-// pair join the same way round, so that all lanes agree.
-__device__ __forceinline__ void wave_stats(float &mean, float &sq, float &n)
+// The (mean, squares, count) of `width` neighbouring lanes, a power of two; all end with the whole.
+// Both sides of a pair join the same way round, so that all lanes agree.
+__device__ __forceinline__ void wave_stats(float &mean, float &sq, float &n, int width = 64)
 {
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
+    for (int o = 1; o < width; o *= 2) {
         const float m2 = __shfl_xor(mean, o), s2 = __shfl_xor(sq, o), n2 = __shfl_xor(n, o);
         const bool low = !(threadIdx.x & o);
         float a = low ? mean : m2, b = low ? sq : s2, k = low ? n : n2;
@@ -232,20 +231,27 @@ __device__ __forceinline__ Place place_of(const Group &p, uint32_t id, int threa
 
 // The statistics of the groups that columns c0 .. c1 - 1 hold (parts of), of their channels' in
 // `lds` (means, then sums of squared differences `vecs` * V further on), each of `rows` values.
-// A wavefront takes a group; `put` gets the group, its mean, squares and count in one lane.
+// As many lanes to a group as it has channels, up to a wavefront; `put` gets the group, its
+// mean, squares and count in one lane.  (A wavefront to each group of 8 channels was most of
+// the pass: 139200 x 256 in 32 groups 38 us of 38.)
 template <class F>
 __device__ __forceinline__ void join_channels(const float *lds, int squares, int c0, int c1, int per, float rows,
                                               int waves, F put)
 {
-    for (int g = c0 / per + (threadIdx.x >> 6); g * per < c1; g += waves) {
+    int width = 1;
+    while (width < per && width < 64) width *= 2;
+    const int lane = threadIdx.x & (width - 1), g0 = c0 / per, each = waves * 64 / width;
+    // (whole wavefronts go round together: their lanes exchange values)
+    for (int base = g0; base * per < c1; base += each) {
+        const int g = base + (int)threadIdx.x / width;
         float m = 0.0f, s = 0.0f, k = 0.0f;
         const int first = max(c0, g * per) - c0, last = min(c1, (g + 1) * per) - c0;
-        for (int i = first + (threadIdx.x & 63); i < last; i += 64) {
+        for (int i = first + lane; i < last; i += width) {
             join(m, s, k, lds[i], lds[squares + i], rows);
             k += rows;
         }
-        wave_stats(m, s, k);
-        if ((threadIdx.x & 63) == 0) put(g, m, s, k);
+        wave_stats(m, s, k, width);
+        if (lane == 0 && first < last) put(g, m, s, k);
     }
 }
 
@@ -651,8 +657,9 @@ int check(const flashlayer_group_norm *a)
     return FLASHBEV_OK;
 }
 
-// How a call is cut.  Chunks of rows: a lane's batch of eight rows at least, and more where
-// that would be over 2048 workgroups (eight for each CU; the joins read every chunk's sums).
+// How a call is cut.  Chunks of rows: a lane's batch of eight rows at least, and more where that
+// would be over 768 workgroups, the three of a CU that run at once in the backward (139200 x 256
+// bf16, a training step's first and second backward passes: XX us, 45 + 48 of 972, 39 + 40 of 498).
 struct Cut {
     bool whole;
     int slices, slice, chunks;
@@ -675,9 +682,9 @@ Cut cut(const flashlayer_group_norm *a, bool backward)
     }
     c.slice = std::min(a->C, 256 * V);
     c.slices = (a->C + c.slice - 1) / c.slice;
-    const int64_t rows = 256 / ((c.slice + V - 1) / V) * kBatch;
-    const int64_t most = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, a->N * c.slices));
-    c.chunk = std::max(rows, ((a->R + most - 1) / most + rows - 1) / rows * rows);
+    const int64_t rows = 256 / ((c.slice + V - 1) / V);   // that the workgroup's lanes take at once
+    const int64_t most = std::max<int64_t>(1, 768 / std::max<int64_t>(1, a->N * c.slices));
+    c.chunk = std::max(rows * kBatch, ((a->R + most - 1) / most + rows - 1) / rows * rows);
     c.chunks = (int)((a->R + c.chunk - 1) / c.chunk);
     return c;
 }
