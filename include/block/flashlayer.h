@@ -91,7 +91,9 @@ int flashlayer_attention_forward(const flashlayer_attention *args, const void *q
                                  uint64_t workspace_bytes, void *stream);
 
 /* Workspace bytes of flashlayer_attention_forward: partial results where few queries leave
- * the keys to be split.  No HIP call. */
+ * the keys to be split; copies of k and v where D is not a multiple of 16 bytes or a boolean
+ * mask leaves keys out altogether (of over 32 rows).  Of the strides only mask_head and mask_row are
+ * read, as zero or not.  No HIP call. */
 int flashlayer_attention_workspace_size(const flashlayer_attention *args, uint64_t *bytes);
 
 /*

@@ -39,6 +39,9 @@ struct Attend {
     uint32_t share_inv;              // ceil(2^32 / share), share > 1
     int kind;                        // flashlayer_mask
     int drops;                       // a boolean mask that is the same for all rows of a problem
+    const uint32_t *words;           // with drops, without other masks: bits of the keys that take part,
+    int64_t words_b, words_g;        // `words_b` words from batch to batch, `words_g` from head to head
+    int Dk;                          // channels of k's and v's rows: D, or that up to whole granules
     float scale;
     int tiles;                       // of rows (forward, grad_q) or of keys (grad_k, grad_v)
     int splits;
@@ -275,12 +278,13 @@ struct Strip {
             }
         }
 
-        __device__ __forceinline__ void places(const Attend &p, int r0, int i0, int64_t stride, int64_t head)
+        template <class A>
+        __device__ __forceinline__ void places(const A &p, int r0, int i0, int64_t stride, int64_t head)
         {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
                 int qi, qj;
-                p.row(min(r0 + row[i], p.rows - 1), qi, qj);
+                p.part_of(min(r0 + row[i], p.rows - 1), qi, qj);
                 off[i] = (uint32_t)(qi - i0) * (uint32_t)stride + (uint32_t)qj * (uint32_t)head + g[i] * 16;
             }
         }
@@ -528,6 +532,16 @@ __device__ __forceinline__ void cut_keys(f32x16 &x, int key0, int h, int end)
         if (key0 + 8 * (i >> 2) + 4 * h + (i & 3) >= end) x[i] = -__builtin_inff();
 }
 
+// The same by a word of the keys' bits.
+__device__ __forceinline__ void cut_word(f32x16 &x, uint32_t word, int h)
+{
+    asm volatile("");
+    word >>= 4 * h;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (!(word >> (8 * (i >> 2) + (i & 3)) & 1)) x[i] = -__builtin_inff();
+}
+
 // The other half's value of the lane's column joined with its own.
 __device__ __forceinline__ float both_max(float v)
 {
@@ -574,9 +588,77 @@ __device__ __forceinline__ float rounded(float v)
 }
 
 // ---------------------------------------------------------------------------
+// copies
+// ---------------------------------------------------------------------------
+// Rows of a problem (the keys of a head of the states, or the rows of a problem) to whole granules.
+struct Copy {
+    const char *from[2];
+    char *to[2];
+    int64_t batch[2], row[2], head[2], group[2];   // bytes: row r at row (r / share) + head (r % share)
+    const uint32_t *words;                         // null: all rows are there
+    int64_t words_b, words_g;
+    const int32_t *lengths;                        // null: all
+    uint64_t items;                                // granules of one tensor
+    int heads, rows, share, D, granules;
+};
+
+template <int DT>
+__global__ void __launch_bounds__(256) attend_copy(Copy p)
+{
+    const uint64_t t = (uint64_t)block_index() * 256 + threadIdx.x;
+    if (t >= 2 * p.items) return;
+    const int which = t >= p.items;
+    const uint64_t at = t - (which ? p.items : 0);
+    uint64_t n = at / p.granules;
+    const int granule = (int)(at - n * p.granules);
+    const uint64_t m = n / p.rows;
+    const int r = (int)(n - m * p.rows);
+    const int b = (int)(m / p.heads), g = (int)(m - (uint64_t)b * p.heads);
+    u32x4 v = {0, 0, 0, 0};
+    const bool there = (!p.words || p.words[b * p.words_b + g * p.words_g + (r >> 5)] >> (r & 31) & 1) &&
+                       (!p.lengths || r < p.lengths[b]);
+    if (there) {
+        const int i = r / p.share, j = r - i * p.share;
+        const char *row = (which ? p.from[1] : p.from[0]) + b * (which ? p.batch[1] : p.batch[0]) +
+                          g * (which ? p.group[1] : p.group[0]) + i * (which ? p.row[1] : p.row[0]) +
+                          j * (which ? p.head[1] : p.head[0]);
+        v = Panel<DT, 32, 32>::granule(row, granule, p.D);
+    }
+    *reinterpret_cast<u32x4 *>((which ? p.to[1] : p.to[0]) + at * 16) = v;
+}
+
+// The keys' bits, from a boolean mask.
+struct Bits {
+    const char *mask;
+    int64_t batch, head;   // bytes
+    uint32_t *words;
+    const int32_t *lengths;
+    int64_t per;           // words of a row
+    uint64_t items;        // words
+    int heads, Lk;
+};
+
+template <int UNUSED>
+__global__ void __launch_bounds__(256) attend_bits(Bits p)
+{
+    const uint64_t t = (uint64_t)block_index() * 256 + threadIdx.x;
+    if (t >= p.items) return;
+    const uint64_t m = t / p.per;
+    const int key0 = (int)(t - m * p.per) * 32, b = (int)(m / p.heads), g = (int)(m - (uint64_t)b * p.heads);
+    const int end = p.lengths ? max(0, min(p.lengths[b], p.Lk)) : p.Lk;
+    const char *row = p.mask + b * p.batch + g * p.head;
+    uint32_t w = 0;
+    for (int i = 0; i < 32; ++i)
+        if (key0 + i < end && row[key0 + i]) w |= 1u << i;
+    p.words[t] = w;
+}
+
+// ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
 constexpr int kCusOfCard = 256;
+
+inline uint64_t align256(uint64_t v) { return (v + 255) & ~255ull; }
 
 inline int check_attention(const flashlayer_attention *a)
 {
@@ -632,14 +714,53 @@ inline bool apart(int n0, int64_t s0, int n1, int64_t s1, int n2, int64_t s2, in
     return true;
 }
 
-inline uint64_t align256(uint64_t v) { return (v + 255) & ~255ull; }
-
 inline int padded_head(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : 128; }
 
-// Whether a call takes the kernels that do all: masks, and rows that end inside a granule.
-inline bool any_of(const flashlayer_attention *a)
+inline int share_of(const flashlayer_attention *a) { return a->Hk ? a->H / a->Hk : 1; }
+
+// A boolean mask that is the same for all rows of a problem leaves its keys out altogether.
+inline bool drops_of(const flashlayer_attention *a)
 {
-    return a->mask != FLASHLAYER_MASK_NONE || a->D % (16 / elem_size(a->dtype)) != 0;
+    return a->mask == FLASHLAYER_MASK_BOOL && (a->mask_row == 0 || a->Lq == 1) &&
+           (a->mask_head == 0 || share_of(a) == 1);
+}
+
+// A mask that differs from row to row.
+inline bool pairs_of(const flashlayer_attention *a) { return a->mask != FLASHLAYER_MASK_NONE && !drops_of(a); }
+
+// Rows that end inside a granule.
+inline bool odd_of(const flashlayer_attention *a) { return a->D % (16 / elem_size(a->dtype)) != 0; }
+
+// Whether a call of one workgroup's few rows takes the kernels that do all.
+inline bool any_of(const flashlayer_attention *a) { return a->mask != FLASHLAYER_MASK_NONE || odd_of(a); }
+
+inline int whole_head(const flashlayer_attention *a)
+{
+    const int E = 16 / elem_size(a->dtype);
+    return (a->D + E - 1) / E * E;
+}
+
+// Copies that keep loads to LDS simple: rows of whole granules, zeros past D and in place of keys
+// that are left out, [B][heads][rows][whole_head]; and the bits of the keys that take part.
+inline uint64_t rows_copy_bytes(const flashlayer_attention *a, int64_t rows, int heads)
+{
+    return align256(size_prod({(uint64_t)a->B, (uint64_t)heads, (uint64_t)rows, (uint64_t)whole_head(a),
+                               (uint64_t)elem_size(a->dtype)}));
+}
+
+inline int64_t words_of(const flashlayer_attention *a) { return ((int64_t)a->Lk + 127) / 128 * 4; }
+
+inline uint64_t words_bytes(const flashlayer_attention *a)
+{
+    return align256((uint64_t)a->B * (a->mask_head ? a->Hk : 1) * words_of(a) * 4);
+}
+
+inline bool copies_keys(const flashlayer_attention *a) { return !pairs_of(a) && (odd_of(a) || drops_of(a)); }
+
+inline uint64_t keys_copy_bytes(const flashlayer_attention *a)
+{
+    if (!copies_keys(a)) return 0;
+    return 2 * rows_copy_bytes(a, a->Lk, a->Hk) + (drops_of(a) ? words_bytes(a) : 0);
 }
 
 inline Attend attend_of(const flashlayer_attention *a)
@@ -676,7 +797,8 @@ inline Attend attend_of(const flashlayer_attention *a)
              : a->dtype == FLASHBEV_F32          ? FLASHLAYER_MASK_ADD_F32
              : a->dtype == FLASHBEV_F16          ? kAddF16
                                                  : kAddBf16;
-    p.drops = a->mask == FLASHLAYER_MASK_BOOL && (a->mask_row == 0 || a->Lq == 1) && (a->mask_head == 0 || p.share == 1);
+    p.drops = drops_of(a);
+    p.Dk = a->D;
     p.scale = a->scale;
     return p;
 }
@@ -696,6 +818,57 @@ int launch_lds(const void *fn, uint64_t blocks, P &p, size_t lds, hipStream_t st
     if (lds > 65536 && hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
         return FLASHBEV_ERR_HIP;
     return launch_kernel(fn, blocks, 256, p, lds, st);
+}
+
+template <int DT>
+int copy_rows(Copy &c, int64_t batches, hipStream_t st)
+{
+    c.items = (uint64_t)batches * c.heads * c.rows * c.granules;
+    return launch_rows((const void *)attend_copy<DT>, (2 * c.items + 255) / 256, 256, c, st);
+}
+
+// k's and v's copies and bits, in `ws` of keys_copy_bytes; p reads them from here on.
+template <int DT>
+int copy_keys(const flashlayer_attention *a, Attend &p, char *ws, hipStream_t st)
+{
+    constexpr int ES = elem_size(DT);
+    const uint64_t each = rows_copy_bytes(a, a->Lk, a->Hk);
+    if (p.drops) {
+        Bits bits{p.mask, p.mb, p.mh, reinterpret_cast<uint32_t *>(ws + 2 * each), p.lengths, words_of(a), 0,
+                  a->mask_head ? a->Hk : 1, a->Lk};
+        bits.items = (uint64_t)a->B * bits.heads * bits.per;
+        if (const int rc = launch_rows((const void *)attend_bits<0>, (bits.items + 255) / 256, 256, bits, st)) return rc;
+        p.words = bits.words;
+        p.words_g = a->mask_head ? bits.per : 0;
+        p.words_b = bits.per * bits.heads;
+    }
+    Copy c{};
+    c.from[0] = p.k;
+    c.from[1] = p.v;
+    c.to[0] = ws;
+    c.to[1] = ws + each;
+    c.batch[0] = p.kb;
+    c.batch[1] = p.vb;
+    c.row[0] = p.kr;
+    c.row[1] = p.vr;
+    c.group[0] = p.kh;
+    c.group[1] = p.vh;
+    c.words = p.words;
+    c.words_b = p.words_b;
+    c.words_g = p.words_g;
+    c.lengths = p.lengths;
+    c.heads = a->Hk;
+    c.rows = a->Lk;
+    c.share = 1;
+    c.D = a->D;
+    p.Dk = whole_head(a);
+    c.granules = p.Dk * ES / 16;
+    p.k = c.to[0];
+    p.v = c.to[1];
+    p.kr = p.vr = (int64_t)p.Dk * ES;
+    p.kh = p.vh = p.kr * a->Lk;
+    p.kb = p.vb = p.kh * a->Hk;
+    return copy_rows<DT>(c, a->B, st);
 }
 
 struct Bytes {

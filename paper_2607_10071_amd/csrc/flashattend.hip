@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) at
     put_row<DT, DP, MASK>(p, b, g, split, r, qi, head, m, l, o, h);
 }
 
-// Without masks: four wavefronts of 32 rows each share tiles of TK keys, which go from memory to LDS
+// Without masks that differ from row to row: four wavefronts of 32 rows each share tiles of TK keys, which go from memory to LDS
 // without passing registers, and take them 32 keys at a time.  In one step a wavefront forms the
 // next 32 keys' scores, this 32's weights and the product of the last 32's with v: matrix
 // and vector instructions that do not wait for each other, in turn.  (Scores, then weights, then
@@ -335,7 +335,8 @@ constexpr int flow_waves(int dt, int dp)
     return dp * elem_size(dt) <= 64 ? 4 : 2;
 }
 
-template <int DT, int DP>
+// KEYS: some keys are left out, by their bits.
+template <int DT, int DP, bool KEYS>
 __global__ void __launch_bounds__(256, flow_waves(DT, DP)) attend_flow(Forward p)
 {
     using F = Flow<DT, DP>;
@@ -372,8 +373,9 @@ __global__ void __launch_bounds__(256, flow_waves(DT, DP)) attend_flow(Forward p
     typename T::Reader read;
     read.start(lane);
     typename T::Loader kl, vl;
-    kl.start(wave, lane, p.D, p.kr);
-    vl.start(wave, lane, p.D, p.vr);
+    kl.start(wave, lane, p.Dk, p.kr);
+    vl.start(wave, lane, p.Dk, p.vr);
+    [[maybe_unused]] const uint32_t *words = p.words + b * p.words_b + g * p.words_g;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds);
     const char *kbase = p.k + b * p.kb + g * p.kh, *vbase = p.v + b * p.vb + g * p.vh;
     // K of tile t lies at k_at(t); V's places turn by one a tile
@@ -419,6 +421,12 @@ __global__ void __launch_bounds__(256, flow_waves(DT, DP)) attend_flow(Forward p
             return i % 2 == 0 ? read.along(lk, 0, i / 2) : read.across(lv, 0, i / 2 / DB, i / 2 % DB * 32);
         };
         if (key0 + 32 > end) cut_keys(x, key0, h, end);
+        if constexpr (KEYS) {
+            if (key0 < end) {
+                const uint32_t word = words[key0 >> 5];
+                if (word != 0xffffffffu) cut_word(x, word, h);
+            }
+        }
         const float mc = m * c;
         float v[16], sum = 0.0f;
         u32x4 f[AHEAD];
@@ -581,6 +589,7 @@ __global__ void __launch_bounds__(256) attend_join(Forward p)
 struct Plan {
     int wq, tiles, splits, dp;   // wq 4: attend_flow; 5: attend with four wavefronts' rows; 1: with one's
     bool any;
+    bool copies;   // k and v are copied first
 };
 
 // A call's shape.  Up to 32 rows: the wavefronts of a workgroup go over the keys in turn.  Where
@@ -591,10 +600,11 @@ Plan plan_of(const flashlayer_attention *a)
     Plan p{};
     const int64_t rows = (int64_t)a->Lq * (a->Hk ? a->H / a->Hk : 1);
     p.dp = padded_head(a->D);
-    p.any = any_of(a);
-    const bool flows = !p.any && p.dp * elem_size(a->dtype) < 512;
+    const bool flows = !pairs_of(a) && p.dp * elem_size(a->dtype) < 512;
     const int64_t problems = (int64_t)a->B * a->Hk;
     p.wq = rows <= 32 ? 1 : flows ? 4 : 5;
+    p.copies = p.wq == 4 && copies_keys(a);
+    p.any = p.wq == 1 ? any_of(a) : p.wq == 5;
     const int bq = p.wq == 1 ? 32 : 128, bk = p.wq == 1 ? 128 : 64;
     p.tiles = (int)((rows + bq - 1) / bq);
     const int64_t base = problems * p.tiles, keys = (a->Lk + bk - 1) / bk;
@@ -614,9 +624,11 @@ uint64_t part_bytes(const flashlayer_attention *a, const Plan &p)
 
 uint64_t forward_bytes(const flashlayer_attention *a)
 {
+    if (!a->B || !a->Lq || !a->H || !a->D) return 0;
     const Plan p = plan_of(a);
-    if (p.splits <= 1) return 0;
-    return part_bytes(a, p) + align256((uint64_t)p.splits * a->B * a->Lq * a->H * 8);
+    const uint64_t copies = p.copies ? keys_copy_bytes(a) : 0;
+    if (p.splits <= 1) return copies;
+    return copies + part_bytes(a, p) + align256((uint64_t)p.splits * a->B * a->Lq * a->H * 8);
 }
 
 template <int DT, int DP>
@@ -626,7 +638,7 @@ int run(Forward &p, const Plan &plan, hipStream_t st)
     size_t lds = 0;
     if constexpr (DP * elem_size(DT) < 512) {
         if (plan.wq == 4) {
-            fn = (const void *)attend_flow<DT, DP>;
+            fn = p.words ? (const void *)attend_flow<DT, DP, true> : (const void *)attend_flow<DT, DP, false>;
             lds = Flow<DT, DP>::LDS;
         }
     }
@@ -644,8 +656,10 @@ int run(Forward &p, const Plan &plan, hipStream_t st)
 }
 
 template <int DT>
-int run_width(Forward &p, const Plan &plan, hipStream_t st)
+int run_width(const flashlayer_attention *a, Forward &p, const Plan &plan, void *workspace, hipStream_t st)
 {
+    if (plan.copies && a->Lk)
+        if (const int rc = copy_keys<DT>(a, p, static_cast<char *>(workspace), st)) return rc;
     switch (plan.dp) {
     case 32: return run<DT, 32>(p, plan, st);
     case 64: return run<DT, 64>(p, plan, st);
@@ -708,14 +722,15 @@ extern "C" int flashlayer_attention_forward(const flashlayer_attention *args, co
     p.stats = stats;
     p.tiles = plan.tiles;
     p.splits = plan.splits;
-    p.any = plan.any || plan.wq == 5;
+    p.any = plan.any;
+    char *ws = static_cast<char *>(workspace) + (plan.copies ? keys_copy_bytes(args) : 0);
     if (p.splits > 1) {
-        p.part = static_cast<float *>(workspace);
-        p.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + part_bytes(args, plan));
+        p.part = reinterpret_cast<float *>(ws);
+        p.part_ml = reinterpret_cast<float *>(ws + part_bytes(args, plan));
     }
     if (const int rc = deal(p, size_prod({(uint64_t)a.B, (uint64_t)a.Hk, (uint64_t)plan.tiles, (uint64_t)plan.splits})))
         return rc;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (a.dtype == FLASHBEV_F32) return run_width<FLASHBEV_F32>(p, plan, st);
-    return a.dtype == FLASHBEV_F16 ? run_width<FLASHBEV_F16>(p, plan, st) : run_width<FLASHBEV_BF16>(p, plan, st);
+    if (a.dtype == FLASHBEV_F32) return run_width<FLASHBEV_F32>(args, p, plan, workspace, st);
+    return a.dtype == FLASHBEV_F16 ? run_width<FLASHBEV_F16>(args, p, plan, workspace, st) : run_width<FLASHBEV_BF16>(args, p, plan, workspace, st);
 }

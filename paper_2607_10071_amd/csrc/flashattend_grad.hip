@@ -52,6 +52,21 @@ struct Backward : Attend {
     float *part;              // splits > 1: grad_q's [splits][B Hk rows][DP] or
                               // grad_k's and grad_v's [2][splits][B Hk Lk][DP]
     int row_tiles;            // of 16
+    // q's and g's rows as grad_k's and grad_v's kernel without masks reads them: row r of head g of the
+    // states at g `group` + (r / rshare) `row` + (r % rshare) `head`, of Dr channels
+    const char *rq, *rg;
+    int64_t rq_b, rq_g, rq_r, rq_h, rg_b, rg_g, rg_r, rg_h;
+    int rshare, Dr;
+
+    __device__ __forceinline__ void part_of(int r, int &i, int &j) const
+    {
+        if (rshare > 1) {
+            row(r, i, j);
+        } else {
+            i = r;
+            j = 0;
+        }
+    }
 };
 
 constexpr int kRowTile = 16;
@@ -364,7 +379,7 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
     const int len = p.keys(b);
     const int k0 = tile * S::BK + wave * 32, key = k0 + (lane & 31);
     const char *mbase = p.mask + b * p.mb + (int64_t)g * p.share * p.mh;
-    const bool key_there = key < len && !(MASK && p.drops && mbase[key] == 0);
+    const bool key_there = key < len && !(p.drops && mbase[key] == 0);
 
     const int all = tile * S::BK < len ? (p.rows + S::BR - 1) / S::BR : 0;
     const int per = (all + p.splits - 1) / p.splits;
@@ -389,10 +404,9 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
     // Rows on their way: row r is query r / share, head r % share.  A thread's places in a tile are
     // the same in every tile where tiles are whole queries.
     typename P::Mover mover;
-    mover.start(tid, p.D, 0);
-    const char *qbase = p.q + b * p.qb + (int64_t)g * p.share * p.qh;
-    const char *gbase = p.g + b * p.ob + (int64_t)g * p.share * p.oh;
-    const bool even = S::BR % p.share == 0, copies = MASK && p.D % P::E != 0;
+    mover.start(tid, p.Dr, 0);
+    const char *qbase = p.rq + b * p.rq_b + g * p.rq_g, *gbase = p.rg + b * p.rg_b + g * p.rg_g;
+    const bool even = S::BR % p.rshare == 0, copies = MASK && p.D % P::E != 0;
     u32x4 qv[P::G], gv[P::G];
     mover.clear(qv);
     mover.clear(gv);
@@ -402,19 +416,19 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
 #pragma unroll
         for (int i = 0; i < P::G; ++i) {
             int qi, qj;   // past the last row the last one again, whose weights are zeros
-            p.row(min(r0 + mover.row + i * P::RP, p.rows - 1), qi, qj);
-            qoff[i] = (uint32_t)(qi - i0) * (uint32_t)p.qr + (uint32_t)qj * (uint32_t)p.qh + mover.g * 16;
-            goff[i] = (uint32_t)(qi - i0) * (uint32_t)p.orow + (uint32_t)qj * (uint32_t)p.oh + mover.g * 16;
+            p.part_of(min(r0 + mover.row + i * P::RP, p.rows - 1), qi, qj);
+            qoff[i] = (uint32_t)(qi - i0) * (uint32_t)p.rq_r + (uint32_t)qj * (uint32_t)p.rq_h + mover.g * 16;
+            goff[i] = (uint32_t)(qi - i0) * (uint32_t)p.rg_r + (uint32_t)qj * (uint32_t)p.rg_h + mover.g * 16;
         }
     };
     auto fetch = [&](int t) {
         const int r0 = t * S::BR;
         if (tid < S::BR && r0 + tid < p.rows) rd = p.data[problem * p.rows + r0 + tid];
         if (copies) return;
-        const int i0 = r0 / p.share;
+        const int i0 = r0 / p.rshare;
         if (t == t0 || !even || r0 + S::BR > p.rows) places(r0, i0);
         if (!mover.mine) return;
-        const char *qt = qbase + i0 * p.qr, *gt = gbase + i0 * p.orow;
+        const char *qt = qbase + i0 * p.rq_r, *gt = gbase + i0 * p.rg_r;
 #pragma unroll
         for (int i = 0; i < P::G; ++i)
             if (mover.inside(i)) {
@@ -450,8 +464,8 @@ __global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_
             if (r0 + i < p.rows) {
                 int qi, qj;
                 p.row(r0 + i, qi, qj);
-                a = P::granule(qbase + qi * p.qr + qj * p.qh, mover.g, p.D);
-                w = P::granule(gbase + qi * p.orow + qj * p.oh, mover.g, p.D);
+                a = P::granule(qbase + qi * p.rq_r + qj * p.rq_h, mover.g, p.D);
+                w = P::granule(gbase + qi * p.rg_r + qj * p.rg_h, mover.g, p.D);
             }
             *reinterpret_cast<u32x4 *>(lq + P::place(i, mover.g)) = a;
             *reinterpret_cast<u32x4 *>(lg + P::place(i, mover.g)) = w;
@@ -526,7 +540,7 @@ constexpr int grad_q_waves(int dt, int dp)
     return dp * elem_size(dt) <= 64 ? 3 : dp * elem_size(dt) <= 256 ? 2 : 1;
 }
 
-template <int DT, int DP>
+template <int DT, int DP, bool KEYS>
 __global__ void __launch_bounds__(256, grad_q_waves(DT, DP)) attend_grad_q_flow(Backward p)
 {
     using F = FlowQ<DT, DP>;
@@ -566,8 +580,9 @@ __global__ void __launch_bounds__(256, grad_q_waves(DT, DP)) attend_grad_q_flow(
     typename T::Reader read;
     read.start(lane);
     typename T::Loader kl, vl;
-    kl.start(wave, lane, p.D, p.kr);
-    vl.start(wave, lane, p.D, p.vr);
+    kl.start(wave, lane, p.Dk, p.kr);
+    vl.start(wave, lane, p.Dk, p.vr);
+    [[maybe_unused]] const uint32_t *words = p.words + b * p.words_b + g * p.words_g;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds);
     const char *kbase = p.k + b * p.kb + g * p.kh, *vbase = p.v + b * p.vb + g * p.vh;
     const auto v_at = [&](int t) { return (t & 1) * T::BYTES; };
@@ -589,6 +604,12 @@ __global__ void __launch_bounds__(256, grad_q_waves(DT, DP)) attend_grad_q_flow(
                                 : read.across(lk0, 0, i / 3 / DB, i / 3 % DB * 32);
         };
         if (key0 + 32 > end) cut_keys(x, key0, h, end);
+        if constexpr (KEYS) {
+            if (key0 < end) {
+                const uint32_t word = words[key0 >> 5];
+                if (word != 0xffffffffu) cut_word(x, word, h);
+            }
+        }
         float v[16];
         u32x4 f[AHEAD];
         next_x = zeros16();
@@ -732,7 +753,8 @@ __global__ void __launch_bounds__(256, grad_kv_waves(DT, DP)) attend_grad_kv_flo
     const int64_t problem = (int64_t)b * p.Hk + g;
     const int len = p.keys(b);
     const int key = tile * 128 + wave * 32 + (lane & 31);
-    const bool key_there = key < len;
+    const bool key_there =
+        key < len && !(p.words && !(p.words[b * p.words_b + g * p.words_g + (key >> 5)] >> (key & 31) & 1));
 
     const int all = tile * 128 < len ? (p.rows + F::TR - 1) / F::TR : 0;
     const int per = (all + p.splits - 1) / p.splits;
@@ -758,18 +780,17 @@ __global__ void __launch_bounds__(256, grad_kv_waves(DT, DP)) attend_grad_kv_flo
     ql.start(wave, lane);
     gl.start(wave, lane);
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds);
-    const char *qbase = p.q + b * p.qb + (int64_t)g * p.share * p.qh;
-    const char *gbase = p.g + b * p.ob + (int64_t)g * p.share * p.oh;
+    const char *qbase = p.rq + b * p.rq_b + g * p.rq_g, *gbase = p.rg + b * p.rg_b + g * p.rg_g;
     const float *lose = p.lose + problem * p.padded, *delta = p.delta + problem * p.padded;
-    const bool even = F::TR % p.share == 0;   // a thread's places are the same in every tile
+    const bool even = F::TR % p.rshare == 0;   // a thread's places are the same in every tile
     const auto load = [&](int t, int stage) {
-        const int r0 = t * F::TR, i0 = r0 / p.share;
+        const int r0 = t * F::TR, i0 = r0 / p.rshare;
         if (t == t0 || !even || r0 + F::TR > p.rows) {
-            ql.places(p, r0, i0, p.qr, p.qh);
-            gl.places(p, r0, i0, p.orow, p.oh);
+            ql.places(p, r0, i0, p.rq_r, p.rq_h);
+            gl.places(p, r0, i0, p.rg_r, p.rg_h);
         }
-        ql.load(qbase + i0 * p.qr, p.D, lds0 + stage, wave);
-        gl.load(gbase + i0 * p.orow, p.D, lds0 + stage + T::BYTES, wave);
+        ql.load(qbase + i0 * p.rq_r, p.Dr, lds0 + stage, wave);
+        gl.load(gbase + i0 * p.rg_r, p.Dr, lds0 + stage + T::BYTES, wave);
         if (wave < 2 * F::TR / 64) {   // exponents, then deltas, 64 rows to an instruction
             const int part = wave * 64 % F::TR;
             word_to_lds((wave * 64 < F::TR ? lose : delta) + r0 + part + lane, lds0 + stage + 2 * T::BYTES + wave * 256);
@@ -944,7 +965,8 @@ __global__ void __launch_bounds__(256) attend_sum(Sum p)
 // ---------------------------------------------------------------------------
 struct Plan {
     int dp, row_tiles, padded;
-    bool any;
+    bool any;      // masks that differ from row to row, and float32 heads of over 96 channels
+    bool copies;   // k and v are copied first, and odd rows of q and g
     int q_tiles, q_splits;
     int k_tiles, k_splits;
 };
@@ -962,7 +984,8 @@ Plan plan_of(const flashlayer_attention *a)
     Plan p{};
     const int64_t rows = (int64_t)a->Lq * (a->Hk ? a->H / a->Hk : 1), problems = (int64_t)a->B * a->Hk;
     p.dp = padded_head(a->D);
-    p.any = any_of(a);
+    p.any = pairs_of(a) || p.dp * elem_size(a->dtype) >= 512;
+    p.copies = !p.any && copies_keys(a);
     p.padded = (int)((rows + 127) / 128 * 128);
     p.row_tiles = p.padded / kRowTile;
     p.q_tiles = (int)((rows + 127) / 128);
@@ -983,6 +1006,12 @@ uint64_t rows_bytes(const flashlayer_attention *a, const Plan &p)
     return align256((uint64_t)a->B * a->Hk * p.padded * 4);
 }
 
+uint64_t copy_bytes(const flashlayer_attention *a, const Plan &p)
+{
+    if (!p.copies) return 0;
+    return keys_copy_bytes(a) + (odd_of(a) ? 2 * rows_copy_bytes(a, (int64_t)a->Lq * share_of(a), a->Hk) : 0);
+}
+
 uint64_t largest_bytes(const flashlayer_attention *a, const Plan &p)
 {
     return align256((uint64_t)a->B * a->Hk * p.row_tiles * 8);
@@ -997,7 +1026,7 @@ uint64_t backward_bytes(const flashlayer_attention *a, bool want_q, bool want_kv
         q = size_prod({(uint64_t)p.q_splits, (uint64_t)a->B * a->Lq * a->H, (uint64_t)p.dp, 4});
     if (want_kv && p.k_splits > 1)
         kv = size_prod({2, (uint64_t)p.k_splits, (uint64_t)a->B * a->Lk * a->Hk, (uint64_t)p.dp, 4});
-    return data_bytes(a) + 2 * rows_bytes(a, p) + largest_bytes(a, p) + align256(std::max(q, kv));
+    return copy_bytes(a, p) + data_bytes(a) + 2 * rows_bytes(a, p) + largest_bytes(a, p) + align256(std::max(q, kv));
 }
 
 template <int DT, int DP>
@@ -1012,7 +1041,8 @@ int run(Backward &p, const Plan &plan, hipStream_t st)
         size_t lds = ShapeQ<DT, DP>::LDS;
         if constexpr (FlowQ<DT, DP>::FITS) {
             if (!plan.any) {
-                fn = (const void *)attend_grad_q_flow<DT, DP>;
+                fn = p.words ? (const void *)attend_grad_q_flow<DT, DP, true>
+                             : (const void *)attend_grad_q_flow<DT, DP, false>;
                 lds = FlowQ<DT, DP>::LDS;
             }
         }
@@ -1050,8 +1080,53 @@ int run(Backward &p, const Plan &plan, hipStream_t st)
 }
 
 template <int DT>
-int run_width(Backward &p, const Plan &plan, hipStream_t st)
+int run_width(const flashlayer_attention *a, Backward &p, const Plan &plan, void *workspace, hipStream_t st)
 {
+    p.rq = p.q;
+    p.rq_b = p.qb;
+    p.rq_g = p.share * p.qh;
+    p.rq_r = p.qr;
+    p.rq_h = p.qh;
+    p.rg = p.g;
+    p.rg_b = p.ob;
+    p.rg_g = p.share * p.oh;
+    p.rg_r = p.orow;
+    p.rg_h = p.oh;
+    p.rshare = p.share;
+    p.Dr = p.D;
+    if (plan.copies && a->Lk) {
+        if (const int rc = copy_keys<DT>(a, p, static_cast<char *>(workspace), st)) return rc;
+        if (odd_of(a) && p.gk && p.rows) {
+            Copy c{};
+            const uint64_t each = rows_copy_bytes(a, p.rows, a->Hk);
+            c.from[0] = p.q;
+            c.from[1] = p.g;
+            c.to[0] = static_cast<char *>(workspace) + keys_copy_bytes(a);
+            c.to[1] = c.to[0] + each;
+            c.batch[0] = p.qb;
+            c.batch[1] = p.ob;
+            c.row[0] = p.qr;
+            c.row[1] = p.orow;
+            c.head[0] = p.qh;
+            c.head[1] = p.oh;
+            c.group[0] = p.rq_g;
+            c.group[1] = p.rg_g;
+            c.heads = a->Hk;
+            c.rows = p.rows;
+            c.share = p.share;
+            c.D = a->D;
+            p.Dr = whole_head(a);
+            c.granules = p.Dr * elem_size(DT) / 16;
+            if (const int rc = copy_rows<DT>(c, a->B, st)) return rc;
+            p.rq = c.to[0];
+            p.rg = c.to[1];
+            p.rq_r = p.rg_r = (int64_t)p.Dr * elem_size(DT);
+            p.rq_h = p.rg_h = 0;
+            p.rq_g = p.rg_g = p.rq_r * p.rows;
+            p.rq_b = p.rg_b = p.rq_g * a->Hk;
+            p.rshare = 1;
+        }
+    }
     const uint64_t tiles = size_prod({(uint64_t)p.B, (uint64_t)p.Hk, (uint64_t)plan.row_tiles});
     if (const int rc = launch_kernel((const void *)attend_rows<DT>, tiles, 256, p, 0, st)) return rc;
     switch (plan.dp) {
@@ -1126,7 +1201,7 @@ extern "C" int flashlayer_attention_backward(const flashlayer_attention *args, c
     p.gv = static_cast<char *>(grad_v);
     p.row_tiles = plan.row_tiles;
     p.padded = plan.padded;
-    char *ws = static_cast<char *>(workspace);
+    char *ws = static_cast<char *>(workspace) + copy_bytes(args, plan);
     p.data = reinterpret_cast<RowData *>(ws);
     ws += data_bytes(args);
     p.lose = reinterpret_cast<float *>(ws);
@@ -1136,6 +1211,6 @@ extern "C" int flashlayer_attention_backward(const flashlayer_attention *args, c
     p.largest = reinterpret_cast<float *>(ws);
     p.part = reinterpret_cast<float *>(ws + largest_bytes(args, plan));
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (a.dtype == FLASHBEV_F32) return run_width<FLASHBEV_F32>(p, plan, st);
-    return a.dtype == FLASHBEV_F16 ? run_width<FLASHBEV_F16>(p, plan, st) : run_width<FLASHBEV_BF16>(p, plan, st);
+    if (a.dtype == FLASHBEV_F32) return run_width<FLASHBEV_F32>(args, p, plan, workspace, st);
+    return a.dtype == FLASHBEV_F16 ? run_width<FLASHBEV_F16>(args, p, plan, workspace, st) : run_width<FLASHBEV_BF16>(args, p, plan, workspace, st);
 }

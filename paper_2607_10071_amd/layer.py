@@ -126,16 +126,17 @@ def _scale(scale, D: int) -> float:
     return (D or 1) ** -0.5 if scale is None else scale
 
 
+# (whether a mask has heads and rows of its own decides how it is read)
 @functools.lru_cache(maxsize=4096)
-def _attention_need(B, Lq, Lk, H, Hk, D, code) -> int:
+def _attention_need(B, Lq, Lk, H, Hk, D, code, kind, heads: bool, rows: bool) -> int:
     return _size("flashlayer_attention_workspace_size", "PP",
-                 _PACK_ATTENTION.pack(*[0] * 15, B, Lq, Lk, H, Hk, D, code, 0, 1.0))
+                 _PACK_ATTENTION.pack(*[0] * 13, heads, rows, B, Lq, Lk, H, Hk, D, code, kind, 1.0))
 
 
 @functools.lru_cache(maxsize=4096)
-def _attention_backward_need(B, Lq, Lk, H, Hk, D, code, q: bool, kv: bool) -> int:
+def _attention_backward_need(B, Lq, Lk, H, Hk, D, code, kind, heads: bool, rows: bool, q: bool, kv: bool) -> int:
     return _size("flashlayer_attention_backward_workspace_size", "PiiP",
-                 _PACK_ATTENTION.pack(*[0] * 15, B, Lq, Lk, H, Hk, D, code, 0, 1.0), q, kv)
+                 _PACK_ATTENTION.pack(*[0] * 13, heads, rows, B, Lq, Lk, H, Hk, D, code, kind, 1.0), q, kv)
 
 
 def attention_forward(q, k, v, mask=None, key_lengths=None, scale=None, out=None, rest=None, stats=None,
@@ -206,7 +207,7 @@ def _attention_call(q, k, v, mask, key_lengths, scale, out, rest, stats, stream)
     dev = _one_device(q, k, v, mask, key_lengths, out, rest, stats)
     s = _stream_handle(stream, dev)
     args = _PACK_ATTENTION.pack(*qs, *ks, *vs, *os, mb, mh, mr, *sizes, code, kind, _scale(scale, D))
-    need = _attention_need(*sizes, code)
+    need = _attention_need(*sizes, code, kind, mh != 0, mr != 0)
     ws = _workspace(need, dev, s) if need else None
     return (_packed_call("flashlayer_attention_forward", "PPPPPPPPPPQP"),
             (args, q.data_ptr(), k.data_ptr(), v.data_ptr(), _addr(mask), lengths, out.data_ptr(),
@@ -261,7 +262,7 @@ def _attention_gradients(grad_out, q, k, v, out, rest, stats, mask, key_lengths,
     gq = torch.empty(q.shape, dtype=q.dtype, device=dev) if want_q else None
     gk, gv = ((torch.empty(k.shape, dtype=q.dtype, device=dev) for _ in "kv") if want_kv else (None, None))
     args = _PACK_ATTENTION.pack(*qs, *ks, *vs, *gs, mb, mh, mr, *sizes, code, kind, _scale(scale, D))
-    need = _attention_backward_need(*sizes, code, want_q, want_kv)
+    need = _attention_backward_need(*sizes, code, kind, mh != 0, mr != 0, want_q, want_kv)
     ws = _workspace(need, dev, s) if need else None
     call = _packed_call("flashlayer_attention_backward", "PPPPPPPPPPPPPPQP")
     with _on_device(dev):

@@ -95,7 +95,7 @@ def masks(kind, B, H, Lq, Lk, dtype, g):
 @pytest.mark.parametrize("kind", ["lengths", "keys", "keys_of_heads", "pairs", "all", "nothing", "add", "inf", "lowest",
                                   "of_type"])
 @pytest.mark.parametrize("shape", [(2, 40, 150, 4, 2, 32), (3, 1, 777, 6, 3, 72), (2, 131, 97, 2, 2, 128),
-                                   (1, 20, 1100, 2, 2, 37)], ids=lambda s: "x".join(map(str, s)))
+                                   (1, 20, 1100, 2, 2, 37), (1, 70, 2500, 2, 1, 41)], ids=lambda s: "x".join(map(str, s)))
 @pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
 def test_masks(shape, kind, dtype):
     (q, k, v, g), gen = make(*shape, dtype, seed=3)
