@@ -312,9 +312,9 @@ __global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) at
     put_row<DT, DP, MASK>(p, b, g, split, r, qi, head, m, l, o, h);
 }
 
-// Without masks that differ from row to row: four wavefronts of 32 rows each share tiles of TK keys, which go from memory to LDS
-// without passing registers, and take them 32 keys at a time.  In one step a wavefront forms the
-// next 32 keys' scores, this 32's weights and the product of the last 32's with v: matrix
+// Without masks that differ from row to row: four wavefronts of 32 rows each share tiles of TK keys,
+// which go from memory to LDS without passing registers, and take them 32 keys at a time.  In one
+// step a wavefront forms the next 32 keys' scores, this 32's weights and the product of the last 32's with v: matrix
 // and vector instructions that do not wait for each other, in turn.  (Scores, then weights, then
 // the product: 2048 queries of 32 heads x 4096 keys x 128 bf16 165 us.)
 template <int DT, int DP>
@@ -324,15 +324,12 @@ struct Flow {
     using T = Strip<DT, DP, TK>;
     // K of two tiles and V of three: a tile's last product is taken with the next one's first step
     static constexpr int LDS = 5 * T::BYTES;
-    // (the place in LDS that a load is told has 17 bits: what went past 128 KiB arrived at its
-    // start.  float32 heads of 128 channels take attend.)
-    static_assert(DP * elem_size(DT) >= 512 || LDS <= 131072, "within a load's reach");
 };
 
 // Wavefronts a SIMD that the registers are to leave room for.
 constexpr int flow_waves(int dt, int dp)
 {
-    return dp * elem_size(dt) <= 64 ? 4 : 2;
+    return dp * elem_size(dt) <= 64 ? 4 : dp * elem_size(dt) < 512 ? 2 : 1;
 }
 
 // KEYS: some keys are left out, by their bits.
@@ -600,7 +597,7 @@ Plan plan_of(const flashlayer_attention *a)
     Plan p{};
     const int64_t rows = (int64_t)a->Lq * (a->Hk ? a->H / a->Hk : 1);
     p.dp = padded_head(a->D);
-    const bool flows = !pairs_of(a) && p.dp * elem_size(a->dtype) < 512;
+    const bool flows = !pairs_of(a);
     const int64_t problems = (int64_t)a->B * a->Hk;
     p.wq = rows <= 32 ? 1 : flows ? 4 : 5;
     p.copies = p.wq == 4 && copies_keys(a);
@@ -636,13 +633,10 @@ int run(Forward &p, const Plan &plan, hipStream_t st)
 {
     const void *fn = nullptr;
     size_t lds = 0;
-    if constexpr (DP * elem_size(DT) < 512) {
-        if (plan.wq == 4) {
-            fn = p.words ? (const void *)attend_flow<DT, DP, true> : (const void *)attend_flow<DT, DP, false>;
-            lds = Flow<DT, DP>::LDS;
-        }
-    }
-    if (plan.wq == 5) {
+    if (plan.wq == 4) {
+        fn = p.words ? (const void *)attend_flow<DT, DP, true> : (const void *)attend_flow<DT, DP, false>;
+        lds = Flow<DT, DP>::LDS;
+    } else if (plan.wq == 5) {
         fn = (const void *)attend<DT, DP, 4, true>;
         lds = Shape<DT, DP, 4>::LDS;
     } else if (plan.wq == 1) {

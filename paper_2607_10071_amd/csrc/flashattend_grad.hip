@@ -532,7 +532,6 @@ struct FlowQ {
     static constexpr int SUBS = TK / 32;
     using T = Strip<DT, DP, TK>;
     static constexpr int LDS = 5 * T::BYTES;   // V of two tiles and K of three
-    static constexpr bool FITS = LDS <= 131072;   // a load's reach
 };
 
 constexpr int grad_q_waves(int dt, int dp)
@@ -721,10 +720,11 @@ struct FlowK {
     using T = Strip<DT, DP, TR>;
     static constexpr int DATA = TR * 8;          // the rows' exponents and deltas
     static constexpr int STAGE = 2 * T::BYTES + DATA, LDS = 3 * STAGE;
-    // Heads of up to 32 16-bit channels have vector instructions for twice the products' time, and
-    // four wavefronts a SIMD of attend_grad_kv do them faster than two of this kernel: 900
-    // queries x 40000 states 115 us and 131.
-    static constexpr bool FITS = LDS <= 131072 && DP * elem_size(DT) > 64;
+    // Three stages of float32 heads of 128 channels are more than a CU's LDS.  Heads of up to 32
+    // 16-bit channels have vector instructions for twice the products' time, and four wavefronts
+    // a SIMD of attend_grad_kv do them faster than two of this kernel: 900 queries x 40000 states
+    // 115 us and 131.
+    static constexpr bool FITS = LDS <= 160 * 1024 - 64 && DP * elem_size(DT) > 64;
 };
 
 constexpr int grad_kv_waves(int dt, int dp)
@@ -971,14 +971,17 @@ struct Plan {
     int k_tiles, k_splits;
 };
 
-int splits_of(int64_t base, int64_t steps)
+// Splits where there are fewer than `enough` workgroups, for about `wanted`.
+int splits_of(int64_t base, int64_t steps, int64_t enough, int64_t wanted)
 {
-    if (base <= 0 || base >= 2 * kCusOfCard) return 1;
-    const int64_t want = (3 * kCusOfCard + base - 1) / base;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(want, steps / 2));
+    if (base <= 0 || base >= enough) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>((wanted + base - 1) / base, steps / 2));
 }
 
-// Splits as the forward's: where there are fewer than two workgroups a CU, for about three.
+// grad_q is split over the keys as the forward is.  grad_k and grad_v, whose parts are two tensors
+// and whose wide heads fill a CU with one workgroup, are split over the rows below one a CU alone
+// (2 x 4 x 32 tiles of 128 keys x 128 bf16: a training pass 619 us whole, 645 and 661 in two
+// and three parts).
 Plan plan_of(const flashlayer_attention *a)
 {
     Plan p{};
@@ -989,9 +992,9 @@ Plan plan_of(const flashlayer_attention *a)
     p.padded = (int)((rows + 127) / 128 * 128);
     p.row_tiles = p.padded / kRowTile;
     p.q_tiles = (int)((rows + 127) / 128);
-    p.q_splits = splits_of(problems * p.q_tiles, (a->Lk + 63) / 64);
+    p.q_splits = splits_of(problems * p.q_tiles, (a->Lk + 63) / 64, 2 * kCusOfCard, 3 * kCusOfCard);
     p.k_tiles = (a->Lk + 127) / 128;
-    p.k_splits = splits_of(problems * p.k_tiles, (rows + 63) / 64);
+    p.k_splits = splits_of(problems * p.k_tiles, (rows + 63) / 64, kCusOfCard, 2 * kCusOfCard);
     return p;
 }
 
@@ -1039,12 +1042,10 @@ int run(Backward &p, const Plan &plan, hipStream_t st)
         if (const int rc = deal(p, size_prod({problems, (uint64_t)p.tiles, (uint64_t)p.splits}))) return rc;
         const void *fn = (const void *)attend_grad_q<DT, DP, true>;
         size_t lds = ShapeQ<DT, DP>::LDS;
-        if constexpr (FlowQ<DT, DP>::FITS) {
-            if (!plan.any) {
-                fn = p.words ? (const void *)attend_grad_q_flow<DT, DP, true>
-                             : (const void *)attend_grad_q_flow<DT, DP, false>;
-                lds = FlowQ<DT, DP>::LDS;
-            }
+        if (!plan.any) {
+            fn = p.words ? (const void *)attend_grad_q_flow<DT, DP, true>
+                         : (const void *)attend_grad_q_flow<DT, DP, false>;
+            lds = FlowQ<DT, DP>::LDS;
         }
         if (const int rc = launch_lds(fn, 8ull * p.per_xcd, p, lds, st)) return rc;
         if (p.splits > 1) {

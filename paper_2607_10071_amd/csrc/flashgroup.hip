@@ -106,6 +106,48 @@ __device__ __forceinline__ float pivot(const Group &p, int64_t n, int g)
     return load_elem<DT>(p.x + n * p.R * p.ldx * elem_size(DT), g * p.per);
 }
 
+// Rows r, r + step, .. of a batch, in flight together: all eight, or the first `rows`.
+template <int DT, class W>
+__device__ __forceinline__ void load_batch(u32x4 (&raw)[kBatch], const char *x, int64_t ld, int64_t r, int64_t step,
+                                           int rows, W whole, int c, int C)
+{
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+        raw[b] = u32x4{0, 0, 0, 0};
+        if (whole.value || b < rows) raw[b] = Lane<DT>::load(x + (r + b * step) * ld * Lane<DT>::ES, c, C);
+    }
+}
+
+// A batch's means, from `from`, and sums of squared differences.
+template <int DT, class W>
+__device__ __forceinline__ void batch_stats(const u32x4 (&raw)[kBatch], int rows, W whole,
+                                            const float (&from)[Lane<DT>::V], float (&s)[Lane<DT>::V],
+                                            float (&q)[Lane<DT>::V])
+{
+    using L = Lane<DT>;
+    float v[L::V];
+#pragma unroll
+    for (int i = 0; i < L::V; ++i) s[i] = q[i] = 0.0f;
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+        L::floats(raw[b], v);
+#pragma unroll
+        for (int i = 0; i < L::V; ++i) s[i] += whole.value || b < rows ? v[i] - from[i] : 0.0f;
+    }
+    const float share = whole.value ? 1.0f / kBatch : 1.0f / (float)rows;
+#pragma unroll
+    for (int i = 0; i < L::V; ++i) s[i] *= share;
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+        L::floats(raw[b], v);
+#pragma unroll
+        for (int i = 0; i < L::V; ++i) {
+            const float d = whole.value || b < rows ? v[i] - from[i] - s[i] : 0.0f;
+            q[i] = __builtin_fmaf(d, d, q[i]);
+        }
+    }
+}
+
 // A lane's channels over the rows r0, r0 + step, .. < r1: means, from their groups' pivots, and
 // sums of squared differences; returns the number of rows.  Eight rows' mean and differences are
 // formed in registers, then joined: 5 operations an element, where row by row would take 7 and a
@@ -116,7 +158,6 @@ __device__ __forceinline__ float lane_stats(const Group &p, int64_t n_, int c, i
 {
     using L = Lane<DT>;
     const char *x = p.x + n_ * p.R * p.ldx * L::ES;
-    const int64_t ld = p.ldx;
     float n = 0.0f, from[L::V];
 #pragma unroll
     for (int i = 0; i < L::V; ++i) {
@@ -125,32 +166,9 @@ __device__ __forceinline__ float lane_stats(const Group &p, int64_t n_, int c, i
     }
     const auto batch = [&](int64_t r, int rows, auto whole) {
         u32x4 raw[kBatch];
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            raw[b] = u32x4{0, 0, 0, 0};
-            if (whole.value || b < rows) raw[b] = L::load(x + (r + b * step) * ld * L::ES, c, C);
-        }
-        float s[L::V], q[L::V], v[L::V];
-#pragma unroll
-        for (int i = 0; i < L::V; ++i) s[i] = q[i] = 0.0f;
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            L::floats(raw[b], v);
-#pragma unroll
-            for (int i = 0; i < L::V; ++i) s[i] += whole.value || b < rows ? v[i] - from[i] : 0.0f;
-        }
-        const float share = whole.value ? 1.0f / kBatch : 1.0f / (float)rows;
-#pragma unroll
-        for (int i = 0; i < L::V; ++i) s[i] *= share;
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            L::floats(raw[b], v);
-#pragma unroll
-            for (int i = 0; i < L::V; ++i) {
-                const float d = whole.value || b < rows ? v[i] - from[i] - s[i] : 0.0f;
-                q[i] = __builtin_fmaf(d, d, q[i]);
-            }
-        }
+        float s[L::V], q[L::V];
+        load_batch<DT>(raw, x, p.ldx, r, step, rows, whole, c, C);
+        batch_stats<DT>(raw, rows, whole, from, s, q);
 #pragma unroll
         for (int i = 0; i < L::V; ++i) join(mean[i], sq[i], n, s[i], q[i], (float)rows);
         n += (float)rows;
@@ -159,35 +177,6 @@ __device__ __forceinline__ float lane_stats(const Group &p, int64_t n_, int c, i
     for (; r + (kBatch - 1) * step < r1; r += kBatch * step) batch(r, kBatch, std::true_type{});
     if (r < r1) batch(r, (int)((r1 - r + step - 1) / step), std::false_type{});
     return n;
-}
-
-// Over the lanes of a column (`rows` of them, lane rr of `width` columns): lane 0 ends with all.
-template <int V>
-__device__ __forceinline__ void column_stats(float *lds, int rr, int rows, int cv, int width, float (&mean)[V],
-                                             float (&sq)[V], float &n)
-{
-    float *at = lds + (rr * width + cv) * (2 * V + 1);
-    for (int left = rows; left > 1;) {
-        const int half = (left + 1) / 2;
-        if (rr >= half && rr < left) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                at[i] = mean[i];
-                at[V + i] = sq[i];
-            }
-            at[2 * V] = n;
-        }
-        __syncthreads();
-        if (rr + half < left) {
-            const float *o = at + half * width * (2 * V + 1);
-            const float m = o[2 * V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) join(mean[i], sq[i], n, o[i], o[V + i], m);
-            n += m;
-        }
-        __syncthreads();
-        left = half;
-    }
 }
 
 // The (mean, squares, count) of `width` neighbouring lanes, a power of two; all end with the whole.
@@ -232,8 +221,8 @@ __device__ __forceinline__ Place place_of(const Group &p, uint32_t id, int threa
 // The statistics of the groups that columns c0 .. c1 - 1 hold (parts of), of their channels' in
 // `lds` (means, then sums of squared differences `vecs` * V further on), each of `rows` values.
 // As many lanes to a group as it has channels, up to a wavefront; `put` gets the group, its
-// mean, squares and count in one lane.  (A wavefront to each group of 8 channels was most of
-// the pass: 139200 x 256 in 32 groups 38 us of 38.)
+// mean, squares and count in one lane.  (The first pass of 139200 x 256 in 32 groups by 972
+// workgroups: 25.6 us, 38 with a wavefront to each group of 8 channels.)
 template <class F>
 __device__ __forceinline__ void join_channels(const float *lds, int squares, int c0, int c1, int per, float rows,
                                               int waves, F put)
@@ -255,16 +244,44 @@ __device__ __forceinline__ void join_channels(const float *lds, int squares, int
     }
 }
 
-// Lanes 0 of the columns leave their channels' statistics in LDS.
-template <int V>
-__device__ __forceinline__ void leave_channels(float *lds, const Place &l, const float (&mean)[V],
-                                               const float (&sq)[V])
+// The channels' statistics of all lanes' of a column (l.rows of them): means in the first l.vecs V
+// of `out`, then squares.  Up to a wavefront's lanes to a channel, which join the rows' lanes in
+// turn and then each other.  (Six samples of 704 x 32 float32 in one launch: 8.8 us, 9.6 with a
+// tree over the rows, which takes two barriers a level.)
+template <int V, int THREADS>
+__device__ __forceinline__ void channel_stats(float *lds, float *out, const Place &l, const float (&mean)[V],
+                                              const float (&sq)[V], float n)
 {
-    if (l.rr == 0) {   // (in the tree's place, which nobody reads any more)
+    constexpr int S = 2 * V + 1;
+    if (l.rr < l.rows) {
+        float *at = lds + (l.rr * l.vecs + l.cv) * S;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            lds[l.cv * V + i] = mean[i];
-            lds[l.vecs * V + l.cv * V + i] = sq[i];
+            at[i] = mean[i];
+            at[V + i] = sq[i];
+        }
+        at[2 * V] = n;
+    }
+    __syncthreads();
+    const int channels = l.vecs * V;
+    int width = 1;
+    while (width < 64 && width < l.rows && 2 * width * channels <= THREADS) width *= 2;
+    const int lane = threadIdx.x & (width - 1);
+    // (whole wavefronts go round together: their lanes exchange values)
+    for (int base = 0; base < channels; base += THREADS / width) {
+        const int c = base + (int)threadIdx.x / width;
+        float m = 0.0f, s = 0.0f, k = 0.0f;
+        if (c < channels) {
+            const float *at = lds + (lane * l.vecs + c / V) * S;
+            for (int r = lane; r < l.rows; r += width, at += width * l.vecs * S) {
+                join(m, s, k, at[c % V], at[V + c % V], at[2 * V]);
+                k += at[2 * V];
+            }
+        }
+        wave_stats(m, s, k, width);
+        if (lane == 0 && c < channels) {
+            out[c] = m;
+            out[channels + c] = s;
         }
     }
     __syncthreads();
@@ -275,7 +292,7 @@ template <int DT>
 __global__ void __launch_bounds__(256) group_stats(Group p)
 {
     using L = Lane<DT>;
-    __shared__ float lds[256 * (2 * L::V + 1)];
+    __shared__ float lds[256 * (2 * L::V + 1)], channels[2 * 256 * L::V];
     const uint32_t id = block_index();
     if (id >= (uint64_t)p.N * p.chunks * p.slices) return;
     const Place l = place_of<L::V>(p, id, 256);
@@ -283,11 +300,10 @@ __global__ void __launch_bounds__(256) group_stats(Group p)
     const int c = l.c0 + l.cv * L::V;
     if (l.rr < l.rows)
         n = lane_stats<DT>(p, l.n, c, l.c1, l.r0 + l.rr, l.r1, l.rows, mean, sq);
-    column_stats<L::V>(lds, l.rr, l.rows, l.cv, l.vecs, mean, sq, n);
-    leave_channels<L::V>(lds, l, mean, sq);
+    channel_stats<L::V, 256>(lds, channels, l, mean, sq, n);
     float *o = p.partial + (l.n * p.chunks + l.chunk) * 2 * (p.groups + p.slices);
     const int s = l.c0 / p.slice;
-    join_channels(lds, l.vecs * L::V, l.c0, l.c1, p.per, (float)(l.r1 - l.r0), 4, [&](int g, float m, float q, float) {
+    join_channels(channels, l.vecs * L::V, l.c0, l.c1, p.per, (float)(l.r1 - l.r0), 4, [&](int g, float m, float q, float) {
         o[2 * (g + s)] = m;
         o[2 * (g + s) + 1] = q;
     });
@@ -336,30 +352,60 @@ struct Factors {
     static constexpr int V = Lane<DT>::V;
     float mean[V], rstd[V], w[V], b[V];
 
-    __device__ __forceinline__ void load(const Group &p, const float *stats, int c, int end)
+    __device__ __forceinline__ void load_params(const Group &p, int c, int end)
     {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int ci = min(c + i, end - 1), g = ci / p.per;
-            mean[i] = stats[2 * g];
-            rstd[i] = stats[2 * g + 1];
+            const int ci = min(c + i, end - 1);
             w[i] = param(p.weight, p.param_f32, DT, ci, 1.0f);
             b[i] = param(p.bias, p.param_f32, DT, ci, 0.0f);
         }
     }
+
+    __device__ __forceinline__ void load_stats(const Group &p, const float *stats, int c, int end)
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int g = min(c + i, end - 1) / p.per;
+            mean[i] = stats[2 * g];
+            rstd[i] = stats[2 * g + 1];
+        }
+    }
+
+    __device__ __forceinline__ void load(const Group &p, const float *stats, int c, int end)
+    {
+        load_params(p, c, end);
+        load_stats(p, stats, c, end);
+    }
+
+    // w becomes rstd weight
+    __device__ __forceinline__ void fold()
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[i] *= rstd[i];
+    }
+
+    // A row's y, after fold().
+    template <int ACT>
+    __device__ __forceinline__ void put(char *y, u32x4 raw, int c, int end) const
+    {
+        float v[V];
+        Lane<DT>::floats(raw, v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = act_value(ACT, __builtin_fmaf(v[i] - mean[i], w[i], b[i]));
+        Lane<DT>::store(y, c, end, v);
+    }
 };
 
 template <int DT, int ACT>
-__device__ __forceinline__ void apply_rows(const Group &p, const Factors<DT> &f, int64_t n, int c, int c1,
-                                           int64_t r0, int64_t r1, int64_t step)
+__device__ __forceinline__ void apply_rows(const Group &p, Factors<DT> &f, int64_t n, int c, int c1, int64_t r0,
+                                           int64_t r1, int64_t step)
 {
     using L = Lane<DT>;
     constexpr int U = 4;
     const char *x = p.x + n * p.R * p.ldx * L::ES;
     char *y = p.y + n * p.R * p.ldy * L::ES;
-    float a[L::V];   // rstd weight
-#pragma unroll
-    for (int i = 0; i < L::V; ++i) a[i] = f.rstd[i] * f.w[i];
+    f.fold();
     for (int64_t r = r0; r < r1; r += U * step) {
         u32x4 raw[U];
 #pragma unroll
@@ -368,11 +414,7 @@ __device__ __forceinline__ void apply_rows(const Group &p, const Factors<DT> &f,
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (r + u * step >= r1) break;
-            float v[L::V];
-            L::floats(raw[u], v);
-#pragma unroll
-            for (int i = 0; i < L::V; ++i) v[i] = act_value(ACT, __builtin_fmaf(v[i] - f.mean[i], a[i], f.b[i]));
-            L::store(y + (r + u * step) * p.ldy * L::ES, c, c1, v);
+            f.template put<ACT>(y + (r + u * step) * p.ldy * L::ES, raw[u], c, c1);
         }
     }
 }
@@ -392,43 +434,57 @@ __global__ void __launch_bounds__(256) group_apply(Group p)
     apply_rows<DT, ACT>(p, f, l.n, c, l.c1, l.r0 + l.rr, l.r1, l.rows);
 }
 
-// Both passes by one workgroup for a sample's slice of whole groups (small maps: one launch in
-// place of three).
-constexpr int kWhole = 1024;
+// Both passes by one workgroup for a sample's slice of whole groups, of up to eight rows a lane,
+// which stay in registers between them (small maps: one launch in place of three).
+constexpr int kWhole = 512;
 
 template <int DT, int ACT>
 __global__ void __launch_bounds__(kWhole) group_whole(Group p)
 {
     using L = Lane<DT>;
-    __shared__ float lds[kWhole * (2 * L::V + 1)];
+    __shared__ float lds[kWhole * (2 * L::V + 1)], channels[2 * (kWhole + L::V)];
     __shared__ float stats[2 * kWhole];   // of the slice's groups
     const uint32_t id = block_index();
     if (id >= (uint64_t)p.N * p.slices) return;
-    const Place l = place_of<L::V>(p, id, kWhole);
-    const int c = l.c0 + l.cv * L::V;
-    float mean[L::V], sq[L::V], n = 0.0f;
-    if (l.rr < l.rows)
-        n = lane_stats<DT>(p, l.n, c, l.c1, l.r0 + l.rr, l.r1, l.rows, mean, sq);
-    column_stats<L::V>(lds, l.rr, l.rows, l.cv, l.vecs, mean, sq, n);
-    leave_channels<L::V>(lds, l, mean, sq);
+    const int64_t n = id / p.slices;
+    Place l;
+    l.c0 = (id - (uint32_t)n * p.slices) * p.slice;
+    l.c1 = min(l.c0 + p.slice, p.C);
+    l.vecs = (l.c1 - l.c0 + L::V - 1) / L::V;
+    l.rr = threadIdx.x / l.vecs;
+    l.cv = threadIdx.x - l.rr * l.vecs;
+    const int R = (int)p.R;
+    l.rows = min(kWhole / l.vecs, R);
+    const int c = l.c0 + l.cv * L::V, mine = l.rr < l.rows ? (R - l.rr + l.rows - 1) / l.rows : 0;
+    u32x4 raw[kBatch];
+    load_batch<DT>(raw, p.x + n * p.R * p.ldx * L::ES, p.ldx, l.rr, l.rows, mine, std::false_type{}, c, l.c1);
+    Factors<DT> f;
+    f.load_params(p, c, l.c1);
+    float mean[L::V], sq[L::V], from[L::V], count = (float)mine;
+#pragma unroll
+    for (int i = 0; i < L::V; ++i) from[i] = pivot<DT>(p, n, min(c + i, l.c1 - 1) / p.per);
+    batch_stats<DT>(raw, max(mine, 1), std::false_type{}, from, mean, sq);
+    channel_stats<L::V, kWhole>(lds, channels, l, mean, sq, count);
     const int g0 = l.c0 / p.per;
-    join_channels(lds, l.vecs * L::V, l.c0, l.c1, p.per, (float)p.R, kWhole / 64,
+    join_channels(channels, l.vecs * L::V, l.c0, l.c1, p.per, (float)R, kWhole / 64,
                   [&](int g, float m, float q, float k) {
                       const float r = 1.0f / sqrtf(q / k + p.eps);
-                      m += pivot<DT>(p, l.n, g);
+                      m += pivot<DT>(p, n, g);
                       stats[2 * (g - g0)] = m;
                       stats[2 * (g - g0) + 1] = r;
                       if (p.stats) {
-                          float *o = p.stats + 2 * (l.n * p.groups + g);
+                          float *o = p.stats + 2 * (n * p.groups + g);
                           o[0] = m;
                           o[1] = r;
                       }
                   });
     __syncthreads();
-    if (l.rr >= l.rows) return;
-    Factors<DT> f;
-    f.load(p, stats - 2 * g0, c, l.c1);
-    apply_rows<DT, ACT>(p, f, l.n, c, l.c1, l.r0 + l.rr, l.r1, l.rows);
+    f.load_stats(p, stats - 2 * g0, c, l.c1);
+    f.fold();
+    char *y = p.y + (n * p.R + l.rr) * p.ldy * L::ES;
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b)
+        if (b < mine) f.template put<ACT>(y + (int64_t)b * l.rows * p.ldy * L::ES, raw[b], c, l.c1);
 }
 
 // ---------------------------------------------------------------------------
@@ -659,7 +715,8 @@ int check(const flashlayer_group_norm *a)
 
 // How a call is cut.  Chunks of rows: a lane's batch of eight rows at least, and more where that
 // would be over 768 workgroups, the three of a CU that run at once in the backward (139200 x 256
-// bf16, a training step's first and second backward passes: XX us, 45 + 48 of 972, 39 + 40 of 498).
+// bf16, a training step's first and second backward passes: 33 + 39 us,
+// 45 + 48 of 972, 39 + 40 of 498).
 struct Cut {
     bool whole;
     int slices, slice, chunks;
@@ -670,11 +727,12 @@ Cut cut(const flashlayer_group_norm *a, bool backward)
 {
     const int es = elem_size(a->dtype), V = 16 / es, per = a->C / a->groups;
     Cut c{};
-    // one workgroup takes up to 32768 elements: 22528 x float32 (704 x 32) 5 us in one launch
-    const int some = ((64 / es + per - 1) / per) * per;   // whole groups of 64 bytes or more
-    if (!backward && some <= kWhole && a->R * std::min(some, a->C) <= 32768) {
+    // whole groups of 64 bytes or more to one workgroup, eight rows at most to its lanes (six samples
+    // of 704 x 32 float32 8.8 us a call, 13.9 in three launches; eight of 128 x 1024 bf16 10.0 and 20.5)
+    const int some = std::min(((64 / es + per - 1) / per) * per, a->C);
+    if (!backward && some <= kWhole && a->R <= kBatch * (kWhole / ((some + V - 1) / V))) {
         c.whole = true;
-        c.slice = std::min(some, a->C);
+        c.slice = some;
         c.slices = (a->C + c.slice - 1) / c.slice;
         c.chunks = 1;
         c.chunk = a->R;
