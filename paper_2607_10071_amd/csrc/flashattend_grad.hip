@@ -720,11 +720,14 @@ struct FlowK {
     using T = Strip<DT, DP, TR>;
     static constexpr int DATA = TR * 8;          // the rows' exponents and deltas
     static constexpr int STAGE = 2 * T::BYTES + DATA, LDS = 3 * STAGE;
-    // Three stages of float32 heads of 128 channels are more than a CU's LDS.  Heads of up to 32
-    // 16-bit channels have vector instructions for twice the products' time, and four wavefronts
-    // a SIMD of attend_grad_kv do them faster than two of this kernel: 900 queries x 40000 states
-    // 115 us and 131.
-    static constexpr bool FITS = LDS <= 160 * 1024 - 64 && DP * elem_size(DT) > 64;
+    // Three stages of float32 heads of 128 channels are more than a CU's LDS: their gradients are
+    // all taken by the kernels with masks.
+    static constexpr bool ROOM = DP * elem_size(DT) < 512;
+    static_assert(!ROOM || LDS <= 160 * 1024 - 64);
+    // Heads of up to 32 16-bit channels have vector instructions for twice the products' time, and
+    // four wavefronts a SIMD of attend_grad_kv do them faster than two of this kernel: 900 queries
+    // x 40000 states 115 us and 131.
+    static constexpr bool FITS = ROOM && DP * elem_size(DT) > 64;
 };
 
 constexpr int grad_kv_waves(int dt, int dp)
@@ -1042,10 +1045,12 @@ int run(Backward &p, const Plan &plan, hipStream_t st)
         if (const int rc = deal(p, size_prod({problems, (uint64_t)p.tiles, (uint64_t)p.splits}))) return rc;
         const void *fn = (const void *)attend_grad_q<DT, DP, true>;
         size_t lds = ShapeQ<DT, DP>::LDS;
-        if (!plan.any) {
-            fn = p.words ? (const void *)attend_grad_q_flow<DT, DP, true>
-                         : (const void *)attend_grad_q_flow<DT, DP, false>;
-            lds = FlowQ<DT, DP>::LDS;
+        if constexpr (FlowK<DT, DP>::ROOM) {
+            if (!plan.any) {
+                fn = p.words ? (const void *)attend_grad_q_flow<DT, DP, true>
+                             : (const void *)attend_grad_q_flow<DT, DP, false>;
+                lds = FlowQ<DT, DP>::LDS;
+            }
         }
         if (const int rc = launch_lds(fn, 8ull * p.per_xcd, p, lds, st)) return rc;
         if (p.splits > 1) {

@@ -285,3 +285,40 @@ def test_same_bits_again_and_on_another_stream():
     call()
     call()
     assert torch.equal(out, first[0])
+
+
+@pytest.mark.parametrize("lq", [1, 150])
+def test_a_long_cache(lq):
+    """Rows and batches further into a cache than 32 bits reach, in elements too."""
+    B, Lk, row = 2, 2300, 1 << 20
+    cache = torch.empty(B * Lk * row, dtype=F16, device="cuda")   # 9.6 GB, of which 64 channels a row
+    k = cache.as_strided((B, Lk, 1, 64), (Lk * row, row, 64, 1))
+    v = cache.as_strided((B, Lk, 1, 64), (Lk * row, row, 64, 1), 128)
+    assert k.stride(0) + (Lk - 1) * row > 1 << 32
+    (q, k0, v0, g), _ = make(B, lq, Lk, 1, 1, 64, F16)
+    k.copy_(k0)
+    v.copy_(v0)
+    n = torch.tensor([Lk, Lk - 100], dtype=torch.int32, device="cuda")
+    stats, stats0 = (torch.empty((B, 1, lq, 2), device="cuda") for _ in range(2))
+    out = fb.attention_forward(q, k, v, key_lengths=n, stats=stats)
+    out0 = fb.attention_forward(q, k0, v0, key_lengths=n, stats=stats0)
+    assert torch.equal(out, out0) and torch.equal(stats, stats0)
+    r = fb.attention_backward(g, q, k, v, out, stats, key_lengths=n)
+    r0 = fb.attention_backward(g, q, k0, v0, out, stats, key_lengths=n)
+    assert all(torch.equal(r[c], r0[c]) for c in "qkv")
+    check_all(q, k0, v0, g, key_lengths=n)
+
+
+@pytest.mark.parametrize("where", ["q", "k", "v"])
+def test_nan_stays_in_its_row_or_column(where):
+    """What is no number reaches the rows that read it, and no others."""
+    (q, k, v, g), _ = make(2, 70, 300, 4, 2, 64, BF16)
+    (q if where == "q" else k if where == "k" else v)[1, 5, 0 if where != "q" else 3, 7] = math.nan
+    out, _, _ = run_forward(q, k, v)
+    bad = torch.isnan(out)
+    if where == "q":
+        assert bad[1, 5, 3].all() and bad.sum() == 64
+    elif where == "k":
+        assert bad[1, :, :2].all() and bad.sum() == 70 * 2 * 64
+    else:
+        assert bad[1, :, :2, 7].all() and bad.sum() == 70 * 2

@@ -253,3 +253,38 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
             call()
     with pytest.raises(TypeError):
         layer._generator(1.5, 0)
+
+
+@pytest.mark.parametrize("kw", [dict(q_row=(1 << 20) + 1), dict(q_head=(1 << 20) + 1), dict(o_row=(1 << 20) + 1),
+                                dict(o_head=(1 << 20) + 1), dict(H=1024, Hk=1, q_head=1 << 19),
+                                dict(H=1024, Hk=1, o_head=1 << 19)])
+def test_attention_rows_that_lie_too_far_apart(kw):
+    """A tile's rows lie within 32 bits of its first one."""
+    assert attention(attention_args(**kw)) == S["ERR_UNSUPPORTED"]
+    assert attention_backward(attention_args(**kw)) == S["ERR_UNSUPPORTED"]
+
+
+def workspace_of(**kw):
+    n = fb.layer.ctypes.c_uint64()
+    assert fb._packed_call("flashlayer_attention_workspace_size", "PP")(attention_args(**kw), fb.layer.ctypes.byref(n)) == 0
+    return n.value
+
+
+def test_attention_workspace_by_mask():
+    """Copies of the keys where a boolean mask is the same for all rows, or rows end inside a granule;
+    what a mask says for each row needs none."""
+    big = dict(B=1, Lq=4096, Lk=4096, H=32, Hk=32)
+    assert workspace_of(**big) == workspace_of(**big, mask=2, mask_row=4096) == workspace_of(**big, mask=1, mask_row=4096) == 0
+    keys = workspace_of(**big, mask=1)
+    assert keys >= 2 * 32 * 4096 * 32 * 2
+    assert workspace_of(**big, mask=1, mask_head=4096) >= keys          # (a head's own rows are its own keys)
+    assert workspace_of(**{**big, "Hk": 16}, mask=1, mask_head=4096) == 0   # (heads that share keys differ)
+    assert workspace_of(**big, D=31) >= 2 * 32 * 4096 * 32 * 2
+    # a workspace that is too small, and none
+    args = attention_args(B=1, Lq=40, Lk=4096, H=1, Hk=1)
+    need = workspace_of(B=1, Lq=40, Lk=4096, H=1, Hk=1)
+    assert need > 0
+    far = [BASE + i * (MB << 4) for i in range(5)]
+    call = lambda ws, wsb: attention(args, far[0], far[1], far[2], out=far[3], ws=ws, wsb=wsb)
+    assert call(far[4], need - 1) == S["ERR_SCRATCH"] and call(0, need) == S["ERR_NULLPTR"]
+    assert call(far[3], need) != 0   # (on the output)
