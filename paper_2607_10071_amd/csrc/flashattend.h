@@ -890,6 +890,30 @@ inline int check_overlaps(std::initializer_list<Bytes> outs, std::initializer_li
     return FLASHBEV_OK;
 }
 
+// Into how many parts a long axis of `steps` tiles is split, for `base` workgroups without
+// that and per_cu that run on a CU at once: the number that takes the fewest steps one after
+// another.  A workgroup's start and end count as 1 1/2 steps, the joining launch as one and an eighth
+// more for each part.  (Gradients of 3 x 777 queries of 2 heads' shares of 3 by 1333 keys x 72 half with
+// a bias, 66 workgroups of grad_k and grad_v, one to a CU: 195, 106, 78 us in 1, 2, 3 parts, 116
+// in 4, whose last workgroups take a round of their own, 89 in 6 and 107 in 12.)
+inline int splits_of(int64_t base, int64_t steps, int per_cu)
+{
+    const int64_t slots = (int64_t)kCusOfCard / 8 * per_cu;   // of an XCD
+    if (base <= 0 || base >= 8 * slots || steps <= 1) return 1;
+    uint32_t best = 1, least = ~0u;
+    const uint32_t most = (uint32_t)std::min<int64_t>(steps, 3 * kCusOfCard), n = (uint32_t)steps;
+    for (uint32_t s = 1; s <= most; s += 1 + s / 16) {
+        const uint32_t rounds = ((uint32_t)((base * s + 7) / 8) + (uint32_t)slots - 1) / (uint32_t)slots;
+        const uint32_t cost = rounds * (2 * ((n + s - 1) / s) + 3) + (s > 1 ? 2 + s / 4 : 0);
+        if (cost < least) {
+            least = cost;
+            best = s;
+        }
+        if (rounds > 4) break;
+    }
+    return (int)best;
+}
+
 inline int check_scratch(const void *ws, uint64_t bytes, uint64_t need)
 {
     if (!need) return FLASHBEV_OK;

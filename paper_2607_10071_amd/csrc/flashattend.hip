@@ -589,9 +589,9 @@ struct Plan {
     bool copies;   // k and v are copied first
 };
 
-// A call's shape.  Up to 32 rows: the wavefronts of a workgroup go over the keys in turn.  Where
-// that leaves fewer than two workgroups a CU the keys are split, for about three of them, at two tiles
-// each or more (at one where all tiles together are not more than two a CU).
+// A call's shape.  Up to 32 rows: the wavefronts of a workgroup go over the keys in turn, and
+// where that leaves fewer than two workgroups a CU the keys are split, for about three of them, at two
+// tiles each or more (at one where all tiles together are not more than two a CU).
 Plan plan_of(const flashlayer_attention *a)
 {
     Plan p{};
@@ -602,11 +602,13 @@ Plan plan_of(const flashlayer_attention *a)
     p.wq = rows <= 32 ? 1 : flows ? 4 : 5;
     p.copies = p.wq == 4 && copies_keys(a);
     p.any = p.wq == 1 ? any_of(a) : p.wq == 5;
-    const int bq = p.wq == 1 ? 32 : 128, bk = p.wq == 1 ? 128 : 64;
+    const int bq = p.wq == 1 ? 32 : 128, bk = p.wq == 1 ? 128 : 64, bytes = p.dp * elem_size(a->dtype);
     p.tiles = (int)((rows + bq - 1) / bq);
     const int64_t base = problems * p.tiles, keys = (a->Lk + bk - 1) / bk;
     p.splits = 1;
-    if (base > 0 && base < 2 * kCusOfCard) {
+    if (p.wq != 1) {
+        p.splits = splits_of(base, keys, p.wq == 4 ? flow_waves(a->dtype, p.dp) : bytes < 384 ? 2 : 1);
+    } else if (base > 0 && base < 2 * kCusOfCard) {
         const int64_t want = (3 * kCusOfCard + base - 1) / base;
         p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(want, base * keys <= 2 * kCusOfCard ? keys : keys / 2));
     }

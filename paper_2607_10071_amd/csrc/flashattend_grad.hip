@@ -162,8 +162,13 @@ struct ShapeQ {
     static constexpr int STAGE = 2 * P::BYTES, LDS = 2 * STAGE;
 };
 
+// Workgroups that are to run on a CU at once of the kernels with masks.  (Two of heads of 96 half
+// channels, of which the compiler spills some registers, hide what one waits for: the gradients at
+// splits_of grad_q 50 -> 38 us, grad_k and grad_v 78 -> 61.)
+constexpr int masked_waves(int bytes) { return bytes > 192 ? 1 : 2; }
+
 template <int DT, int DP, bool MASK>
-__global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_grad_q(Backward p)
+__global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_grad_q(Backward p)
 {
     using S = ShapeQ<DT, DP>;
     using P = typename S::P;
@@ -358,7 +363,7 @@ struct ShapeK {
 };
 
 template <int DT, int DP, bool MASK>
-__global__ void __launch_bounds__(256, DP * elem_size(DT) > 128 ? 1 : 2) attend_grad_kv(Backward p)
+__global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_grad_kv(Backward p)
 {
     using S = ShapeK<DT, DP>;
     using P = typename S::P;
@@ -534,13 +539,11 @@ struct FlowQ {
     static constexpr int LDS = 5 * T::BYTES;   // V of two tiles and K of three
 };
 
-constexpr int grad_q_waves(int dt, int dp)
-{
-    return dp * elem_size(dt) <= 64 ? 3 : dp * elem_size(dt) <= 256 ? 2 : 1;
-}
+// Wavefronts a SIMD, of heads of `bytes`.
+constexpr int grad_q_waves(int bytes) { return bytes <= 64 ? 3 : bytes <= 256 ? 2 : 1; }
 
 template <int DT, int DP, bool KEYS>
-__global__ void __launch_bounds__(256, grad_q_waves(DT, DP)) attend_grad_q_flow(Backward p)
+__global__ void __launch_bounds__(256, grad_q_waves(DP * elem_size(DT))) attend_grad_q_flow(Backward p)
 {
     using F = FlowQ<DT, DP>;
     using T = typename F::T;
@@ -730,13 +733,10 @@ struct FlowK {
     static constexpr bool FITS = ROOM && DP * elem_size(DT) > 64;
 };
 
-constexpr int grad_kv_waves(int dt, int dp)
-{
-    return dp * elem_size(dt) <= 128 ? 2 : 1;
-}
+constexpr int grad_kv_waves(int bytes) { return bytes <= 128 ? 2 : 1; }
 
 template <int DT, int DP>
-__global__ void __launch_bounds__(256, grad_kv_waves(DT, DP)) attend_grad_kv_flow(Backward p)
+__global__ void __launch_bounds__(256, grad_kv_waves(DP * elem_size(DT))) attend_grad_kv_flow(Backward p)
 {
     using F = FlowK<DT, DP>;
     using T = typename F::T;
@@ -974,17 +974,6 @@ struct Plan {
     int k_tiles, k_splits;
 };
 
-// Splits where there are fewer than `enough` workgroups, for about `wanted`.
-int splits_of(int64_t base, int64_t steps, int64_t enough, int64_t wanted)
-{
-    if (base <= 0 || base >= enough) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>((wanted + base - 1) / base, steps / 2));
-}
-
-// grad_q is split over the keys as the forward is.  grad_k and grad_v, whose parts are two tensors
-// and whose wide heads fill a CU with one workgroup, are split over the rows below one a CU alone
-// (2 x 4 x 32 tiles of 128 keys x 128 bf16: a training pass 619 us whole, 645 and 661 in two
-// and three parts).
 Plan plan_of(const flashlayer_attention *a)
 {
     Plan p{};
@@ -995,9 +984,11 @@ Plan plan_of(const flashlayer_attention *a)
     p.padded = (int)((rows + 127) / 128 * 128);
     p.row_tiles = p.padded / kRowTile;
     p.q_tiles = (int)((rows + 127) / 128);
-    p.q_splits = splits_of(problems * p.q_tiles, (a->Lk + 63) / 64, 2 * kCusOfCard, 3 * kCusOfCard);
     p.k_tiles = (a->Lk + 127) / 128;
-    p.k_splits = splits_of(problems * p.k_tiles, (rows + 63) / 64, kCusOfCard, 2 * kCusOfCard);
+    // (steps of 64 keys, and of 64 rows)
+    const int wide = p.dp * elem_size(a->dtype);
+    p.q_splits = splits_of(problems * p.q_tiles, (a->Lk + 63) / 64, p.any ? masked_waves(wide) : grad_q_waves(wide));
+    p.k_splits = splits_of(problems * p.k_tiles, (rows + 63) / 64, p.any ? masked_waves(wide) : grad_kv_waves(wide));
     return p;
 }
 
