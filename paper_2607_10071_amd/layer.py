@@ -12,7 +12,7 @@ import ctypes
 import functools
 import struct
 
-from . import (FlashBevError, _dtype_code, _on_device, _one_device, _Prepared, _packed_call,
+from . import (FlashBevError, _dtype_code, _on_device, _on_stream, _one_device, _Prepared, _packed_call,
                _stream_handle, _workspace)
 from .block import (_act_code, _addr, _as_rows, _near, _no_copies, _restored, _rows, _same, _size, _vector,
                     _wanted, LD_MAX)
@@ -67,7 +67,21 @@ def _heads(t, name: str, shape):
     s = t.stride()
     if s[3] != 1 and shape[3] > 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
-    return s[0], s[1], s[2]
+    return s[0], s[1] if shape[1] > 1 else 0, s[2] if shape[2] > 1 else 0   # (no step along one element)
+
+
+def _near_heads(t, strides, share: int, dev, s: int, again: bool = False):
+    """(t, its strides), or a copy, made on the stream ``s`` of the call that reads it, where
+    the library does not take rows so far apart.  share: of the query heads that one head of
+    the states serves (queries and their gradients), or 0 (states, whose heads may be anywhere)."""
+    _, row, head = strides
+    if row <= LD_MAX and (share == 0 or (head <= LD_MAX and share * head <= 1 << 28)):
+        return t, strides
+    if again:
+        raise ValueError(f"a prepared call takes rows and heads at most {LD_MAX} elements apart")
+    with _on_stream(dev, s):
+        t = t.contiguous()
+    return t, _heads(t, "the copy", t.shape)
 
 
 def _sizes(q, k, v):
@@ -145,7 +159,8 @@ def attention_forward(q, k, v, mask=None, key_lengths=None, scale=None, out=None
 
     q            CUDA tensor [B, Lq, H, D] (float32, float16 or bfloat16), D at most 128,
                  its channels contiguous, any other strides: a product's [B, Lq, H D] rows
-                 seen as heads, say.
+                 seen as heads, say.  Where rows, or the heads of q, lie more than 2^20 elements
+                 apart a copy is read (prepared calls and outputs are refused).
     k, v         [B, Lk, Hk, D] in q's dtype, strides likewise (the halves of one projection,
                  a cache longer than what it holds); query head h reads head h // (H / Hk).
     mask         optional [B or 1, H or 1, Lq or 1, Lk], its keys contiguous: torch.bool (False
@@ -164,7 +179,7 @@ def attention_forward(q, k, v, mask=None, key_lengths=None, scale=None, out=None
     Scores, softmax and sums are float32; p is rounded to q's dtype for its product with v.  A
     query that sees no key gets zeros.  Returns ``out``; asynchronous.
     """
-    call, args, keep, out, dev = _attention_call(q, k, v, mask, key_lengths, scale, out, rest, stats, stream)
+    call, args, keep, out, dev = _attention_call(q, k, v, mask, key_lengths, scale, out, rest, stats, stream, False)
     with _on_device(dev):
         rc = call(*args)
     if rc != 0:
@@ -179,11 +194,11 @@ def prepare_attention_forward(q, k, v, mask=None, key_lengths=None, scale=None, 
     allocated once, here."""
     if out is None:
         raise ValueError("a prepared call needs out")
-    call, args, keep, _, dev = _attention_call(q, k, v, mask, key_lengths, scale, out, None, stats, stream)
+    call, args, keep, _, dev = _attention_call(q, k, v, mask, key_lengths, scale, out, None, stats, stream, True)
     return _Prepared(call, args, keep, "flashlayer_attention_forward", dev)
 
 
-def _attention_call(q, k, v, mask, key_lengths, scale, out, rest, stats, stream):
+def _attention_call(q, k, v, mask, key_lengths, scale, out, rest, stats, stream, again):
     """(C call, its arguments, the tensors they point into, out, device)."""
     import torch
 
@@ -206,6 +221,8 @@ def _attention_call(q, k, v, mask, key_lengths, scale, out, rest, stats, stream)
             raise ValueError(f"{name} must be contiguous")
     dev = _one_device(q, k, v, mask, key_lengths, out, rest, stats)
     s = _stream_handle(stream, dev)
+    (q, qs), (k, ks), (v, vs) = (_near_heads(t, st, share, dev, s, again) for t, st, share in
+                                 ((q, qs, H // Hk if Hk else 1), (k, ks, 0), (v, vs, 0)))
     args = _PACK_ATTENTION.pack(*qs, *ks, *vs, *os, mb, mh, mr, *sizes, code, kind, _scale(scale, D))
     need = _attention_need(*sizes, code, kind, mh != 0, mr != 0)
     ws = _workspace(need, dev, s) if need else None
@@ -259,6 +276,9 @@ def _attention_gradients(grad_out, q, k, v, out, rest, stats, mask, key_lengths,
     lengths = _lengths(key_lengths, B)
     dev = _one_device(grad_out, q, k, v, out, rest, stats, mask, key_lengths)
     s = _stream_handle(stream, dev)
+    share = H // Hk if Hk else 1
+    (q, qs), (grad_out, gs), (k, ks), (v, vs) = (_near_heads(t, st, n, dev, s) for t, st, n in
+                                                 ((q, qs, share), (grad_out, gs, share), (k, ks, 0), (v, vs, 0)))
     gq = torch.empty(q.shape, dtype=q.dtype, device=dev) if want_q else None
     gk, gv = ((torch.empty(k.shape, dtype=q.dtype, device=dev) for _ in "kv") if want_kv else (None, None))
     args = _PACK_ATTENTION.pack(*qs, *ks, *vs, *gs, mb, mh, mr, *sizes, code, kind, _scale(scale, D))

@@ -322,3 +322,42 @@ def test_nan_stays_in_its_row_or_column(where):
         assert bad[1, :, :2].all() and bad.sum() == 70 * 2 * 64
     else:
         assert bad[1, :, :2, 7].all() and bad.sum() == 70 * 2
+
+
+@pytest.mark.parametrize("what", ["rows", "heads", "share"])
+def test_far_rows_and_heads(what):
+    """Rows and query heads further apart than the library takes are read from a copy, also on another
+    stream and as gradients; outputs and prepared calls are refused.  Single rows have no step."""
+    # (the third: heads within the limit, 512 of which are not)
+    H, Hk, far = (2, 2, (1 << 20) + 8) if what != "share" else (512, 1, (1 << 20) - 8)
+    (q0, k0, v0, g0), _ = make(1, 40, 50, H, Hk, 32, BF16)
+
+    def apart(t):
+        n, h = t.shape[1], t.shape[2]
+        step, head = (far, 32) if what == "rows" else (32, far)
+        view = torch.empty((n - 1) * step + (h - 1) * head + 32, dtype=BF16, device="cuda").as_strided(
+            t.shape, (0, step, head, 1))
+        view.copy_(t)
+        return view
+
+    q, k, v, g = map(apart, (q0, k0, v0, g0))
+    stats, stats0 = (torch.empty((1, H, 40, 2), device="cuda") for _ in range(2))
+    out0 = fb.attention_forward(q0, k0, v0, stats=stats0)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    out = fb.attention_forward(q, k, v, stats=stats, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(out, out0) and torch.equal(stats, stats0)
+    r, r0 = (fb.attention_backward(*a, out, stats) for a in ((g, q, k, v), (g0, q0, k0, v0)))
+    assert all(torch.equal(r[n], r0[n]) for n in "qkv")
+    with pytest.raises(ValueError, match="prepared call"):
+        fb.prepare_attention_forward(q, k, v, out=out)
+    with pytest.raises(fb.FlashBevError):
+        fb.attention_forward(q0, k0, v0, out=q)
+    leaves = [t.requires_grad_() for t in (q, k, v)]
+    got = torch.autograd.grad(fb.attention_autograd(*leaves), leaves, g)
+    want = torch.autograd.grad(fb.attention_autograd(*[t.requires_grad_() for t in (q0, k0, v0)]), [q0, k0, v0], g0)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    # one row of a tensor whose rows are far apart is not far from anything
+    one = q.detach()[:, :1]
+    assert torch.equal(fb.attention_forward(one, k0, v0), fb.attention_forward(q0[:, :1].contiguous(), k0, v0))
