@@ -322,8 +322,8 @@ __global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) at
 // and vector instructions that do not wait for each other, in turn.  (Scores, then weights, then
 // the product: 2048 queries of 32 heads x 4096 keys x 128 bf16 165 us.)
 //
-// Heads of 32 are bound by vector instructions, 16 exponentials and some 60 others a step beside
-// 4 products of 32 clocks each: 40000 queries x 8700 keys of 8 heads, bf16, 519 us, the vector units
+// Heads of 32 are bound by vector instructions, 16 exponentials of 8 clocks and some 40 others of 4 a
+// step beside 4 products of 32 each: 40000 queries x 8700 keys of 8 heads, bf16, 519 us, the vector units
 // busy 83% of the time, the matrix units 32%. Wide heads by both and what they wait for each
 // other: the case above 150 us, 49% each, 920 TFLOP/s.
 //

@@ -149,3 +149,20 @@ def test_captured_graph_drops_anew():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, fb.dropout_forward(x, 0.5, 5, step)), step
+
+
+@pytest.mark.parametrize("residual", [False, True])
+def test_prepared(residual):
+    """The same call again, of what its tensors then hold; with a device tensor as the seed too."""
+    x, r = torch.randn(33, 70, device="cuda"), torch.randn(33, 70, device="cuda") if residual else None
+    state = torch.tensor([5, 6], device="cuda")
+    out = torch.empty_like(x)
+    calls = [(fb.prepare_dropout_forward(x, 0.4, 5, 6, residual=r, scale=0.5, out=out), (5, 6)),
+             (fb.prepare_dropout_forward(x, 0.4, state, residual=r, scale=0.5, out=out), None)]
+    for step in range(3):
+        x.copy_(torch.randn_like(x))
+        state.copy_(torch.tensor([step, 9]))
+        for call, seed in calls:
+            out.fill_(7)
+            call()
+            assert torch.equal(out, fb.dropout_forward(x, 0.4, *(seed or (step, 9)), residual=r, scale=0.5))

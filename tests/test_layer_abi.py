@@ -288,3 +288,21 @@ def test_attention_workspace_by_mask():
     call = lambda ws, wsb: attention(args, far[0], far[1], far[2], out=far[3], ws=ws, wsb=wsb)
     assert call(far[4], need - 1) == S["ERR_SCRATCH"] and call(0, need) == S["ERR_NULLPTR"]
     assert call(far[3], need) != 0   # (on the output)
+
+
+def test_a_thread_sees_all_autograd_classes_or_none(monkeypatch):
+    """The classes are made on first use, and several threads may be the first."""
+    seen = []
+
+    class Watched(dict):
+        def update(self, other):
+            super().update(other)
+            seen.append(set(self))
+
+        def __setitem__(self, k, v):
+            super().__setitem__(k, v)
+            seen.append(set(self))
+
+    monkeypatch.setattr(layer, "_AUTOGRAD", Watched())
+    names = {"attention", "group_norm", "dropout"}
+    assert set(layer._autograd_functions()) == names and seen == [names]
