@@ -111,7 +111,7 @@ int flashlayer_attention_workspace_size(const flashlayer_attention *args, uint64
  *   stats        the forward's.
  *   grad_q       [B, Lq, H, D] contiguous, or NULL to skip it.
  *   grad_k, grad_v  [B, Lk, Hk, D] contiguous; both or neither.  Rows of keys that are left
- *                out are zeros.
+ *                out are zeros, and so are all where there are no queries (no mask is read then).
  *   workspace    flashlayer_attention_backward_workspace_size bytes.
  */
 int flashlayer_attention_backward(const flashlayer_attention *args, const void *grad_out,

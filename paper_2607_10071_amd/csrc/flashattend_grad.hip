@@ -1021,7 +1021,7 @@ uint64_t largest_bytes(const flashlayer_attention *a, const Plan &p)
 
 uint64_t backward_bytes(const flashlayer_attention *a, bool want_q, bool want_kv)
 {
-    if (!a->B || !a->H || !a->D) return 0;
+    if (!a->B || !a->Lq || !a->H || !a->D) return 0;
     const Plan p = plan_of(a);
     uint64_t q = 0, kv = 0;   // one after the other in one place
     if (want_q && p.q_splits > 1)
@@ -1035,7 +1035,7 @@ template <int DT, int DP>
 int run(Backward &p, const Plan &plan, hipStream_t st)
 {
     const uint64_t problems = (uint64_t)p.B * p.Hk;
-    if (p.gq && p.rows) {
+    if (p.gq) {
         p.tiles = plan.q_tiles;
         p.splits = plan.q_splits;
         if (const int rc = deal(p, size_prod({problems, (uint64_t)p.tiles, (uint64_t)p.splits}))) return rc;
@@ -1081,6 +1081,18 @@ int run(Backward &p, const Plan &plan, hipStream_t st)
     return FLASHBEV_OK;
 }
 
+// grad_k and grad_v of no rows: zeros (a sum of no parts).
+template <int DT>
+int no_rows(const Backward &p, hipStream_t st)
+{
+    for (char *out : {p.gk, p.gv}) {
+        Sum s{nullptr, out, (int64_t)p.B * p.Hk * p.Lk, 0, p.D};
+        const uint64_t lanes = (uint64_t)s.n * (FLASHLAYER_HEAD_MAX / 4);
+        if (const int rc = launch_rows((const void *)attend_sum<DT, FLASHLAYER_HEAD_MAX>, (lanes + 255) / 256, 256, s, st)) return rc;
+    }
+    return FLASHBEV_OK;
+}
+
 template <int DT>
 int run_width(const flashlayer_attention *a, Backward &p, const Plan &plan, void *workspace, hipStream_t st)
 {
@@ -1096,9 +1108,10 @@ int run_width(const flashlayer_attention *a, Backward &p, const Plan &plan, void
     p.rg_h = p.oh;
     p.rshare = p.share;
     p.Dr = p.D;
+    if (!p.rows) return no_rows<DT>(p, st);   // (and no mask: one of no rows has no address)
     if (plan.copies && a->Lk) {
         if (const int rc = copy_keys<DT>(a, p, static_cast<char *>(workspace), st)) return rc;
-        if (odd_of(a) && p.gk && p.rows) {
+        if (odd_of(a) && p.gk) {
             Copy c{};
             const uint64_t each = rows_copy_bytes(a, p.rows, a->Hk);
             c.from[0] = p.q;

@@ -361,3 +361,22 @@ def test_far_rows_and_heads(what):
     # one row of a tensor whose rows are far apart is not far from anything
     one = q.detach()[:, :1]
     assert torch.equal(fb.attention_forward(one, k0, v0), fb.attention_forward(q0[:, :1].contiguous(), k0, v0))
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("D", [32, 31, 128])
+def test_gradients_without_queries(D, dtype):
+    """Zeros for k and v, whatever the mask of no queries."""
+    q = torch.ones((2, 0, 4, D), device="cuda", dtype=dtype)
+    k = torch.ones((2, 150, 2, D), device="cuda", dtype=dtype)
+    for mask in (None, torch.ones((2, 1, 0, 150), device="cuda", dtype=torch.bool),
+                 torch.ones((1, 4, 0, 150), device="cuda", dtype=torch.bool),
+                 torch.ones((2, 1, 1, 150), device="cuda", dtype=torch.bool),
+                 torch.ones((2, 4, 0, 150), device="cuda")):
+        leaves = [t.clone().requires_grad_() for t in (q, k, k)]
+        out = fb.attention_autograd(*leaves, mask=mask)
+        del_me = [torch.full_like(k, math.nan) for _ in range(4)]   # (what the gradients' memory may hold)
+        del del_me
+        got = torch.autograd.grad(out, leaves, torch.empty_like(q))
+        assert out.shape == q.shape and got[0].shape == q.shape
+        assert got[1].shape == got[2].shape == k.shape and (got[1] == 0).all() and (got[2] == 0).all()

@@ -306,3 +306,19 @@ def test_a_thread_sees_all_autograd_classes_or_none(monkeypatch):
     monkeypatch.setattr(layer, "_AUTOGRAD", Watched())
     names = {"attention", "group_norm", "dropout"}
     assert set(layer._autograd_functions()) == names and seen == [names]
+
+
+def backward_workspace_of(want_q=1, want_kv=1, **kw):
+    n = fb.layer.ctypes.c_uint64()
+    size = fb._packed_call("flashlayer_attention_backward_workspace_size", "PiiP")
+    assert size(attention_args(**kw), want_q, want_kv, fb.layer.ctypes.byref(n)) == 0
+    return n.value
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(mask=1), dict(mask=1, mask_row=16), dict(mask=3), dict(D=31), dict(D=31, mask=1),
+                                dict(D=128, dtype=0, mask=1)])
+def test_a_backward_without_queries_reads_nothing(kw):
+    """There is no mask to read then (that of no queries has no address), and nothing to copy: grad_k and
+    grad_v are zeros."""
+    assert backward_workspace_of(Lq=0, **kw) == 0
+    assert backward_workspace_of(Lq=1, **kw) > 0
