@@ -756,8 +756,9 @@ uint64_t partial_bytes(const flashlayer_group_norm *a, const Cut &c, bool backwa
 
 uint64_t forward_bytes(const flashlayer_group_norm *a)
 {
+    if (!a->N || !a->R || !a->C) return 0;   // (there is nothing to cut)
     const Cut c = cut(a, false);
-    if (c.whole || !a->N || !a->R || !a->C) return 0;
+    if (c.whole) return 0;
     return partial_bytes(a, c, false) + round256((uint64_t)a->N * a->groups * 8);
 }
 
@@ -890,8 +891,9 @@ extern "C" int flashlayer_group_norm_backward(const flashlayer_group_norm *args,
     const int dt = args->dtype, act = args->act, es = elem_size(dt), ps = elem_size(args->param_dtype);
     const int64_t M = args->N * args->R;
     const uint64_t need = backward_bytes(args), vec = (uint64_t)args->C * ps;
-    if (!grad_x && !grad_weight && !grad_bias) return FLASHBEV_ERR_NULLPTR;
     if (!args->C) return FLASHBEV_OK;
+    // (a gradient without elements may be null)
+    if (!grad_x && !grad_weight && !grad_bias) return M ? FLASHBEV_ERR_NULLPTR : FLASHBEV_OK;
     if (misaligned(grad_weight, ps) || misaligned(grad_bias, ps)) return FLASHBEV_ERR_ALIGN;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const uint64_t extra = grad_weight || grad_bias ? ((uint64_t)args->C + 255) / 256 : 0;

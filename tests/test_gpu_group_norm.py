@@ -205,3 +205,19 @@ def test_same_bits_again_and_on_another_stream():
     call()
     call()
     assert torch.equal(out, first)
+
+
+@pytest.mark.parametrize("groups", [1, 3])
+def test_no_channels(groups):
+    x = torch.zeros((2, 100, 0), device="cuda", requires_grad=True)
+    out = torch.full_like(x, 3.0)
+    assert fb.group_norm_forward(x.detach(), groups).shape == x.shape
+    fb.prepare_group_norm_forward(x.detach(), groups, out=out.detach())()
+    w = torch.zeros(0, device="cuda", requires_grad=True)
+    y = fb.group_norm_autograd(x, groups, w, w, "silu")
+    got = torch.autograd.grad(y, [x, w], torch.zeros_like(x))
+    assert y.shape == x.shape and got[0].shape == x.shape and got[1].shape == w.shape
+    for shape in ((0, 5, 8), (2, 0, 8), (2, 5, 0)):   # the gradient of x alone
+        x = torch.zeros(shape, device="cuda", requires_grad=True)
+        (gx,) = torch.autograd.grad(fb.group_norm_autograd(x, 1), [x], torch.zeros_like(x))
+        assert gx.shape == shape

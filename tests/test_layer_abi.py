@@ -322,3 +322,13 @@ def test_a_backward_without_queries_reads_nothing(kw):
     grad_v are zeros."""
     assert backward_workspace_of(Lq=0, **kw) == 0
     assert backward_workspace_of(Lq=1, **kw) > 0
+
+
+@pytest.mark.parametrize("kw", [dict(C=0, groups=1), dict(C=0, groups=3), dict(N=0), dict(R=0), dict(C=0, groups=1, R=5000)])
+def test_group_norm_without_elements(kw):
+    n = fb.layer.ctypes.c_uint64()
+    for size in ("flashlayer_group_norm_workspace_size", "flashlayer_group_norm_backward_workspace_size"):
+        n.value = 7
+        assert fb._packed_call(size, "PP")(group_args(**kw), fb.layer.ctypes.byref(n)) == 0 and n.value == 0
+    assert group_norm(group_args(**kw), x=0, y=0, ws=0) == 0
+    assert group_norm_backward(group_args(**kw), g=0, x=0, stats=0, gx=0, gw=0, gb=0, ws=0) == 0
