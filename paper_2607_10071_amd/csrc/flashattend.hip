@@ -598,7 +598,8 @@ __global__ void __launch_bounds__(256) attend_join(Forward p)
 // host
 // ---------------------------------------------------------------------------
 struct Plan {
-    int wq, tiles, splits, dp;   // wq 4: attend_flow; 5: attend with four wavefronts' rows; 1: with one's
+    // wq 4: attend_flow, where k and v allow loads to LDS; 5: attend with four wavefronts' rows; 1: with one's
+    int wq, tiles, splits, dp;
     bool any;
     bool copies;   // k and v are copied first
 };
@@ -649,13 +650,14 @@ int run(Forward &p, const Plan &plan, hipStream_t st)
 {
     const void *fn = nullptr;
     size_t lds = 0;
-    if (plan.wq == 4) {
+    if (plan.wq == 4 && keys_to_lds(p)) {
         fn = p.words ? (const void *)attend_flow<DT, DP, true> : (const void *)attend_flow<DT, DP, false>;
         lds = Flow<DT, DP>::LDS;
-    } else if (plan.wq == 5) {
+    } else if (plan.wq != 1) {
         fn = (const void *)attend<DT, DP, 4, true>;
         lds = Shape<DT, DP, 4>::LDS;
-    } else if (plan.wq == 1) {
+        p.any = true;
+    } else {
         fn = plan.any ? (const void *)attend<DT, DP, 1, true> : (const void *)attend<DT, DP, 1, false>;
         lds = Shape<DT, DP, 1>::LDS;
     }

@@ -1031,6 +1031,12 @@ uint64_t backward_bytes(const flashlayer_attention *a, bool want_q, bool want_kv
     return copy_bytes(a, p) + data_bytes(a) + 2 * rows_bytes(a, p) + largest_bytes(a, p) + align256(std::max(q, kv));
 }
 
+bool rows_to_lds(const Backward &p)
+{
+    return to_lds_reads(p.rq, {{p.B, p.rq_b}, {p.Hk, p.rq_g}, {p.Lq, p.rq_r}, {p.rshare, p.rq_h}}) &&
+           to_lds_reads(p.rg, {{p.B, p.rg_b}, {p.Hk, p.rg_g}, {p.Lq, p.rg_r}, {p.rshare, p.rg_h}});
+}
+
 template <int DT, int DP>
 int run(Backward &p, const Plan &plan, hipStream_t st)
 {
@@ -1042,7 +1048,7 @@ int run(Backward &p, const Plan &plan, hipStream_t st)
         const void *fn = (const void *)attend_grad_q<DT, DP, true>;
         size_t lds = ShapeQ<DT, DP>::LDS;
         if constexpr (FlowK<DT, DP>::ROOM) {
-            if (!plan.any) {
+            if (!plan.any && keys_to_lds(p)) {
                 fn = p.words ? (const void *)attend_grad_q_flow<DT, DP, true>
                              : (const void *)attend_grad_q_flow<DT, DP, false>;
                 lds = FlowQ<DT, DP>::LDS;
@@ -1065,7 +1071,7 @@ int run(Backward &p, const Plan &plan, hipStream_t st)
         if (!plan.any) fn = (const void *)attend_grad_kv<DT, DP, false>;
     }
     if constexpr (FlowK<DT, DP>::FITS) {
-        if (!plan.any) {
+        if (!plan.any && rows_to_lds(p)) {
             fn = (const void *)attend_grad_kv_flow<DT, DP>;
             lds = FlowK<DT, DP>::LDS;
         }

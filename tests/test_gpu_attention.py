@@ -380,3 +380,38 @@ def test_gradients_without_queries(D, dtype):
         got = torch.autograd.grad(out, leaves, torch.empty_like(q))
         assert out.shape == q.shape and got[0].shape == q.shape
         assert got[1].shape == got[2].shape == k.shape and (got[1] == 0).all() and (got[2] == 0).all()
+
+
+def off_16_bytes(t, how):
+    """t's values at addresses that are not multiples of 16 bytes: all of them, those of odd rows, of odd
+    heads, or of odd batches."""
+    B, L, H, D = t.shape
+    head = D + (how == "heads")
+    row = H * head + (how == "rows")
+    batch = L * row + (how == "batches")
+    flat = torch.zeros(B * batch + 1, dtype=t.dtype, device="cuda")
+    view = flat.as_strided(t.shape, (batch, row, head, 1), 1 if how == "all" else 0)
+    view.copy_(t)
+    assert view.data_ptr() % 16 or any(s * t.element_size() % 16 for s in view.stride()[:3])
+    return view
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 70, 333, 4, 2, 32), (2, 130, 200, 2, 2, 64), (2, 60, 150, 4, 2, 128),
+                                   (2, 5, 300, 2, 2, 64), (2, 45, 2100, 2, 1, 96)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("how", ["all", "rows", "heads", "batches"])
+@pytest.mark.parametrize("which", ["q", "k", "v", "g", "qkvg"])
+def test_rows_off_16_bytes(which, how, shape, dtype):
+    """Elements of any alignment where loads to LDS take 16 bytes at multiples of them, with and without
+    keys that a mask leaves out."""
+    ts, gen = make(*shape, dtype, seed=8)
+    moved = [off_16_bytes(t, how) if n in which else t for n, t in zip("qkvg", ts)]
+    for mask in (None, torch.rand((2, 1, 1, shape[2]), generator=gen, device="cuda") < 0.7):
+        check_all(*moved, mask=mask)
+    (q, k, v, g), lengths = moved, torch.tensor([shape[2], shape[2] // 3], dtype=torch.int32, device="cuda")
+    check_all(q, k, v, g, key_lengths=lengths)
+    leaves = [t.detach().requires_grad_() for t in (q, k, v)]
+    got = torch.autograd.grad(fb.attention_autograd(*leaves), leaves, g)
+    want, tol = ref.attention(*ts[:3], None, None, None, g)
+    for n, t in zip("qkv", got):
+        ref.check(t, want["grad_" + n], tol["grad_" + n], "grad_" + n)
