@@ -30,8 +30,17 @@ struct RowData {
     float m;       // its scores' reference; 0 for an empty row
     float log2l;   // of the sum of exp(s - m); infinite for an empty row, whose weights are then 0
     float delta;   // g . out
-    float norm;    // |g|
+    float norm;    // float16: |g|
 };
+
+// What a row's dS is multiplied by for grad_q's product.  float16 alone needs it: bfloat16 and float32
+// hold what |g| makes of dS, and |g| itself would be squared beyond float32's range.
+template <int DT>
+__device__ __forceinline__ float row_factor(const RowData &row)
+{
+    if constexpr (DT == FLASHBEV_F16) return row.norm > 0.0f ? 0.125f / row.norm : 1.0f;
+    return 1.0f;
+}
 
 // an exponent whose power is a normal float32
 __device__ __forceinline__ float within_range(float e)
@@ -43,7 +52,7 @@ struct Backward : Attend {
     const char *out, *rest;   // [B, Lq, H, D]; rest null: none
     const float *stats;
     RowData *data;            // [B Hk][rows]
-    float *largest;           // [B Hk][padded / 16][2]: the largest 1 / l and |g| / l of 16 rows
+    float *largest;           // float16: [B Hk][padded / 16][2], the largest 1 / l and |g| / l of 16 rows
     // [B Hk][padded rows] each, for grad_k's and grad_v's kernel without masks: the exponent that a
     // row's weights lose, m log2(e) + log2(l), infinite past the last row; and delta
     float *lose, *delta;
@@ -71,7 +80,7 @@ struct Backward : Attend {
 
 constexpr int kRowTile = 16;
 
-// delta and |g| of a tile of 16 rows, 16 lanes to a row.
+// delta and (float16) |g| of a tile of 16 rows, 16 lanes to a row.
 template <int DT>
 __global__ void __launch_bounds__(256) attend_rows(Backward p)
 {
@@ -103,7 +112,7 @@ __global__ void __launch_bounds__(256) attend_rows(Backward p)
             for (int i = 0; i < E; ++i) {
                 delta = __builtin_fmaf(vg[i], vo[i], delta);
                 if (p.rest) delta = __builtin_fmaf(vg[i], vr[i], delta);
-                sq = __builtin_fmaf(vg[i], vg[i], sq);
+                if constexpr (DT == FLASHBEV_F16) sq = __builtin_fmaf(vg[i], vg[i], sq);
             }
         }
 #pragma unroll
@@ -201,7 +210,7 @@ __global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_
     const float c = (MASK ? 1.0f : p.scale) * kLog2;
     // weights are p l; an empty row's are exp(-inf - 0) = 0
     const float mc = row.m * kLog2;
-    const float inv = row.norm > 0.0f ? 0.125f / row.norm : 1.0f, off = -row.delta * inv;
+    const float inv = row_factor<DT>(row), off = -row.delta * inv;
     const char *kbase = p.k + b * p.kb + g * p.kh, *vbase = p.v + b * p.vb + g * p.vh;
     f32x16 o[DB];
 #pragma unroll
@@ -578,7 +587,7 @@ __global__ void __launch_bounds__(256, grad_q_waves(DP * elem_size(DT))) attend_
     row_fragments<DT, DP>(gf, p.g + b * p.ob + qi * p.orow + head * p.oh, row_there, p.D, lane);
     const RowData row = p.data[((int64_t)b * p.Hk + g) * p.rows + min(r, p.rows - 1)];
     const float c = p.scale * kLog2, mc = row.m * kLog2;   // weights are p l
-    const float inv = row.norm > 0.0f ? 0.125f / row.norm : 1.0f, off = -row.delta * inv;
+    const float inv = row_factor<DT>(row), off = -row.delta * inv;
 
     f32x16 o[DB];
 #pragma unroll

@@ -415,3 +415,34 @@ def test_rows_off_16_bytes(which, how, shape, dtype):
     want, tol = ref.attention(*ts[:3], None, None, None, g)
     for n, t in zip("qkv", got):
         ref.check(t, want["grad_" + n], tol["grad_" + n], "grad_" + n)
+
+
+def backward_checked(q, k, v, g, mask=None, key_lengths=None, more=None):
+    """All gradients within their bounds (``more``: what to add to them)."""
+    kw = dict(mask=mask, key_lengths=key_lengths)
+    want, tol = ref.attention(q, k, v, None, mask, key_lengths, g)
+    out, rest, stats = run_forward(q, k, v, **kw)
+    ref.check(out, want["out"], tol["out"], "out")
+    r = fb.attention_backward(g, q, k, v, out, stats, rest=rest if q.dtype != F32 else None, **kw)
+    for n in "qkv":
+        ref.check(r[n], want["grad_" + n], tol["grad_" + n] + (more or {}).get(n, 0.0), "grad_" + n)
+    return r
+
+
+def some_masks(B, H, Lq, Lk, gen):
+    def rand(*s):
+        return torch.rand(s, generator=gen, device="cuda")
+
+    return {"none": None, "keys": rand(B, 1, 1, Lk) < 0.7, "pairs": rand(B, 1, Lq, Lk) < 0.6,
+            "add": 2 * torch.randn((1, H, Lq, Lk), generator=gen, device="cuda")}
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", [1e20, 3e30, 1e-25])
+@pytest.mark.parametrize("kind", ["none", "keys", "pairs", "add"])
+@pytest.mark.parametrize("D", [32, 64, 63, 128])
+def test_gradients_whose_squares_leave_float32(D, kind, size, dtype):
+    """Rows of grad_out with norms that float32 cannot square, next to ordinary ones."""
+    (q, k, v, g), gen = make(2, 70, 150, 4, 2, D, dtype, seed=9)
+    g[:, ::2] = (g[:, ::2].float() * size).to(dtype)
+    backward_checked(q, k, v, g, some_masks(2, 4, 70, 150, gen)[kind])
