@@ -61,6 +61,7 @@ struct Backward : Attend {
     float *part;              // splits > 1: grad_q's [splits][B Hk rows][DP] or
                               // grad_k's and grad_v's [2][splits][B Hk Lk][DP]
     int row_tiles;            // of 16
+    uint32_t row_blocks;      // of all problems
     // q's and g's rows as grad_k's and grad_v's kernel without masks reads them: row r of head g of the
     // states at g `group` + (r / rshare) `row` + (r % rshare) `head`, of Dr channels
     const char *rq, *rg;
@@ -86,7 +87,9 @@ __global__ void __launch_bounds__(256) attend_rows(Backward p)
 {
     constexpr int ES = elem_size(DT), E = 16 / ES;
     __shared__ float lds[2][4];
-    const int tile = blockIdx.x % p.row_tiles, problem = blockIdx.x / p.row_tiles;
+    const uint32_t id = block_index();
+    if (id >= p.row_blocks) return;
+    const int tile = id % p.row_tiles, problem = id / p.row_tiles;
     const int b = problem / p.Hk, g = problem - b * p.Hk;
     const int part = threadIdx.x & 15;
     float most_l = 0.0f, most_g = 0.0f;
@@ -157,7 +160,7 @@ __global__ void __launch_bounds__(256) attend_rows(Backward p)
     if (threadIdx.x < 2) {
         float v = lds[threadIdx.x][0];
         for (int w = 1; w < 4; ++w) v = __builtin_fmaxf(v, lds[threadIdx.x][w]);
-        p.largest[2 * (int64_t)blockIdx.x + threadIdx.x] = v;
+        p.largest[2 * (int64_t)id + threadIdx.x] = v;
     }
 }
 
@@ -1158,7 +1161,8 @@ int run_width(const flashlayer_attention *a, Backward &p, const Plan &plan, void
         }
     }
     const uint64_t tiles = size_prod({(uint64_t)p.B, (uint64_t)p.Hk, (uint64_t)plan.row_tiles});
-    if (const int rc = launch_kernel((const void *)attend_rows<DT>, tiles, 256, p, 0, st)) return rc;
+    p.row_blocks = (uint32_t)tiles;   // (launch_rows refuses what does not fit)
+    if (const int rc = launch_rows((const void *)attend_rows<DT>, tiles, 256, p, st)) return rc;
     switch (plan.dp) {
     case 32: return run<DT, 32>(p, plan, st);
     case 64: return run<DT, 64>(p, plan, st);

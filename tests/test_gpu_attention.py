@@ -446,3 +446,19 @@ def test_gradients_whose_squares_leave_float32(D, kind, size, dtype):
     (q, k, v, g), gen = make(2, 70, 150, 4, 2, D, dtype, seed=9)
     g[:, ::2] = (g[:, ::2].float() * size).to(dtype)
     backward_checked(q, k, v, g, some_masks(2, 4, 70, 150, gen)[kind])
+
+
+def test_gradients_of_many_problems():
+    """More tiles of 16 rows than one row of the grid takes, the last ones too."""
+    B, Lq, Lk, D = (1 << 21) + 3, 1, 2, 8
+    (q, k, v, g), _ = make(B, Lq, Lk, 1, 1, D, BF16)
+    out, rest, stats = run_forward(q, k, v)
+    r = fb.attention_backward(g, q, k, v, out, stats, rest=rest)
+    for b in (0, 1 << 18, 1 << 20, (1 << 21) - 1, B - 2):
+        s = slice(b, b + 2)
+        want, tol = ref.attention(q[s], k[s], v[s], grad_out=g[s])
+        ref.check(out[s], want["out"], tol["out"], "out")
+        for n in "qkv":
+            ref.check(r[n][s], want["grad_" + n], tol["grad_" + n], "grad_" + n)
+    del out, rest, stats, r
+    torch.cuda.empty_cache()
