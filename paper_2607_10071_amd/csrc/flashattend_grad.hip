@@ -14,7 +14,8 @@
 // range; float16 loses digits below 6e-5, where weights of one in 40000 and scaled losses'
 // gradients lie, so its factors are kept near one: grad_q's kernel takes p l (at most 2^6) and
 // g / (8 |g|), a row's factors coming back at the end; the other one takes p and dS times powers of
-// two that bring the largest 1 / l and |g| / l of its rows to about one.
+// two that bring the largest 1 / l and |g| / l of its rows to about one.  Both divide by one more for each
+// power of two of |v| above 2^11 (`spread`).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -32,15 +33,6 @@ struct RowData {
     float delta;   // g . out
     float norm;    // float16: |g|
 };
-
-// What a row's dS is multiplied by for grad_q's product.  float16 alone needs it: bfloat16 and float32
-// hold what |g| makes of dS, and |g| itself would be squared beyond float32's range.
-template <int DT>
-__device__ __forceinline__ float row_factor(const RowData &row)
-{
-    if constexpr (DT == FLASHBEV_F16) return row.norm > 0.0f ? 0.125f / row.norm : 1.0f;
-    return 1.0f;
-}
 
 // an exponent whose power is a normal float32
 __device__ __forceinline__ float within_range(float e)
@@ -62,6 +54,9 @@ struct Backward : Attend {
                               // grad_k's and grad_v's [2][splits][B Hk Lk][DP]
     int row_tiles;            // of 16
     uint32_t row_blocks;      // of all problems
+    float *most_v;            // float16: [B Hk][key_tiles], the largest |v| of key_tile keys each
+    int key_tiles, key_tile;  // 0 for other types
+    uint32_t blocks_v;
     // q's and g's rows as grad_k's and grad_v's kernel without masks reads them: row r of head g of the
     // states at g `group` + (r / rshare) `row` + (r % rshare) `head`, of Dr channels
     const char *rq, *rg;
@@ -80,14 +75,92 @@ struct Backward : Attend {
 };
 
 constexpr int kRowTile = 16;
+constexpr int kMostTiles = 256;   // of largest |v|: four loads of a wavefront
 
-// delta and (float16) |g| of a tile of 16 rows, 16 lanes to a row.
+// How many powers of two float16's dS is made smaller by for large values.  Weights p l reach 2^6 (a
+// forward's reference may lag so far) and |g v^T - delta| is at most 2 |g| |v|: an eighth of one for
+// |g| keeps their product within 2^15 up to |v| = 2^11, and each power of two of the problem's largest |v|
+// above that takes another one.  (float16's largest, in 128 channels, takes 9; a |v| that is infinite
+// makes dS what it makes it.)
+__device__ __forceinline__ int spread(const Backward &p, int64_t problem, int lane)
+{
+    float most = 0.0f;
+#pragma unroll
+    for (int i = lane; i < lane + kMostTiles; i += 64)
+        if (i < p.key_tiles) most = __builtin_fmaxf(most, p.most_v[problem * p.key_tiles + i]);
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, o));
+    int e = 0;
+    while (e < 9 && most > (float)(2048 << e)) ++e;
+    return e;
+}
+
+// What a row's dS is multiplied by for grad_q's product.  float16 alone needs it: bfloat16 and float32
+// hold what |g| makes of dS, and |g| itself would be squared beyond float32's range.
+template <int DT>
+__device__ __forceinline__ float row_factor(const Backward &p, const RowData &row, int64_t problem, int lane)
+{
+    if constexpr (DT == FLASHBEV_F16) {
+        const float least = __builtin_ldexpf(0.125f, -spread(p, problem, lane));
+        return row.norm > 0.0f ? least / row.norm : 1.0f;
+    }
+    return 1.0f;
+}
+
+// The largest |v| of a tile of keys, a lane to a granule of a key and four keys of its in flight.  (Copies are
+// whole granules; masks that differ from row to row leave odd ones.)
+template <int DT>
+__device__ __forceinline__ void largest_values(const Backward &p, uint32_t id, float (&shared)[4])
+{
+    constexpr int ES = elem_size(DT), E = 16 / ES, N = 4;
+    static_assert(16 * E >= FLASHLAYER_HEAD_MAX, "at most 16 granules");
+    const int tile = id % p.key_tiles, problem = id / p.key_tiles, b = problem / p.Hk, g = problem - b * p.Hk;
+    const int width = p.Dk, lanes = width <= 4 * E ? 4 : width <= 8 * E ? 8 : 16, step = 256 / lanes;
+    const bool whole = width % E == 0;
+    const int d = (threadIdx.x & (lanes - 1)) * E, end = (int)min((int64_t)p.keys(b), (int64_t)(tile + 1) * p.key_tile);
+    const char *base = p.v + b * p.vb + g * p.vh;
+    float most = 0.0f;
+    for (int key0 = tile * p.key_tile + (int)threadIdx.x / lanes; key0 < end; key0 += step * N) {
+        u32x4 w[N][1];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const char *row = base + (key0 + step * n) * p.vr;
+            w[n][0] = u32x4{0, 0, 0, 0};
+            if (key0 + step * n < end && d < width)
+                w[n][0] = whole ? load16(row + d * ES) : load_granule_edge<DT>(row, d, width);
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            float v[E], sq = 0.0f;
+            elems_of<DT>(w[n], v);
+#pragma unroll
+            for (int i = 0; i < E; ++i) sq = __builtin_fmaf(v[i], v[i], sq);
+            for (int o = 1; o < lanes; o *= 2) sq += __shfl_xor(sq, o);
+            most = __builtin_fmaxf(most, sq);
+        }
+    }
+#pragma unroll
+    for (int o = 4; o < 64; o *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, o));
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        p.most_v[id] = sqrtf(__builtin_fmaxf(__builtin_fmaxf(shared[0], shared[1]), __builtin_fmaxf(shared[2], shared[3])));
+}
+
+// delta and (float16) |g| of a tile of 16 rows, 16 lanes to a row; and by the workgroups past the rows'
+// float16's largest |v|.
 template <int DT>
 __global__ void __launch_bounds__(256) attend_rows(Backward p)
 {
     constexpr int ES = elem_size(DT), E = 16 / ES;
     __shared__ float lds[2][4];
     const uint32_t id = block_index();
+    if constexpr (DT == FLASHBEV_F16) {
+        if (id >= p.row_blocks) {
+            if (id - p.row_blocks < p.blocks_v) largest_values<DT>(p, id - p.row_blocks, lds[0]);
+            return;
+        }
+    }
     if (id >= p.row_blocks) return;
     const int tile = id % p.row_tiles, problem = id / p.row_tiles;
     const int b = problem / p.Hk, g = problem - b * p.Hk;
@@ -213,7 +286,7 @@ __global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_
     const float c = (MASK ? 1.0f : p.scale) * kLog2;
     // weights are p l; an empty row's are exp(-inf - 0) = 0
     const float mc = row.m * kLog2;
-    const float inv = row_factor<DT>(row), off = -row.delta * inv;
+    const float inv = row_factor<DT>(p, row, (int64_t)b * p.Hk + g, lane), off = -row.delta * inv;
     const char *kbase = p.k + b * p.kb + g * p.kh, *vbase = p.v + b * p.vb + g * p.vh;
     f32x16 o[DB];
 #pragma unroll
@@ -326,11 +399,10 @@ __device__ __forceinline__ void factors(const Backward &p, int64_t problem, int 
     __syncthreads();
     most_l = __builtin_fmaxf(__builtin_fmaxf(shared[0][0], shared[0][1]), __builtin_fmaxf(shared[0][2], shared[0][3]));
     most_g = __builtin_fmaxf(__builtin_fmaxf(shared[1][0], shared[1][1]), __builtin_fmaxf(shared[1][2], shared[1][3]));
-    // weights reach 2^6 times 1 / l and g v^T - delta 2 |g| |v|: an eighth of one leaves |v|
-    // up to 4000 (as in grad_q's kernel)
+    // (dS as in grad_q's kernel)
     up = most_l > 0.0f ? -__builtin_ceilf(log2_fast(most_l)) : 0.0f;
-    const float down = most_g > 0.0f && most_g < __builtin_inff() ? -__builtin_ceilf(log2_fast(most_g)) - 3.0f : 0.0f;
-    more = exp2_fast(within_range(down - up));
+    const float down = most_g > 0.0f && most_g < __builtin_inff() ? -__builtin_ceilf(log2_fast(most_g)) : 0.0f;
+    more = exp2_fast(within_range(down - 3.0f - (float)spread(p, problem, tid & 63) - up));
 }
 
 // A key's gradients of a wavefront (both halves' channels), or its part of them.
@@ -590,7 +662,7 @@ __global__ void __launch_bounds__(256, grad_q_waves(DP * elem_size(DT))) attend_
     row_fragments<DT, DP>(gf, p.g + b * p.ob + qi * p.orow + head * p.oh, row_there, p.D, lane);
     const RowData row = p.data[((int64_t)b * p.Hk + g) * p.rows + min(r, p.rows - 1)];
     const float c = p.scale * kLog2, mc = row.m * kLog2;   // weights are p l
-    const float inv = row_factor<DT>(row), off = -row.delta * inv;
+    const float inv = row_factor<DT>(p, row, (int64_t)b * p.Hk + g, lane), off = -row.delta * inv;
 
     f32x16 o[DB];
 #pragma unroll
@@ -1031,6 +1103,19 @@ uint64_t largest_bytes(const flashlayer_attention *a, const Plan &p)
     return align256((uint64_t)a->B * a->Hk * p.row_tiles * 8);
 }
 
+// keys to a tile of largest |v|
+int key_tile_of(const flashlayer_attention *a) { return std::max(128, ((a->Lk - 1) / kMostTiles + 16) / 16 * 16); }
+
+int key_tiles_of(const flashlayer_attention *a)
+{
+    return a->dtype == FLASHBEV_F16 && a->Lk ? (a->Lk - 1) / key_tile_of(a) + 1 : 0;
+}
+
+uint64_t values_bytes(const flashlayer_attention *a)
+{
+    return align256((uint64_t)a->B * a->Hk * key_tiles_of(a) * 4);
+}
+
 uint64_t backward_bytes(const flashlayer_attention *a, bool want_q, bool want_kv)
 {
     if (!a->B || !a->Lq || !a->H || !a->D) return 0;
@@ -1040,7 +1125,7 @@ uint64_t backward_bytes(const flashlayer_attention *a, bool want_q, bool want_kv
         q = size_prod({(uint64_t)p.q_splits, (uint64_t)a->B * a->Lq * a->H, (uint64_t)p.dp, 4});
     if (want_kv && p.k_splits > 1)
         kv = size_prod({2, (uint64_t)p.k_splits, (uint64_t)a->B * a->Lk * a->Hk, (uint64_t)p.dp, 4});
-    return copy_bytes(a, p) + data_bytes(a) + 2 * rows_bytes(a, p) + largest_bytes(a, p) + align256(std::max(q, kv));
+    return copy_bytes(a, p) + data_bytes(a) + 2 * rows_bytes(a, p) + largest_bytes(a, p) + values_bytes(a) + align256(std::max(q, kv));
 }
 
 bool rows_to_lds(const Backward &p)
@@ -1161,8 +1246,10 @@ int run_width(const flashlayer_attention *a, Backward &p, const Plan &plan, void
         }
     }
     const uint64_t tiles = size_prod({(uint64_t)p.B, (uint64_t)p.Hk, (uint64_t)plan.row_tiles});
+    const uint64_t tiles_v = size_prod({(uint64_t)p.B, (uint64_t)p.Hk, (uint64_t)p.key_tiles});
     p.row_blocks = (uint32_t)tiles;   // (launch_rows refuses what does not fit)
-    if (const int rc = launch_rows((const void *)attend_rows<DT>, tiles, 256, p, st)) return rc;
+    p.blocks_v = (uint32_t)tiles_v;
+    if (const int rc = launch_rows((const void *)attend_rows<DT>, tiles + tiles_v, 256, p, st)) return rc;
     switch (plan.dp) {
     case 32: return run<DT, 32>(p, plan, st);
     case 64: return run<DT, 64>(p, plan, st);
@@ -1243,7 +1330,11 @@ extern "C" int flashlayer_attention_backward(const flashlayer_attention *args, c
     p.delta = reinterpret_cast<float *>(ws);
     ws += rows_bytes(args, plan);
     p.largest = reinterpret_cast<float *>(ws);
-    p.part = reinterpret_cast<float *>(ws + largest_bytes(args, plan));
+    ws += largest_bytes(args, plan);
+    p.most_v = reinterpret_cast<float *>(ws);
+    p.key_tiles = key_tiles_of(args);
+    p.key_tile = key_tile_of(args);
+    p.part = reinterpret_cast<float *>(ws + values_bytes(args));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (a.dtype == FLASHBEV_F32) return run_width<FLASHBEV_F32>(args, p, plan, workspace, st);
     return a.dtype == FLASHBEV_F16 ? run_width<FLASHBEV_F16>(args, p, plan, workspace, st) : run_width<FLASHBEV_BF16>(args, p, plan, workspace, st);

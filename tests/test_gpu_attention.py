@@ -462,3 +462,57 @@ def test_gradients_of_many_problems():
             ref.check(r[n][s], want["grad_" + n], tol["grad_" + n], "grad_" + n)
     del out, rest, stats, r
     torch.cuda.empty_cache()
+
+
+def spread_of(v):
+    """The power of two that float16's dS loses for the largest row of v: 1 up to 2048 (the most of weights
+    of 2^6 and twice |v| over 8 is then 2^15), and as much more as that row passes it."""
+    most = v.detach().double().square().sum(-1).sqrt().amax().item()
+    return 2.0 ** max(0, math.ceil(math.log2(most)) - 11)
+
+
+def more_of(q, k, v, g):
+    """What float16's steps below its normal numbers add where dS is made smaller by ``spread_of``, per unit
+    of the bounds' own terms (with weights of one): n steps of 2^-25 of 8 |g|, rows of 16."""
+    d, share = q.shape[-1] ** -0.5 * 2.0 ** -25 * spread_of(v), q.shape[2] // k.shape[2]
+    norm = g.double().square().sum(-1).sqrt()
+    return {"q": d * k.shape[1] * 8 * norm[..., None] * k.double().abs().amax(),
+            "k": d * q.shape[1] * share * 16 * norm.amax() * q.double().abs().amax()}
+
+
+@pytest.mark.parametrize("size", [300.0, 2000.0, 60000.0])
+@pytest.mark.parametrize("kind", ["none", "lengths", "keys", "pairs", "add"])
+@pytest.mark.parametrize("shape", [(2, 70, 333, 4, 2, 32), (1, 150, 333, 2, 2, 64), (2, 5, 700, 4, 2, 63), (1, 130, 400, 2, 1, 128),
+                                   (1, 40, 2500, 2, 2, 96)], ids=lambda s: "x".join(map(str, s)))
+def test_large_values_in_float16(shape, kind, size):
+    """Values up to float16's largest: dS, of which the forward's reference may leave weights of 2^6, stays
+    within float16."""
+    B, Lq, Lk, H, Hk, D = shape
+    (q, k, v, g), gen = make(*shape, F16, seed=10)
+    # (values and gradients along one direction of each head: their products are as large as they get)
+    u = torch.where(torch.rand((Hk, D), generator=gen, device="cuda") < 0.5, -1.0, 1.0)
+    v = (v.float() * 0.01 + torch.rand((B, Lk, Hk, 1), generator=gen, device="cuda") * 2 - 1).mul(u).mul(size / 1.1).to(F16)
+    g = ((g.float() * 0.1 + 1) * u.repeat_interleave(H // Hk, 0) * 3 / size).to(F16)
+    # scores that grow by a few units behind the first keys, which the references follow late
+    q, k = (q.float().abs() * 0.5).to(F16), (k.float() * 0.3 + torch.linspace(0, 1.0, Lk, device="cuda")[None, :, None, None]).to(F16)
+    mask = some_masks(B, H, Lq, Lk, gen).get(kind)
+    lengths = torch.tensor([Lk, Lk // 2][:B], dtype=torch.int32, device="cuda") if kind == "lengths" else None
+    r = backward_checked(q, k, v, g, mask, lengths, more_of(q, k, v, g))
+    if kind in ("lengths", "keys"):   # keys that are left out have no say in it
+        gone = ~mask[:, 0, 0] if mask is not None else torch.arange(Lk, device="cuda") >= lengths[:, None]
+        for bad in (math.nan, math.inf, -65504.0):
+            kb, vb = k.clone(), v.clone()
+            kb[gone], vb[gone] = bad, bad
+            out, rest, stats = run_forward(q, kb, vb, mask=mask, key_lengths=lengths)
+            again = fb.attention_backward(g, q, kb, vb, out, stats, mask, lengths, rest=rest)
+            assert all(torch.equal(r[n], again[n]) for n in "qkv")
+
+
+def test_one_score_above_the_first_keys():
+    """float16, v of 30000: a weight of 2^5.5 above its reference, whose dS was infinite."""
+    q, k = torch.zeros((1, 64, 1, 32), device="cuda", dtype=F16), torch.zeros((1, 333, 1, 32), device="cuda", dtype=F16)
+    v, g = torch.zeros_like(k), torch.zeros_like(q)
+    q[..., 0], k[:, 200, :, 0] = 4.0, 3.8 * 32 ** 0.5 / 4.0
+    v[..., 1], v[:, 200, :, 1] = -30000.0, 30000.0
+    g[..., 1] = 0.01
+    backward_checked(q, k, v, g, more=more_of(q, k, v, g))
