@@ -86,8 +86,8 @@ __device__ __forceinline__ void put_param(char *p, int f32, int dt, int c, float
 
 // (mean, sum of squared differences) of n values joined with those of m others.  No difference of
 // large sums is taken.  The join's term d^2 carries the means' errors times 2 d, so means are kept
-// relative to a value of the group itself (its first channel at the first position), which an
-// offset far above the spread leaves small.
+// relative to a value of the group itself (pivot, below), which an offset far above the spread
+// leaves small.
 __device__ __forceinline__ void join(float &mean, float &sq, float n, float mean2, float sq2, float m)
 {
     const float tot = n + m;
@@ -99,11 +99,29 @@ __device__ __forceinline__ void join(float &mean, float &sq, float n, float mean
 
 constexpr int kBatch = 8;   // rows of a lane that are in flight together
 
-// The value that a group's means are relative to.
+// The value that a group's means are relative to: the middle one of its first channel's at the first,
+// middle and last position.  (The first alone cost the means 2^-24 of what it was away from the others.)
 template <int DT>
 __device__ __forceinline__ float pivot(const Group &p, int64_t n, int g)
 {
-    return load_elem<DT>(p.x + n * p.R * p.ldx * elem_size(DT), g * p.per);
+    const char *x = p.x + n * p.R * p.ldx * elem_size(DT);
+    return __builtin_amdgcn_fmed3f(load_elem<DT>(x, g * p.per), load_elem<DT>(x, (p.R - 1) / 2 * p.ldx + g * p.per),
+                                   load_elem<DT>(x, (p.R - 1) * p.ldx + g * p.per));
+}
+
+// The pivots of a lane's channels, of which the last is end - 1.
+template <int DT>
+__device__ __forceinline__ void pivots(const Group &p, int64_t n, int c, int end, float (&from)[Lane<DT>::V])
+{
+    constexpr int V = Lane<DT>::V;
+    if (p.per % V == 0) {   // (one group's)
+        from[0] = pivot<DT>(p, n, c / p.per);
+#pragma unroll
+        for (int i = 1; i < V; ++i) from[i] = from[0];
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) from[i] = pivot<DT>(p, n, min(c + i, end - 1) / p.per);
+    }
 }
 
 // Rows r, r + step, .. of a batch, in flight together: all eight, or the first `rows`.
@@ -160,10 +178,8 @@ __device__ __forceinline__ float lane_stats(const Group &p, int64_t n_, int c, i
     const char *x = p.x + n_ * p.R * p.ldx * L::ES;
     float n = 0.0f, from[L::V];
 #pragma unroll
-    for (int i = 0; i < L::V; ++i) {
-        mean[i] = sq[i] = 0.0f;
-        from[i] = pivot<DT>(p, n_, min(c + i, C - 1) / p.per);
-    }
+    for (int i = 0; i < L::V; ++i) mean[i] = sq[i] = 0.0f;
+    pivots<DT>(p, n_, c, C, from);
     const auto batch = [&](int64_t r, int rows, auto whole) {
         u32x4 raw[kBatch];
         float s[L::V], q[L::V];
@@ -461,8 +477,7 @@ __global__ void __launch_bounds__(kWhole) group_whole(Group p)
     Factors<DT> f;
     f.load_params(p, c, l.c1);
     float mean[L::V], sq[L::V], from[L::V], count = (float)mine;
-#pragma unroll
-    for (int i = 0; i < L::V; ++i) from[i] = pivot<DT>(p, n, min(c + i, l.c1 - 1) / p.per);
+    pivots<DT>(p, n, c, l.c1, from);
     batch_stats<DT>(raw, max(mine, 1), std::false_type{}, from, mean, sq);
     channel_stats<L::V, kWhole>(lds, channels, l, mean, sq, count);
     const int g0 = l.c0 / p.per;

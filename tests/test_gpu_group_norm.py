@@ -221,3 +221,28 @@ def test_no_channels(groups):
         x = torch.zeros(shape, device="cuda", requires_grad=True)
         (gx,) = torch.autograd.grad(fb.group_norm_autograd(x, 1), [x], torch.zeros_like(x))
         assert gx.shape == shape
+
+
+@pytest.mark.parametrize("R", [60, 5000, 60000])
+@pytest.mark.parametrize("where", [0, 0.3, 0.5, 1])
+def test_one_value_far_from_the_others(where, R):
+    """One position 1e5 spreads away, the first, middle and last one too: means lose no digits by it."""
+    x, w, b, gy = make(2, R, 64, F32, F32, mean=0.0)
+    x[:, int(where * (R - 1))] += 1e5
+    stats = torch.empty((2, 8, 2), device="cuda")
+    out = fb.group_norm_forward(x, 8, w, b, stats=stats)
+    t = x.double().reshape(2, R, 8, 8)
+    mean, var = t.mean((1, 3)), t.var((1, 3), correction=0)
+    rstd = (var + 1e-5).rsqrt()
+    # joins of some 16 roundings relative to the differences from a value among the others; rstd as in
+    # check_all, where a join's d^2 has 2 d times the means' errors
+    e_from = 16 * ref.U32 * (t - t.median(1, keepdim=True)[0][..., :1]).abs().mean((1, 3))
+    assert ((stats[..., 0].double() - mean).abs() <= e_from + ref.U32 * mean.abs()).all()
+    assert ((stats[..., 1].double() - rstd).abs() <= 40 * ref.U32 * rstd + rstd ** 2 * e_from).all()
+    want = ref.group_norm(x.double(), 8, w.double(), b.double(), "none")
+    wide = lambda s: s.repeat_interleave(8, -1)[:, None]   # noqa: E731
+    # x - mean rounded once, relative to x; rstd's error and some 8 roundings of the factors relative to y
+    xhat = (x.double() - wide(mean)) * wide(rstd)
+    tol = w.double().abs() * (wide(rstd * (e_from + ref.U32 * mean.abs())) + 2 * ref.U32 * x.double().abs() * wide(rstd)
+                              + xhat.abs() * (48 * ref.U32 + wide(rstd * e_from))) + 8 * ref.U32 * (want.abs() + b.double().abs())
+    ref.check(out, want, tol + 1e-30, "y")
