@@ -246,3 +246,12 @@ def test_one_value_far_from_the_others(where, R):
     tol = w.double().abs() * (wide(rstd * (e_from + ref.U32 * mean.abs())) + 2 * ref.U32 * x.double().abs() * wide(rstd)
                               + xhat.abs() * (48 * ref.U32 + wide(rstd * e_from))) + 8 * ref.U32 * (want.abs() + b.double().abs())
     ref.check(out, want, tol + 1e-30, "y")
+
+
+@pytest.mark.parametrize("dtype,pdt", TYPES, ids=IDS)
+@pytest.mark.parametrize("shape", [(1000, 49, 64, 8), (2500, 1, 96, 12), (300, 600, 33, 3)], ids=lambda s: "x".join(map(str, s)))
+def test_many_samples(shape, dtype, pdt):
+    """Region features and rows: weight's and bias's gradients are sums over all samples."""
+    N, R, C, groups = shape
+    x, w, b, gy = make(N, R, C, dtype, pdt, seed=4)
+    check_all(x, groups, w, b, gy, "relu" if R > 1 else "gelu")
