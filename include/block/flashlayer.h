@@ -53,7 +53,8 @@ typedef enum {
 
 /* An attention call's sizes, types and strides (in elements).  The channels of a head are
  * contiguous, and so are a mask's keys.  (Rows of q, k, v and grad_out may begin at any element; where all
- * begin at multiples of 16 bytes, long calls take up to half the time.) */
+ * begin at multiples of 16 bytes, long calls take up to half the time.)  Tiles, B Hk ((Lq H / Hk + 127) / 128) of
+ * queries' heads and in the backward B Hk ((Lk + 127) / 128) of keys, at most 2^24 - 8. */
 typedef struct {
     int64_t q_batch, q_row, q_head;        /* of q */
     int64_t k_batch, k_row, k_head;        /* of k */
@@ -74,7 +75,8 @@ typedef struct {
  *                Places left out by MASK_BOOL or by -inf get no weight.  A boolean mask
  *                that is the same for all queries and heads (mask_row and mask_head 0) leaves
  *                its keys out altogether, as key_lengths does: their k and v may hold anything.  (With
- *                other masks a NaN or infinite v reaches every query of its batch and head.)
+ *                other masks a NaN or infinite v reaches every query of its batch and head, a NaN or
+ *                infinite k their grad_q, and an infinite score with -inf added is no number.)
  *   key_lengths  [B] int32, or NULL: keys from key_lengths[b] on are left out and not read.
  *                Values are taken as within 0 .. Lk.
  *   out          [B, Lq, H, D] in dtype; every element is written once.

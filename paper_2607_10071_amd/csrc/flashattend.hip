@@ -97,7 +97,8 @@ __device__ __forceinline__ void put_row(const Forward &p, int b, int g, int spli
 // WQ = 4: a wavefront has 32 rows, the four of them share tiles of 64 keys.  WQ = 1: the
 // wavefronts share 32 rows and take 32 keys each of tiles of 128; their results are joined.
 // Few rows read each key once and little else: tokens of 8 sequences, 32 heads on 8 x 128 bf16, caches of
-// up to 8192: 195 MB read in 45 us, 4.3 TB/s.  With masks a wavefront's products, masks and exponentials wait for each
+// 3712 to 8192: 195 MB read in 45 us, 4.3 TB/s.  Each XCD has one of the sequences there, and the longest one's 34 MB
+// take as long.  With masks a wavefront's products, masks and exponentials wait for each
 // other: 3 x 777 queries by 1333 keys of 6 heads x 72 half with a bias 36 us, the matrix units
 // busy 10% of the time, the vector units 29%.
 template <int DT, int DP, int WQ>
@@ -322,15 +323,11 @@ __global__ void __launch_bounds__(256, DT == FLASHBEV_F32 && DP > 64 ? 1 : 2) at
 // and vector instructions that do not wait for each other, in turn.  (Scores, then weights, then
 // the product: 2048 queries of 32 heads x 4096 keys x 128 bf16 165 us.)
 //
-// Heads of 32 are bound by vector instructions, 16 exponentials of 8 clocks and some 40 others of 4 a
-// step beside 4 products of 32 each: 40000 queries x 8700 keys of 8 heads, bf16, 519 us, the vector units
-// busy 83% of the time, the matrix units 32%. Wide heads by both and what they wait for each
-// other: the case above 150 us, 49% each, 920 TFLOP/s.
-//
-// Heads of 32 are bound by vector instructions, 16 exponentials and some 60 more a step beside
-// 2 products of 32 clocks each: 40000 queries x 8700 keys of 8 heads, bf16, 519 us, vector units busy 83% of
-// the time and matrix units 32%. Wide heads by both and what they wait for each other: the case
-// above 150 us, 49% each, 920 TFLOP/s.
+// Heads of 32 are bound by vector instructions: by the counters a step has 16 exponentials of 8 clocks, 46
+// others of 4 and the issue of 4 products, 330 clocks of the 396 that it takes (16 of the others scale scores, 8
+// round weights, 8 sum them), and the products 128.  40000 queries x 8700 keys of 8 heads, bf16, 519 us at some 2.0
+// GHz, the vector units busy 83% of the time, the matrix units 32%. Wide heads by both and what they
+// wait for each other: the case above 150 us, 49% each, 920 TFLOP/s.
 template <int DT, int DP>
 struct Flow {
     static constexpr int TK = DP * elem_size(DT) <= 64 ? 128 : 64;
@@ -699,7 +696,7 @@ extern "C" int flashlayer_attention_forward(const flashlayer_attention *args, co
     const flashlayer_attention &a = *args;
     const int es = elem_size(a.dtype);
     if (!a.B || !a.Lq || !a.H) return FLASHBEV_OK;
-    if (!a.D) return a.D || !stats ? FLASHBEV_OK : FLASHBEV_ERR_UNSUPPORTED;
+    if (!a.D) return stats ? FLASHBEV_ERR_UNSUPPORTED : FLASHBEV_OK;
     if (!q || !out || (a.Lk && (!k || !v))) return FLASHBEV_ERR_NULLPTR;
     if (a.mask && a.Lk && !mask) return FLASHBEV_ERR_NULLPTR;
     if (!apart(a.B, a.o_batch, a.Lq, a.o_row, a.H, a.o_head, a.D)) return FLASHBEV_ERR_SHAPE;

@@ -247,12 +247,13 @@ struct ShapeQ {
     static constexpr int STAGE = 2 * P::BYTES, LDS = 2 * STAGE;
 };
 
-// Workgroups that are to run on a CU at once of the kernels with masks.  (Two of heads of 96 half
-// channels, of which the compiler spills some registers, hide what one waits for: the gradients at
-// splits_of grad_q 50 -> 38 us, grad_k and grad_v 78 -> 61.)
+// Workgroups that are to run on a CU at once of the kernels with masks: two, whose wavefronts fill what one
+// waits for, where 256 registers nearly do.  (They do up to heads of 64 16-bit channels; of 96 grad_k's and
+// grad_v's kernel spills 41: the gradients at splits_of grad_q 50 -> 38 us, grad_k and grad_v 78 -> 61.  Heads of
+// 128 would spill 112 and 191.)
 constexpr int masked_waves(int bytes) { return bytes > 192 ? 1 : 2; }
 
-template <int DT, int DP, bool MASK>
+template <int DT, int DP>
 __global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_grad_q(Backward p)
 {
     using S = ShapeQ<DT, DP>;
@@ -283,9 +284,7 @@ __global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_
     row_fragments<DT, DP>(gf, p.g + b * p.ob + qi * p.orow + head * p.oh, row_there, p.D, lane);
     const char *mrow = p.mask + b * p.mb + head * p.mh + qi * p.mr;
     const RowData row = p.data[((int64_t)b * p.Hk + g) * p.rows + min(r, p.rows - 1)];
-    const float c = (MASK ? 1.0f : p.scale) * kLog2;
-    // weights are p l; an empty row's are exp(-inf - 0) = 0
-    const float mc = row.m * kLog2;
+    // (weights are p l; an empty row's are exp(-inf - 0) = 0)
     const float inv = row_factor<DT>(p, row, (int64_t)b * p.Hk + g, lane), off = -row.delta * inv;
     const char *kbase = p.k + b * p.kb + g * p.kh, *vbase = p.v + b * p.vb + g * p.vh;
     f32x16 o[DB];
@@ -300,7 +299,7 @@ __global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_
     u32x4 kv[P::G], vv[P::G];
     km.clear(kv);
     vm.clear(vv);
-    const bool copies = MASK && (p.drops || p.D % P::E != 0);
+    const bool copies = p.drops || p.D % P::E != 0;
     auto fetch = [&](int t) {
         if (copies) return;
         const int k0 = t * S::BK;
@@ -330,18 +329,18 @@ __global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_
         for (int n = 0; n < 2; ++n) {
             const int k0 = t * S::BK + n * 32;
             f32x16 x = zeros16(), y = zeros16();
-            [[maybe_unused]] MaskBlock mask;
-            if constexpr (MASK) mask.load_row(p, mrow, k0, h);
+            MaskBlock mask;
+            mask.load_row(p, mrow, k0, h);
 #pragma unroll
             for (int e = 0; e < P::CHUNKS; ++e) {
                 mma<DT>(x, read.along(lk, n * 32, e), qf[e]);
                 mma<DT>(y, read.along(lv, n * 32, e), gf[e]);
             }
-            if constexpr (MASK) mask.apply_row(p, x);
+            mask.apply_row(p, x);
             if (k0 + 32 > len) cut_keys(x, k0, h, len);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float w = MASK ? exp2_fast((x[i] - row.m) * c) : exp2_fast(__builtin_fmaf(x[i], c, -mc));
+                const float w = exp2_fast((x[i] - row.m) * kLog2);
                 x[i] = w * __builtin_fmaf(y[i], inv, off);
             }
 #pragma unroll
@@ -1142,7 +1141,7 @@ int run(Backward &p, const Plan &plan, hipStream_t st)
         p.tiles = plan.q_tiles;
         p.splits = plan.q_splits;
         if (const int rc = deal(p, size_prod({problems, (uint64_t)p.tiles, (uint64_t)p.splits}))) return rc;
-        const void *fn = (const void *)attend_grad_q<DT, DP, true>;
+        const void *fn = (const void *)attend_grad_q<DT, DP>;
         size_t lds = ShapeQ<DT, DP>::LDS;
         if constexpr (FlowK<DT, DP>::ROOM) {
             if (!plan.any && keys_to_lds(p)) {
