@@ -10,7 +10,10 @@
 // over the keys, one with keys across sums grad_k and grad_v over the rows.  Five products
 // in one kernel would leave grad_q to float atomics, whose order changes results.
 //
-// Digits.  p and dS are rounded to the inputs' type for their products.  bfloat16 has float32's
+// Digits.  p and dS are rounded to the inputs' type for their products: 900 x 40000 of 8 heads x 32 bf16 has
+// grad_q off by 0.0025 of its norm, where the rounding of grad_q itself makes 0.0017, that of dS another 0.0018
+// and the forward's rounded weights, in delta, 0.0005.  (dS in two terms would take 14 to 18% more of grad_q's
+// kernel.)  bfloat16 has float32's
 // range; float16 loses digits below 6e-5, where weights of one in 40000 and scaled losses'
 // gradients lie, so its factors are kept near one: grad_q's kernel takes p l (at most 2^6) and
 // g / (8 |g|), a row's factors coming back at the end; the other one takes p and dS times powers of

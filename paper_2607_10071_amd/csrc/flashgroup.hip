@@ -743,7 +743,7 @@ Cut cut(const flashlayer_group_norm *a, bool backward)
     const int es = elem_size(a->dtype), V = 16 / es, per = a->C / a->groups;
     Cut c{};
     // whole groups of 64 bytes or more to one workgroup, eight rows at most to its lanes (six samples
-    // of 704 x 32 float32 8.8 us a call, 13.9 in three launches; eight of 128 x 1024 bf16 10.0 and 20.5)
+    // of 704 x 32 float32 8.9 us a call, 13.9 in three launches; eight of 128 x 1024 bf16 9.5 and 20.5)
     const int some = std::min(((64 / es + per - 1) / per) * per, a->C);
     if (!backward && some <= kWhole && a->R <= kBatch * (kWhole / ((some + V - 1) / V))) {
         c.whole = true;

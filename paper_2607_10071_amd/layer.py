@@ -159,7 +159,8 @@ def attention_forward(q, k, v, mask=None, key_lengths=None, scale=None, out=None
 
     q            CUDA tensor [B, Lq, H, D] (float32, float16 or bfloat16), D at most 128,
                  its channels contiguous, any other strides: a product's [B, Lq, H D] rows
-                 seen as heads, say.  Where rows, or the heads of q, lie more than 2^20 elements
+                 seen as heads, say (long calls are up to twice as fast where all rows begin at
+                 multiples of 16 bytes).  Where rows, or the heads of q, lie more than 2^20 elements
                  apart a copy is read (prepared calls and outputs are refused).
     k, v         [B, Lk, Hk, D] in q's dtype, strides likewise (the halves of one projection,
                  a cache longer than what it holds); query head h reads head h // (H / Hk).
