@@ -253,7 +253,7 @@ struct ShapeQ {
 // Workgroups that are to run on a CU at once of the kernels with masks: two, whose wavefronts fill what one
 // waits for, where 256 registers nearly do.  (They do up to heads of 64 16-bit channels; of 96 grad_k's and
 // grad_v's kernel spills 41: the gradients at splits_of grad_q 50 -> 38 us, grad_k and grad_v 78 -> 61.  Heads of
-// 128 would spill 112 and 191.)
+// 128 take 368 and 447.)
 constexpr int masked_waves(int bytes) { return bytes > 192 ? 1 : 2; }
 
 template <int DT, int DP>
