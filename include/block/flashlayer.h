@@ -106,8 +106,9 @@ int flashlayer_attention_workspace_size(const flashlayer_attention *args, uint64
  *   grad_q = scale dS k,   grad_k = scale dS^T q,   grad_v = p^T grad_out
  *
  * (k's and v's summed over the query heads that share them).  p and dS are rounded to dtype
- * for the products; float16 ones first take powers of two by the largest |grad_out|, 1 / sum exp(s - m)
- * and, above 2^11, |v| of a batch's head of the states (keys that are left out altogether aside), so that none
+ * for the products; float16 ones first take powers of two by the largest |grad_out| and
+ * 1 / sum exp(s - m), and above 2^11 by |v|, of a key for its own gradients and for grad_q the largest of a
+ * batch's head of the states (keys that are left out altogether aside), so that none
  * overflows and small ones keep digits.  The mask gets no gradient.
  *
  *   args         as in the forward, with grad_out's strides as o_*.

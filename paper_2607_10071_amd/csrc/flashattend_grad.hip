@@ -18,7 +18,7 @@
 // gradients lie, so its factors are kept near one: grad_q's kernel takes p l (at most 2^6) and
 // g / (8 |g|), a row's factors coming back at the end; the other one takes p and dS times powers of
 // two that bring the largest 1 / l and |g| / l of its rows to about one.  Both divide by one more for each
-// power of two of |v| above 2^11 (`spread`).
+// power of two of |v| above 2^11, of a problem's largest or of each key's own (`spread`).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -47,7 +47,7 @@ struct Backward : Attend {
     const char *out, *rest;   // [B, Lq, H, D]; rest null: none
     const float *stats;
     RowData *data;            // [B Hk][rows]
-    float *largest;           // float16: [B Hk][padded / 16][2], the largest 1 / l and |g| / l of 16 rows
+    float *largest;           // float16: [B Hk][padded / 16][3], the largest 1 / l, |g| / l and |out| of 16 rows
     // [B Hk][padded rows] each, for grad_k's and grad_v's kernel without masks: the exponent that a
     // row's weights lose, m log2(e) + log2(l), infinite past the last row; and delta
     float *lose, *delta;
@@ -81,11 +81,18 @@ constexpr int kRowTile = 16;
 constexpr int kMostTiles = 256;   // of largest |v|: four loads of a wavefront
 
 // How many powers of two float16's dS is made smaller by for large values.  Weights p l reach 2^6 (a
-// forward's reference may lag so far) and |g v^T - delta| is at most 2 |g| |v|: an eighth of one for
-// |g| keeps their product within 2^15 up to |v| = 2^11, and each power of two of the problem's largest |v|
-// above that takes another one.  (float16's largest, in 128 channels, takes 9; a |v| that is infinite
-// makes dS what it makes it.)
-__device__ __forceinline__ int spread(const Backward &p, int64_t problem, int lane)
+// forward's reference may lag so far) and |g v^T - delta| is at most |g| (|v| + |out|): an eighth of one for
+// |g| keeps their product within 2^15 up to |v| + |out| = 2^12, and each power of two above that takes another
+// one.  (float16's largest, in 128 channels, takes 9; what is infinite makes dS what it makes it.)
+__device__ __forceinline__ int spread(float sizes)
+{
+    int e = 0;
+    while (e < 9 && sizes > (float)(4096 << e)) ++e;
+    return e;
+}
+
+// The same by a problem's largest |v|, which no |out| passes.
+__device__ __forceinline__ int spread_of_values(const Backward &p, int64_t problem, int lane)
 {
     float most = 0.0f;
 #pragma unroll
@@ -93,9 +100,23 @@ __device__ __forceinline__ int spread(const Backward &p, int64_t problem, int la
         if (i < p.key_tiles) most = __builtin_fmaxf(most, p.most_v[problem * p.key_tiles + i]);
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, o));
-    int e = 0;
-    while (e < 9 && most > (float)(2048 << e)) ++e;
-    return e;
+    return spread(2.0f * most);
+}
+
+// The same by a key's |v|, of its lane's fragments and the other half's, and its rows' largest |out|.
+template <int N>
+__device__ __forceinline__ int spread_of_key(const u32x4 (&vf)[N], float most_out)
+{
+    float sq = 0.0f;
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        const u32x4 w[1] = {vf[c]};
+        float v[8];
+        elems_of<FLASHBEV_F16>(w, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sq = __builtin_fmaf(v[i], v[i], sq);
+    }
+    return spread(sqrtf(both_sum(sq)) + most_out);
 }
 
 // What a row's dS is multiplied by for grad_q's product.  float16 alone needs it: bfloat16 and float32
@@ -104,7 +125,7 @@ template <int DT>
 __device__ __forceinline__ float row_factor(const Backward &p, const RowData &row, int64_t problem, int lane)
 {
     if constexpr (DT == FLASHBEV_F16) {
-        const float least = __builtin_ldexpf(0.125f, -spread(p, problem, lane));
+        const float least = __builtin_ldexpf(0.125f, -spread_of_values(p, problem, lane));
         return row.norm > 0.0f ? least / row.norm : 1.0f;
     }
     return 1.0f;
@@ -156,7 +177,7 @@ template <int DT>
 __global__ void __launch_bounds__(256) attend_rows(Backward p)
 {
     constexpr int ES = elem_size(DT), E = 16 / ES;
-    __shared__ float lds[2][4];
+    __shared__ float lds[3][4];
     const uint32_t id = block_index();
     if constexpr (DT == FLASHBEV_F16) {
         if (id >= p.row_blocks) {
@@ -168,7 +189,7 @@ __global__ void __launch_bounds__(256) attend_rows(Backward p)
     const int tile = id % p.row_tiles, problem = id / p.row_tiles;
     const int b = problem / p.Hk, g = problem - b * p.Hk;
     const int part = threadIdx.x & 15;
-    float most_l = 0.0f, most_g = 0.0f;
+    float most_l = 0.0f, most_g = 0.0f, most_out = 0.0f;
     const int r = tile * kRowTile + (threadIdx.x >> 4);
     if (r < p.rows) {   // (whole groups of 16 lanes)
         int qi, qj;
@@ -176,7 +197,7 @@ __global__ void __launch_bounds__(256) attend_rows(Backward p)
         const int head = g * p.share + qj;
         const char *gr = p.g + b * p.ob + qi * p.orow + head * p.oh;
         const int64_t at = (((int64_t)b * p.Lq + qi) * p.H + head) * p.D;
-        float delta = 0.0f, sq = 0.0f;
+        float delta = 0.0f, sq = 0.0f, sq_out = 0.0f;
         for (int d = part * E; d < p.D; d += 16 * E) {
             float vg[E], vo[E], vr[E];
             u32x4 w[1] = {load_granule_edge<DT>(gr, d, p.D)};
@@ -191,13 +212,17 @@ __global__ void __launch_bounds__(256) attend_rows(Backward p)
             for (int i = 0; i < E; ++i) {
                 delta = __builtin_fmaf(vg[i], vo[i], delta);
                 if (p.rest) delta = __builtin_fmaf(vg[i], vr[i], delta);
-                if constexpr (DT == FLASHBEV_F16) sq = __builtin_fmaf(vg[i], vg[i], sq);
+                if constexpr (DT == FLASHBEV_F16) {
+                    sq = __builtin_fmaf(vg[i], vg[i], sq);
+                    sq_out = __builtin_fmaf(vo[i], vo[i], sq_out);
+                }
             }
         }
 #pragma unroll
         for (int o = 1; o < 16; o *= 2) {
             delta += __shfl_xor(delta, o);
             sq += __shfl_xor(sq, o);
+            sq_out += __shfl_xor(sq_out, o);
         }
         const float *st = p.stats + (((int64_t)b * p.H + head) * p.Lq + qi) * 2;
         RowData row;
@@ -213,6 +238,7 @@ __global__ void __launch_bounds__(256) attend_rows(Backward p)
             const float inv = exp2_fast(-row.log2l);
             most_l = __builtin_fmaxf(most_l, inv);
             most_g = __builtin_fmaxf(most_g, row.norm * inv);
+            most_out = __builtin_fmaxf(most_out, sqrtf(sq_out));
         }
         if (part == 0) {
             p.data[(int64_t)problem * p.rows + r] = row;
@@ -227,16 +253,18 @@ __global__ void __launch_bounds__(256) attend_rows(Backward p)
     for (int o = 16; o < 64; o *= 2) {
         most_l = __builtin_fmaxf(most_l, __shfl_xor(most_l, o));
         most_g = __builtin_fmaxf(most_g, __shfl_xor(most_g, o));
+        most_out = __builtin_fmaxf(most_out, __shfl_xor(most_out, o));
     }
     if ((threadIdx.x & 63) == 0) {
         lds[0][threadIdx.x >> 6] = most_l;
         lds[1][threadIdx.x >> 6] = most_g;
+        lds[2][threadIdx.x >> 6] = most_out;
     }
     __syncthreads();
-    if (threadIdx.x < 2) {
+    if (threadIdx.x < 3) {
         float v = lds[threadIdx.x][0];
         for (int w = 1; w < 4; ++w) v = __builtin_fmaxf(v, lds[threadIdx.x][w]);
-        p.largest[2 * (int64_t)id + threadIdx.x] = v;
+        p.largest[3 * (int64_t)id + threadIdx.x] = v;
     }
 }
 
@@ -377,34 +405,37 @@ __global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_
 // ---------------------------------------------------------------------------
 // grad_k and grad_v: 32 keys across to a wavefront, tiles of rows
 // ---------------------------------------------------------------------------
-// float16's factors (above) for rows r0 .. r1 - 1 of a problem: 2^up and 2^up times `more`.
-__device__ __forceinline__ void factors(const Backward &p, int64_t problem, int r0, int r1, float (&shared)[2][4],
-                                        float &up, float &more)
+// float16's factors (above) for rows r0 .. r1 - 1 of a problem: 2^up and 2^up times `more`, and times `key` of a
+// lane's key.
+template <int N>
+__device__ __forceinline__ void factors(const Backward &p, int64_t problem, int r0, int r1, const u32x4 (&vf)[N],
+                                        float (&shared)[3][4], float &up, float &more, float &key)
 {
     const int tid = threadIdx.x, wave = tid >> 6;
-    float most_l = 0.0f, most_g = 0.0f;
-    const float *at = p.largest + problem * p.row_tiles * 2;
+    float most[3] = {0.0f, 0.0f, 0.0f};
+    const float *at = p.largest + problem * p.row_tiles * 3;
     const int s1 = min(p.row_tiles, (r1 + kRowTile - 1) / kRowTile);
-    for (int s = r0 / kRowTile + tid; s < s1; s += 256) {
-        most_l = __builtin_fmaxf(most_l, at[2 * s]);
-        most_g = __builtin_fmaxf(most_g, at[2 * s + 1]);
-    }
+    for (int s = r0 / kRowTile + tid; s < s1; s += 256)
 #pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        most_l = __builtin_fmaxf(most_l, __shfl_xor(most_l, o));
-        most_g = __builtin_fmaxf(most_g, __shfl_xor(most_g, o));
-    }
-    if ((tid & 63) == 0) {
-        shared[0][wave] = most_l;
-        shared[1][wave] = most_g;
+        for (int i = 0; i < 3; ++i) most[i] = __builtin_fmaxf(most[i], at[3 * s + i]);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) most[i] = __builtin_fmaxf(most[i], __shfl_xor(most[i], o));
+        if ((tid & 63) == 0) shared[i][wave] = most[i];
     }
     __syncthreads();
-    most_l = __builtin_fmaxf(__builtin_fmaxf(shared[0][0], shared[0][1]), __builtin_fmaxf(shared[0][2], shared[0][3]));
-    most_g = __builtin_fmaxf(__builtin_fmaxf(shared[1][0], shared[1][1]), __builtin_fmaxf(shared[1][2], shared[1][3]));
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        most[i] = __builtin_fmaxf(__builtin_fmaxf(shared[i][0], shared[i][1]), __builtin_fmaxf(shared[i][2], shared[i][3]));
     // (dS as in grad_q's kernel)
-    up = most_l > 0.0f ? -__builtin_ceilf(log2_fast(most_l)) : 0.0f;
-    const float down = most_g > 0.0f && most_g < __builtin_inff() ? -__builtin_ceilf(log2_fast(most_g)) : 0.0f;
-    more = exp2_fast(within_range(down - 3.0f - (float)spread(p, problem, tid & 63) - up));
+    const auto same = [](float v) {   // in all lanes
+        return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+    };
+    up = same(most[0] > 0.0f ? -__builtin_ceilf(log2_fast(most[0])) : 0.0f);
+    const float down = most[1] > 0.0f && most[1] < __builtin_inff() ? -__builtin_ceilf(log2_fast(most[1])) : 0.0f;
+    more = same(exp2_fast(within_range(down - 3.0f - up)));
+    key = __builtin_ldexpf(1.0f, -spread_of_key(vf, most[2]));
 }
 
 // A key's gradients of a wavefront (both halves' channels), or its part of them.
@@ -458,7 +489,7 @@ __global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_
     using P = typename S::P;
     constexpr int DB = DP / 32;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ float shared[2][4];
+    __shared__ float shared[3][4];
 
     uint32_t id = item_of(p);
     if (id >= p.blocks) return;
@@ -479,15 +510,17 @@ __global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_
     const int per = (all + p.splits - 1) / p.splits;
     const int t0 = split * per, t1 = min(all, t0 + per);
 
-    // the factors of p and dS: 2^up and 2^up times `more`
-    float up = 0.0f, more = 1.0f;
-    if constexpr (DT == FLASHBEV_F16) factors(p, problem, t0 * S::BR, t1 * S::BR, shared, up, more);
-
     u32x4 kf[P::CHUNKS], vf[P::CHUNKS];
     const int64_t key_at = min(key, p.Lk - 1);
     row_fragments<DT, DP>(kf, p.k + b * p.kb + g * p.kh + key_at * p.kr, key_there, p.D, lane);
     row_fragments<DT, DP>(vf, p.v + b * p.vb + g * p.vh + key_at * p.vr, key_there, p.D, lane);
     const float c = (MASK ? 1.0f : p.scale) * kLog2;
+    // the factors of p and dS: 2^up and 2^up `more`, which all keys have but for large values' own
+    float up = 0.0f, all_keys = 1.0f, of_key = 1.0f;
+    if constexpr (DT == FLASHBEV_F16) factors(p, problem, t0 * S::BR, t1 * S::BR, vf, shared, up, all_keys, of_key);
+    // (large values are rare: without masks vector instructions are what bounds this, with them registers)
+    const float more = MASK ? all_keys : all_keys * of_key;
+    const bool large = DT == FLASHBEV_F16 && !MASK && __any(of_key != 1.0f);
 
     f32x16 ok[DB], ov[DB];
 #pragma unroll
@@ -544,7 +577,7 @@ __global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_
             const float e = there ? rd.log2l - up : __builtin_inff();
             f[tid] = there ? rd.m : 0.0f;
             f[S::BR + tid] = MASK || !there ? e : __builtin_fmaf(rd.m, kLog2, e);
-            f[2 * S::BR + tid] = there ? rd.delta * more : 0.0f;
+            f[2 * S::BR + tid] = there ? rd.delta * all_keys : 0.0f;
         }
         if (!copies) {
             mover.store(qv, lq);
@@ -589,7 +622,12 @@ __global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const f32x4 e4 = *reinterpret_cast<const f32x4 *>(f + S::BR + 8 * k);
-                const f32x4 d4 = *reinterpret_cast<const f32x4 *>(f + 2 * S::BR + 8 * k);
+                f32x4 d4 = *reinterpret_cast<const f32x4 *>(f + 2 * S::BR + 8 * k);
+                if (large) {
+                    asm volatile("");   // (a branch, not selections)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) d4[i] *= of_key;
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float s = x[4 * k + i];
@@ -599,6 +637,7 @@ __global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_
                         s = exp2_fast(__builtin_fmaf(s, c, -e4[i]));
                     }
                     x[4 * k + i] = s;
+                    if constexpr (DT == FLASHBEV_F16 && MASK) s *= of_key;
                     y[4 * k + i] = s * __builtin_fmaf(y[4 * k + i], more, -d4[i]);
                 }
             }
@@ -613,7 +652,7 @@ __global__ void __launch_bounds__(256, masked_waves(DP * elem_size(DT))) attend_
             }
         }
     }
-    put_key<DT, DP>(p, b, g, split, key, key_there, up, more, ok, ov, h);
+    put_key<DT, DP>(p, b, g, split, key, key_there, up, all_keys * of_key, ok, ov, h);
 }
 
 // ---------------------------------------------------------------------------
@@ -833,7 +872,7 @@ __global__ void __launch_bounds__(256, grad_kv_waves(DP * elem_size(DT))) attend
     using T = typename F::T;
     constexpr int DB = DP / 32, PAIRS = 8, E = T::E;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ float shared[2][4];
+    __shared__ float shared[3][4];
 
     uint32_t id = item_of(p);
     if (id >= p.blocks) return;
@@ -853,16 +892,17 @@ __global__ void __launch_bounds__(256, grad_kv_waves(DP * elem_size(DT))) attend
     const int all = tile * 128 < len ? (p.rows + F::TR - 1) / F::TR : 0;
     const int per = (all + p.splits - 1) / p.splits;
     const int t0 = split * per, t1 = min(all, t0 + per);
-    float up = 0.0f, more = 1.0f;
-    if constexpr (DT == FLASHBEV_F16) {
-        factors(p, problem, t0 * F::TR, t1 * F::TR, shared, up, more);
-    }
-
     u32x4 kf[T::CHUNKS], vf[T::CHUNKS];
     const int64_t key_at = min(key, p.Lk - 1);
     row_fragments<DT, DP>(kf, p.k + b * p.kb + g * p.kh + key_at * p.kr, key_there, p.D, lane);
     row_fragments<DT, DP>(vf, p.v + b * p.vb + g * p.vh + key_at * p.vr, key_there, p.D, lane);
     const float c = p.scale * kLog2;
+    float up = 0.0f, more = 1.0f;
+    if constexpr (DT == FLASHBEV_F16) {
+        float of_key;
+        factors(p, problem, t0 * F::TR, t1 * F::TR, vf, shared, up, more, of_key);
+        more *= of_key;
+    }
 
     f32x16 ok[DB], ov[DB];
 #pragma unroll
@@ -1102,7 +1142,7 @@ uint64_t copy_bytes(const flashlayer_attention *a, const Plan &p)
 
 uint64_t largest_bytes(const flashlayer_attention *a, const Plan &p)
 {
-    return align256((uint64_t)a->B * a->Hk * p.row_tiles * 8);
+    return align256((uint64_t)a->B * a->Hk * p.row_tiles * 12);
 }
 
 // keys to a tile of largest |v|
@@ -1248,7 +1288,7 @@ int run_width(const flashlayer_attention *a, Backward &p, const Plan &plan, void
         }
     }
     const uint64_t tiles = size_prod({(uint64_t)p.B, (uint64_t)p.Hk, (uint64_t)plan.row_tiles});
-    const uint64_t tiles_v = size_prod({(uint64_t)p.B, (uint64_t)p.Hk, (uint64_t)p.key_tiles});
+    const uint64_t tiles_v = p.gq ? size_prod({(uint64_t)p.B, (uint64_t)p.Hk, (uint64_t)p.key_tiles}) : 0;   // (grad_q's)
     p.row_blocks = (uint32_t)tiles;   // (launch_rows refuses what does not fit)
     p.blocks_v = (uint32_t)tiles_v;
     if (const int rc = launch_rows((const void *)attend_rows<DT>, tiles + tiles_v, 256, p, st)) return rc;

@@ -516,3 +516,20 @@ def test_one_score_above_the_first_keys():
     v[..., 1], v[:, 200, :, 1] = -30000.0, 30000.0
     g[..., 1] = 0.01
     backward_checked(q, k, v, g, more=more_of(q, k, v, g))
+
+
+@pytest.mark.parametrize("D", [32, 64, 96, 128])
+@pytest.mark.parametrize("kind", ["inf", "pairs"])
+def test_large_values_behind_masks_of_rows_in_float16(kind, D):
+    """Keys that an added mask, or one for each row, leaves out for all rows: their values take nothing from the
+    other keys' gradients."""
+    (q, k, v, g), gen = make(2, 90, 300, 4, 2, D, F16, seed=11)
+    gone = torch.rand((2, 1, 1, 300), generator=gen, device="cuda") < 0.3
+    mask = torch.zeros((2, 1, 90, 300), device="cuda").masked_fill(gone, -math.inf)
+    if kind == "pairs":
+        mask = mask == 0
+    far = v.clone()
+    far[gone[:, 0, 0]] = 60000.0
+    clean = backward_checked(q, k, v, g, mask)
+    r = backward_checked(q, k, far, g, mask, more=more_of(q, k, far, g))
+    assert torch.equal(r["k"], clean["k"]) and torch.equal(r["v"], clean["v"])
